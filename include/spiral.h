@@ -49,6 +49,12 @@ extern "C" {
 #define SPIRAL_WEIGHT_FP32 0
 #define SPIRAL_WEIGHT_BF16 1
 
+/* element types of the buffers of the sampler with given numbers, the policy gradient and the optimiser */
+#define SPIRAL_DTYPE_FP32 0
+#define SPIRAL_DTYPE_BF16 1
+#define SPIRAL_DTYPE_FP16 2
+#define SPIRAL_DTYPE_E4M3 3          /* optimiser states only: 8-bit floats (4 exponent, 3 mantissa bits) under a scale per block */
+
 #define SPIRAL_MAX_BATCH 1024        /* sequences per prefill / decode / sample call */
 
 /* Decoder geometry.  The paper names its policies only by model family (Sec. 4,
@@ -299,6 +305,101 @@ int spiral_sample_truncated_ws(const float* dev_logits, int B, int V, float temp
                                uint64_t seed, const int32_t* host_seq_ids, const int32_t* host_steps,
                                const float* dev_noise, int32_t* dev_out_tokens, float* dev_threshold_out,
                                void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* ---- sampling from given uniform numbers ---------------------------------------------------------
+ * One token a row by the inverse of the cumulative distribution, with the log-probability under which it was drawn (the
+ * old policy's in the ratio of the objective below).  Every row has its own settings, so that one call serves a batch of
+ * requests.  With m = max_v logit_v and w_v = exp((logit_v - m) / T), evaluated in 64 bits:
+ *     top_k in (0, V): keep the logits that are no less than the k-th largest                (<= 0 or >= V: off)
+ *     top_p in (0, 1): over the top-k survivors, walk the logits in descending order and stop where the running sum of w
+ *                      first reaches top_p times their sum; keep the logits that are no less than that one  (1: off)
+ *     min_p in (0, 1]: keep w_v >= min_p                                                     (0: off)
+ *     token = the least v whose running sum of the kept w_0 .. w_v exceeds u times their whole sum
+ *     logp  = log( w_token / sum of the kept w )
+ * Equal logits are kept or dropped together.  T == 0 is greedy: the lowest index of the maximum, logp 0, cuts and u ignored.
+ * An undefined logit counts as -inf and is never drawn; logits of +inf share all of the mass; a row with nothing above
+ * -inf gives token 0 with logp -inf.  u is meant to be uniform in [0, 1): less (or NaN) counts as 0, more as the number below 1.
+ * A row's results depend on that row alone, not on the batch it is in, and repeat bit for bit.
+ * dev_logits: [B, V] of logits_dtype (SPIRAL_DTYPE_FP32, _BF16 or _FP16), rows row_stride >= V elements apart, aligned to an
+ * element.  host_temperature, host_top_k, host_top_p, host_min_p: [B] each, consumed before the call returns, or NULL for 1, off,
+ * off, off.  dev_uniform: fp32 [B], read when the kernels run: a captured call that is replayed draws from what stands there then.
+ * dev_out_tokens: int32 [B]; dev_out_logp: fp32 [B] or NULL.  dev_workspace: 256-byte aligned,
+ * spiral_sample_uniform_workspace_bytes(B, V) bytes (0 for an invalid B or V), contents undefined before and after; calls that share it
+ * must be ordered on one stream.
+ * Errors: INVALID_ARG (null or misaligned pointer, B outside [1, SPIRAL_MAX_BATCH], V < 1, unknown type, row_stride < V, temperature
+ * negative or not finite, top_p outside (0, 1], min_p outside [0, 1], workspace too small), HIP. */
+size_t spiral_sample_uniform_workspace_bytes(int B, int V);
+int spiral_sample_uniform(const void* dev_logits, int logits_dtype, long long row_stride, int B, int V,
+                          const float* host_temperature, const int32_t* host_top_k, const float* host_top_p,
+                          const float* host_min_p, const float* dev_uniform, void* dev_workspace, size_t workspace_bytes,
+                          int32_t* dev_out_tokens, float* dev_out_logp, void* stream);
+
+/* ---- gradient of the policy objective (learner side) ---------------------------------------------
+ * For the learner's own logits of n_rows tokens, with z = logit / temperature and y the row's target:
+ *     logp_t = z_y - log sum_v exp(z_v) ,  r_t = exp(logp_t - old_t)
+ *     J      = sum_t mask_t * min( r_t * A_t, clip(r_t, 1 - clip_eps, 1 + clip_eps) * A_t )
+ * (dev_logp_old NULL: J = sum_t mask_t * A_t * logp_t, the REINFORCE sum), the call returns every logp_t and the gradient of
+ * the loss -scale * J in the logits:
+ *     grad[t, v] = -scale * mask_t * A_t * r_t * [r_t A_t <= clip(r_t) A_t] * (1{v = y_t} - softmax(z_t)_v) / temperature
+ * (without the ratio and the bracket where dev_logp_old is NULL).  spiral_policy_objective gives the values of J from dev_logp.
+ * Rows with mask 0 or a target < 0 count for nothing: logp 0, a gradient row of zeros, their logits are not read.  A target
+ * >= V, a NaN or +inf logit or a row without any above -inf leaves that row's logp, and its gradient, NaN.  Sums are fp32
+ * or more; the gradient is rounded once, to the logits' type.  Results repeat bit for bit.
+ * dev_logits [n_rows, V], rows row_stride apart, dev_grad [n_rows, V], rows grad_stride apart, both of `dtype` (SPIRAL_DTYPE_FP32, _BF16,
+ * _FP16) and aligned to an element; the gradient may be written in place (same pointer, same stride) but not overlap the logits in another way.
+ * dev_targets int32, dev_logp_old fp32 or NULL, dev_advantage fp32, dev_mask int32 or NULL, dev_logp fp32: [n_rows] each.
+ * dev_workspace: 256-byte aligned, spiral_policy_gradient_workspace_bytes(n_rows, V) bytes (0 for invalid sizes), contents undefined before
+ * and after; calls that share it must be ordered on one stream.
+ * Errors: INVALID_ARG (null or misaligned pointer, n_rows or V < 1, more than 2^31 - 1 rows, unknown type, a stride < V,
+ * overlapping buffers, temperature not positive and finite, clip_eps negative or not finite, scale not finite, workspace too small), HIP. */
+size_t spiral_policy_gradient_workspace_bytes(long long n_rows, int V);
+int spiral_policy_gradient(const void* dev_logits, int dtype, long long row_stride, long long n_rows, int V,
+                           const int32_t* dev_targets, const float* dev_logp_old, const float* dev_advantage,
+                           const int32_t* dev_mask, float temperature, float clip_eps, float scale, float* dev_logp,
+                           void* dev_grad, long long grad_stride, void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* ---- AdamW (learner side) --------------------------------------------------------------------------
+ * One step over all tensors of a model at once, e.g. the weights that spiral_model_load was given (a repacked model is repacked
+ * again afterwards).  With g = grad_scale * gradient, N = the 2-norm of all g together, c = min(1, max_norm / N):
+ *     m <- beta1 m + (1 - beta1) c g ,   v <- beta2 v + (1 - beta2) (c g)^2
+ *     p <- p (1 - lr * weight_decay) - lr * (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32 (the sum of N in 64 bits), rounded to the parameter's type where there is a master copy, which holds p in fp32.
+ * States of SPIRAL_DTYPE_FP32 hold m and v.  States of SPIRAL_DTYPE_E4M3 hold, for every block of SPIRAL_ADAMW_BLOCK elements of a tensor
+ * (the last one may be shorter), codes and an fp32 scale: m = code * m_scale, sqrt(v) = code * v_scale, each scale the block's
+ * largest magnitude / 448, codes rounded to nearest even, but a positive sqrt(v) never to 0 (the denominator would be eps): to
+ * the least code, 2^-9, instead.  A block whose largest magnitude is at most 1e-30 holds zeros.  The root is what is stored because its codes
+ * reach the same 5 decades of gradient sizes that m's do.  All-zero states (codes and scales) are those of step 0. */
+#define SPIRAL_ADAMW_BLOCK 256
+typedef struct spiral_adamw spiral_adamw;
+typedef struct spiral_adamw_tensor {
+    void*       dev_param;      /* [n] of param_dtype (FP32, BF16, FP16), updated */
+    const void* dev_grad;       /* [n] of grad_dtype (FP32, BF16, FP16) */
+    float*      dev_master;     /* [n] fp32, read and updated in the parameter's place, or NULL: the parameter itself; NULL for FP32 */
+    void*       dev_m;          /* [n] of state_dtype (FP32, E4M3), updated */
+    void*       dev_v;          /* [n] of state_dtype: v, or the codes of sqrt(v), updated */
+    float*      dev_m_scale;    /* [ceil(n / SPIRAL_ADAMW_BLOCK)] for E4M3, NULL for FP32 */
+    float*      dev_v_scale;
+    long long   n;              /* >= 1 */
+    int32_t     param_dtype, grad_dtype, state_dtype;
+    int32_t     decay;          /* 0: weight_decay is not applied (gains, biases), 1: it is */
+} spiral_adamw_tensor;
+/* spiral_adamw_create copies the table into the caller's device memory (dev_mem, spiral_adamw_bytes(n_tensors) bytes, 0 on a bad count; 256-byte
+ * aligned), enqueued on `stream`; it must stay valid as long as the object, and nothing else is kept.  Tensors are aligned to their elements.
+ * No buffer that a step writes may overlap another buffer of the table; gradients are only read.  spiral_adamw_set_grads exchanges the
+ * gradients' addresses (host_dev_grads [n_tensors], same sizes and types) for the steps enqueued on `stream` after it.
+ * Errors: INVALID_ARG (null or misaligned pointer, unknown or impossible types, n < 1, overlap), HIP; NOT_LOADED (null object). */
+size_t spiral_adamw_bytes(int n_tensors);
+int  spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int n_tensors, void* dev_mem, size_t bytes, void* stream,
+                         spiral_adamw** out);
+int  spiral_adamw_set_grads(spiral_adamw* o, const void* const* host_dev_grads, void* stream);
+/* step >= 1 is the number of this step (a captured call that is replayed keeps it, as it keeps lr and the others).
+ * max_norm == 0: gradients are not clipped.  dev_norm (fp32 [1] or NULL) receives N.  Where N is computed (max_norm > 0 or
+ * dev_norm given) and is not finite in fp32, the step changes no parameter and no state.  Steps of one object must be ordered on one stream.
+ * Errors: NOT_LOADED, INVALID_ARG (betas outside [0, 1), eps <= 0, a negative or not finite lr, weight_decay or max_norm, a grad_scale
+ * that is not finite, step < 1, misaligned dev_norm), HIP. */
+int  spiral_adamw_step(spiral_adamw* o, double lr, double beta1, double beta2, double eps, double weight_decay, int step,
+                       float grad_scale, float max_norm, float* dev_norm, void* stream);
+void spiral_adamw_free(spiral_adamw* o);
 
 /* ---- measurement hooks (for benchmarks; not part of the method) --------------------------------
  * Between spiral_profile_begin and spiral_profile_end every launch of the chosen kernel class made

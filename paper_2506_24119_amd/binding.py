@@ -21,6 +21,11 @@ SPIRAL_ERR_SHAPE = -2
 SPIRAL_ERR_OOM_KV = -3
 SPIRAL_ERR_NOT_LOADED = -4
 SPIRAL_ERR_HIP = -5
+SPIRAL_DTYPE_FP32 = 0
+SPIRAL_DTYPE_BF16 = 1
+SPIRAL_DTYPE_FP16 = 2
+SPIRAL_DTYPE_E4M3 = 3
+SPIRAL_ADAMW_BLOCK = 256
 SPIRAL_MAX_BATCH = 1024
 SPIRAL_LAYER_SLOTS = 14
 
@@ -32,6 +37,8 @@ EXPORTS = [
     "spiral_rae_free", "spiral_model_tune", "spiral_kv_pool_status_offset", "spiral_decode_sample_step",
     "spiral_decode_step_static", "spiral_static_workspace_bytes", "spiral_probe_stream_read",
     "spiral_sample_truncated_ws", "spiral_sample_truncated_workspace_bytes",
+    "spiral_sample_uniform", "spiral_sample_uniform_workspace_bytes", "spiral_policy_gradient", "spiral_policy_gradient_workspace_bytes",
+    "spiral_adamw_bytes", "spiral_adamw_create", "spiral_adamw_set_grads", "spiral_adamw_step", "spiral_adamw_free",
 ]
 
 
@@ -41,6 +48,12 @@ class spiral_model_config(C.Structure):
                 ("vocab", C.c_int32), ("rope_theta", C.c_float), ("rms_eps", C.c_float),
                 ("qk_norm", C.c_int32), ("qkv_bias", C.c_int32), ("tie_lm_head", C.c_int32),
                 ("weight_dtype", C.c_int32), ("kv_block_tokens", C.c_int32)]
+
+
+class spiral_adamw_tensor_t(C.Structure):
+    _fields_ = [("dev_param", C.c_void_p), ("dev_grad", C.c_void_p), ("dev_master", C.c_void_p), ("dev_m", C.c_void_p), ("dev_v", C.c_void_p),
+                ("dev_m_scale", C.c_void_p), ("dev_v_scale", C.c_void_p), ("n", C.c_longlong), ("param_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("state_dtype", C.c_int32), ("decay", C.c_int32)]
 
 
 class SpiralError(RuntimeError):
@@ -130,6 +143,25 @@ def load_library(path: Optional[str] = None):
     lib.spiral_sample_truncated_ws.restype = C.c_int
     lib.spiral_sample_truncated_ws.argtypes = [f32p, C.c_int, C.c_int, C.c_float, C.c_int, C.c_float, C.c_uint64, i32p, i32p, vp, vp,
                                                vp, vp, C.c_size_t, vp]
+    lib.spiral_sample_uniform_workspace_bytes.restype = C.c_size_t
+    lib.spiral_sample_uniform_workspace_bytes.argtypes = [C.c_int, C.c_int]
+    lib.spiral_sample_uniform.restype = C.c_int
+    lib.spiral_sample_uniform.argtypes = [vp, C.c_int, C.c_longlong, C.c_int, C.c_int, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp, vp]
+    lib.spiral_policy_gradient_workspace_bytes.restype = C.c_size_t
+    lib.spiral_policy_gradient_workspace_bytes.argtypes = [C.c_longlong, C.c_int]
+    lib.spiral_policy_gradient.restype = C.c_int
+    lib.spiral_policy_gradient.argtypes = [vp, C.c_int, C.c_longlong, C.c_longlong, C.c_int, vp, vp, vp, vp, C.c_float, C.c_float, C.c_float, vp,
+                                           vp, C.c_longlong, vp, C.c_size_t, vp]
+    lib.spiral_adamw_bytes.restype = C.c_size_t
+    lib.spiral_adamw_bytes.argtypes = [C.c_int]
+    lib.spiral_adamw_create.restype = C.c_int
+    lib.spiral_adamw_create.argtypes = [C.POINTER(spiral_adamw_tensor_t), C.c_int, vp, C.c_size_t, vp, C.POINTER(vp)]
+    lib.spiral_adamw_set_grads.restype = C.c_int
+    lib.spiral_adamw_set_grads.argtypes = [vp, C.POINTER(C.c_void_p), vp]
+    lib.spiral_adamw_step.restype = C.c_int
+    lib.spiral_adamw_step.argtypes = [vp, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, C.c_int, C.c_float, C.c_float, vp, vp]
+    lib.spiral_adamw_free.restype = None
+    lib.spiral_adamw_free.argtypes = [vp]
     lib.spiral_rae_create.restype = C.c_int
     lib.spiral_rae_create.argtypes = [C.c_int, C.c_double, C.POINTER(vp)]
     lib.spiral_rae_update.restype = C.c_int
@@ -359,6 +391,131 @@ def spiral_sample_truncated_ws(dev_logits, B: int, V: int, temperature: float, t
                                                      C.c_uint64(seed), _ip(ids), _ip(st), _ptr(dev_noise), _ptr(dev_out_tokens),
                                                      _ptr(dev_threshold_out), _ptr(dev_workspace), C.c_size_t(workspace_bytes),
                                                      _stream_handle(stream)))
+
+
+# ------------------------------------------------------------------------- the policy's update
+_dtype_codes = {}
+
+
+def _dtype(t) -> int:
+    """The library's code of a tensor's element type."""
+    if not _dtype_codes:
+        import torch
+        _dtype_codes.update({torch.float32: SPIRAL_DTYPE_FP32, torch.bfloat16: SPIRAL_DTYPE_BF16, torch.float16: SPIRAL_DTYPE_FP16,
+                             torch.float8_e4m3fn: SPIRAL_DTYPE_E4M3})
+    if t.dtype not in _dtype_codes:
+        raise TypeError(f"element type {t.dtype} is not supported")
+    return _dtype_codes[t.dtype]
+
+
+def _rows_of(t, what: str):
+    """(rows, columns, row stride) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is needed, got shape {tuple(t.shape)}, strides {t.stride()}")
+    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vector(t, n: int, dtype: str, what: str):
+    """Address of a contiguous device vector of n elements of that type; None stays None."""
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_contiguous() or not str(t.dtype).endswith("." + dtype):
+        raise ValueError(f"{what}: {n} contiguous elements of {dtype} are needed, got {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def _setting(a, n: int, dtype, what: str):
+    """(array kept alive, its address) of a per-row setting: None, one value for all rows, or n of them."""
+    if a is None:
+        return None, None
+    if not (isinstance(a, np.ndarray) and a.dtype == dtype and a.ndim == 1 and a.flags.c_contiguous):
+        a = np.asarray(a, dtype=dtype)
+        a = np.full(n, a, dtype=dtype) if a.ndim == 0 else np.ascontiguousarray(a)
+    if a.shape != (n,):
+        raise ValueError(f"{what}: one value or {n} of them are needed, got shape {a.shape}")
+    return a, a.ctypes.data
+
+
+def spiral_sample_uniform_workspace_bytes(B: int, V: int) -> int:
+    return int(load_library().spiral_sample_uniform_workspace_bytes(B, V))
+
+
+def spiral_sample_uniform(dev_logits, temperature, top_k, top_p, min_p, dev_uniform, dev_workspace, dev_out_tokens, dev_out_logp=None, stream=None):
+    """dev_logits: [B, V] fp32, bf16 or fp16 with contiguous rows; the settings: None, one value, or one per row."""
+    B, V, stride = _rows_of(dev_logits, "logits")
+    T, Tp = _setting(temperature, B, np.float32, "temperature")
+    k, kp = _setting(top_k, B, np.int32, "top_k")
+    p, pp = _setting(top_p, B, np.float32, "top_p")
+    mp, mpp = _setting(min_p, B, np.float32, "min_p")
+    _check(load_library().spiral_sample_uniform(dev_logits.data_ptr(), _dtype(dev_logits), stride, B, V, Tp, kp, pp, mpp,
+                                                _vector(dev_uniform, B, "float32", "uniform"), _ptr(dev_workspace),
+                                                0 if dev_workspace is None else dev_workspace.numel() * dev_workspace.element_size(),
+                                                _vector(dev_out_tokens, B, "int32", "tokens"), _vector(dev_out_logp, B, "float32", "logp"),
+                                                _stream_handle(stream)))
+
+
+def spiral_policy_gradient_workspace_bytes(n_rows: int, V: int) -> int:
+    return int(load_library().spiral_policy_gradient_workspace_bytes(n_rows, V))
+
+
+def spiral_policy_gradient(dev_logits, dev_targets, dev_logp_old, dev_advantage, dev_mask, temperature: float, clip_eps: float, scale: float,
+                           dev_logp, dev_grad, dev_workspace, stream=None):
+    """dev_logits, dev_grad: [n, V] of one type with contiguous rows (the same tensor: in place)."""
+    n, V, stride = _rows_of(dev_logits, "logits")
+    gn, gV, gstride = _rows_of(dev_grad, "gradient")
+    if (gn, gV) != (n, V) or dev_grad.dtype != dev_logits.dtype:
+        raise ValueError(f"gradient: {n} x {V} of {dev_logits.dtype} is needed, got {gn} x {gV} of {dev_grad.dtype}")
+    _check(load_library().spiral_policy_gradient(dev_logits.data_ptr(), _dtype(dev_logits), stride, n, V, _vector(dev_targets, n, "int32", "targets"),
+                                                 _vector(dev_logp_old, n, "float32", "old logp"), _vector(dev_advantage, n, "float32", "advantage"),
+                                                 _vector(dev_mask, n, "int32", "mask"), temperature, clip_eps, scale,
+                                                 _vector(dev_logp, n, "float32", "logp"), dev_grad.data_ptr(), gstride, _ptr(dev_workspace),
+                                                 0 if dev_workspace is None else dev_workspace.numel() * dev_workspace.element_size(),
+                                                 _stream_handle(stream)))
+
+
+def spiral_adamw_tensor(param, grad, m, v, master=None, m_scale=None, v_scale=None, decay: bool = True) -> spiral_adamw_tensor_t:
+    """The record of one tensor: param fp32, bf16 or fp16 with its gradient, states fp32, or float8_e4m3fn codes with their scales.  The tensors
+    stay the caller's and have to outlive the optimiser."""
+    n = param.numel()
+    blocks = -(-n // SPIRAL_ADAMW_BLOCK)
+    for t, k, what in ((param, n, "param"), (grad, n, "grad"), (master, n, "master"), (m, n, "m"), (v, n, "v"),
+                       (m_scale, blocks, "m_scale"), (v_scale, blocks, "v_scale")):
+        if t is not None and (t.numel() != k or not t.is_contiguous()):
+            raise ValueError(f"{what}: {k} contiguous elements are needed, got {tuple(t.shape)}")
+        if what in ("master", "m_scale", "v_scale") and t is not None and _dtype(t) != SPIRAL_DTYPE_FP32:
+            raise ValueError(f"{what}: float32 is needed, got {t.dtype}")
+    if m.dtype != v.dtype:
+        raise ValueError(f"m and v: one type is needed, got {m.dtype} and {v.dtype}")
+    return spiral_adamw_tensor_t(_ptr(param), _ptr(grad), _ptr(master), _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), n, _dtype(param),
+                                 _dtype(grad), _dtype(m), int(bool(decay)))
+
+
+def spiral_adamw_bytes(tensors) -> int:
+    return int(load_library().spiral_adamw_bytes(len(tensors)))
+
+
+def spiral_adamw_create(tensors: Sequence[spiral_adamw_tensor_t], dev_mem, stream=None) -> int:
+    arr = (spiral_adamw_tensor_t * len(tensors))(*tensors)
+    out = C.c_void_p()
+    _check(load_library().spiral_adamw_create(arr, len(tensors), _ptr(dev_mem), dev_mem.numel() * dev_mem.element_size(), _stream_handle(stream),
+                                              C.byref(out)))
+    return out.value
+
+
+def spiral_adamw_set_grads(opt: int, grads, stream=None):
+    """grads: one contiguous tensor of the record's size and type per record."""
+    arr = (C.c_void_p * len(grads))(*[g.data_ptr() for g in grads])
+    _check(load_library().spiral_adamw_set_grads(opt, arr, _stream_handle(stream)))
+
+
+def spiral_adamw_step(opt: int, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int, grad_scale: float = 1.0,
+                      max_norm: float = 0.0, dev_norm=None, stream=None):
+    _check(load_library().spiral_adamw_step(opt, lr, beta1, beta2, eps, weight_decay, step, grad_scale, max_norm,
+                                            _vector(dev_norm, 1, "float32", "norm"), _stream_handle(stream)))
+
+
+def spiral_adamw_free(opt: int):
+    load_library().spiral_adamw_free(opt)
 
 
 # ------------------------------------------------------------------------- RAE (host only)

@@ -219,6 +219,59 @@ hipError_t launch_sample_truncated_ws(const float* logits, int B, int V, float t
                                       const uint64_t* host_keys, const float* noise, int32_t* out, float* tau_out,
                                       void* workspace, hipStream_t s);
 
+// draws from given uniform numbers: the settings of a launch's rows travel by value
+constexpr int kDrawRows = 128;
+struct DrawRows { float temperature[kDrawRows]; int32_t top_k[kDrawRows]; float top_p[kDrawRows], min_p[kDrawRows]; };
+struct DrawArgs {
+    const void* logits;       // [B][V], rows row_stride elements apart
+    long long row_stride;
+    int32_t B, V;
+    const float* uniform;     // [B]
+    int32_t* tokens;          // [B]
+    float* logp;              // [B] or null
+};
+size_t draw_workspace_bytes(int B, int V);
+hipError_t launch_draw(const DrawArgs& a, int dtype, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                       void* workspace, hipStream_t s);
+
+// gradient of the policy objective in the logits
+struct GradArgs {
+    const void* logits; long long row_stride;
+    void* grad; long long grad_stride;        // same type as the logits, the logits themselves or apart from them
+    long long n_rows;
+    int32_t V;
+    const int32_t* targets;
+    const float* logp_old;                    // or null: no ratio
+    const float* advantage;
+    const int32_t* mask;                      // or null
+    float inv_t, clip_eps, scale;
+    float* logp;
+};
+size_t policy_grad_workspace_bytes(long long n_rows, int V);
+hipError_t launch_policy_grad(const GradArgs& a, int dtype, void* workspace, hipStream_t s);
+
+// AdamW over many tensors
+constexpr int kAdamwBlock = SPIRAL_ADAMW_BLOCK;
+constexpr int kAdamwParts = 1024;             // workgroups, and partial sums of the norm, at most
+constexpr float kE4m3Max = 448.f;
+constexpr float kAdamwTiny = 1e-30f;          // a block of 8-bit states whose largest value is no more holds zeros (448 over less may be infinite)
+struct AdamwRec {
+    void* param; const void* grad; float* master; void* m; void* v; float* m_scale; float* v_scale;
+    long long n, first_chunk;
+    int32_t param_dtype, grad_dtype, state_dtype, decay;
+};
+struct AdamwArgs {
+    const AdamwRec* table;
+    int32_t n_tensors, n_part;                // n_part: partial sums of the norm, 0: none
+    long long chunks;
+    double* part;                             // [kAdamwParts]
+    float* norm;                              // or null
+    // rest1 = 1 - beta1, rest2 = 1 - beta2 (in 32 bits 1 - 0.9f is 2e-7 off), keep = 1 - lr wd, step_size = lr / (1 - beta1^t), root_scale = (1 - beta2^t)^-1/2
+    float beta1, rest1, beta2, rest2, eps, keep, step_size, root_scale, grad_scale, max_norm;
+};
+long long adamw_chunks(long long n);          // chunks that a tensor of n elements is cut into
+hipError_t launch_adamw(const AdamwArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------------------------------------
 // device helpers
 // ---------------------------------------------------------------------------------------------

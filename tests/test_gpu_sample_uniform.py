@@ -1,0 +1,179 @@
+"""spiral_sample_uniform against the float64 oracle.  Tokens are whole numbers and compared wherever the oracle says that neither the draw nor
+a cut comes within 1e-9 of the kept mass to a border (kernel and oracle add about 10^5 terms of 64 bits in different orders: 1e-12 at worst);
+log-probabilities are rounded to fp32 once, half a step of 2^-23 and those 1e-9."""
+import numpy as np
+import pytest
+
+from oracle import update as ou
+
+pytestmark = pytest.mark.gpu
+SLACK = 1e-9
+
+
+@pytest.fixture(scope="module")
+def sb():
+    import torch
+    assert torch.cuda.is_available()
+    from paper_2506_24119_amd import binding
+    binding.load_library()
+    return binding
+
+
+def place(values, dtype, pad, offset):
+    """The rows on the device, `pad` elements apart and `offset` elements behind an aligned address."""
+    import torch
+    B, V = values.shape
+    t = torch.full((B * (V + pad) + offset,), float("nan"), dtype=getattr(torch, dtype), device="cuda")
+    rows = t[offset:].view(B, V + pad)[:, :V]
+    rows.copy_(torch.from_numpy(values))
+    return rows
+
+
+def run(sb, rows, u, T=None, k=None, p=None, mp=None, fill=0xA5):
+    import torch
+    B, V = rows.shape
+    ws = torch.full((sb.spiral_sample_uniform_workspace_bytes(B, V),), fill, dtype=torch.uint8, device="cuda")
+    tok = torch.full((B + 2,), -7, dtype=torch.int32, device="cuda")
+    lp = torch.full((B + 2,), 9.0, device="cuda")
+    sb.spiral_sample_uniform(rows, T, k, p, mp, torch.from_numpy(np.asarray(u, np.float32)).cuda(), ws, tok[1:-1], lp[1:-1])
+    torch.cuda.synchronize()
+    tok, lp = tok.cpu().numpy(), lp.cpu().numpy()
+    assert tok[0] == tok[-1] == -7 and lp[0] == lp[-1] == 9.0
+    return tok[1:-1], lp[1:-1]
+
+
+def check(rows, u, got, T=None, k=None, p=None, mp=None, least=0.9):
+    tok, lp = got
+    x = rows.float().cpu().numpy()
+    at = lambda a, i, none: none if a is None else a if np.ndim(a) == 0 else a[i]  # noqa: E731
+    decided = 0
+    for i in range(len(x)):
+        want, wlp, slack = ou.draw_row(x[i], u[i], at(T, i, 1.0), at(k, i, 0), at(p, i, 1.0), at(mp, i, 0.0))
+        if slack < SLACK:
+            continue
+        decided += 1
+        assert tok[i] == want, (i, tok[i], want, slack)
+        assert lp[i] == wlp or abs(float(lp[i]) - wlp) <= abs(wlp) * 2.0 ** -24 + 1e-9, (i, lp[i], wlp)
+    assert decided >= least * len(x), decided
+
+
+SETTINGS = [dict(), dict(T=0.6, p=0.95), dict(k=50), dict(k=20, p=0.9, T=0.8), dict(p=0.5), dict(T=1.3, k=1), dict(mp=0.05), dict(T=0.7, k=200, p=0.99, mp=0.01),
+            dict(p=1e-6), dict(mp=1.0), dict(T=0.0), dict(k=3000, p=0.999), dict(T=2.0, p=0.9999)]
+
+
+@pytest.mark.parametrize("V,dtype,pad,offset", [(151936, "float32", 0, 0), (152064, "bfloat16", 24, 0), (50257, "float16", 5, 3), (40000, "float32", 1, 1),
+                                                (16384, "bfloat16", 0, 0), (16385, "float32", 0, 0), (4099, "float16", 0, 1), (1000, "float32", 0, 0), (64, "bfloat16", 0, 0),
+                                                (7, "float32", 2, 1), (1, "float16", 0, 0)])
+def test_tokens_and_log_probabilities(sb, V, dtype, pad, offset):
+    rng = np.random.default_rng(V + pad)
+    B = 11
+    for j, s in enumerate(SETTINGS):
+        x = (rng.normal(size=(B, V)) * rng.choice([0.2, 1.0, 3.0], size=(B, 1))).astype(np.float32)
+        x[1] = np.round(x[1] * 2) / 2                                  # many equal logits
+        x[2, rng.random(V) < 0.9] = -np.inf                            # a mask that leaves a tenth
+        x[3, rng.integers(0, V, 3)] += 12
+        x[4] -= 60
+        x[5, rng.random(V) < 0.01] = np.nan
+        u = rng.random(B).astype(np.float32)
+        rows = place(x, dtype, pad, offset)
+        s = {n: (min(v, max(1, V - 1)) if n == "k" and V > 1 else v) for n, v in s.items()}
+        check(rows, u, run(sb, rows, u, **s), **s, least=0.8 if V > 100 else 0.6)
+
+
+@pytest.mark.parametrize("V", [151936, 20000, 3001])
+def test_rows_with_settings_of_their_own(sb, V):
+    rng = np.random.default_rng(3)
+    B = 150                                                             # more than a launch's rows
+    x = (rng.normal(size=(B, V)) * rng.uniform(0.5, 3, size=(B, 1))).astype(np.float32)
+    T = rng.choice([0.0, 0.6, 1.0, 1.5], size=B).astype(np.float32)
+    k = rng.choice([0, -1, 1, 5, 100, V // 2, V, V + 5], size=B).astype(np.int32)
+    p = rng.choice([0.3, 0.9, 0.99, 1.0], size=B).astype(np.float32)
+    mp = rng.choice([0.0, 0.01, 0.2], size=B).astype(np.float32)
+    u = rng.random(B).astype(np.float32)
+    rows = place(x, "float32", 0, 0)
+    got = run(sb, rows, u, T, k, p, mp)
+    check(rows, u, got, T, k, p, mp)
+    # a row's result is its own: alone, in another batch, another place, on other scratch contents
+    for i in (0, 7, 149):
+        one = run(sb, rows[i:i + 1], u[i:i + 1], T[i:i + 1], k[i:i + 1], p[i:i + 1], mp[i:i + 1], fill=0)
+        assert one[0][0] == got[0][i] and one[1][0] == got[1][i]
+    again = run(sb, rows.flip(0).contiguous(), u[::-1].copy(), T[::-1], k[::-1], p[::-1], mp[::-1], fill=0xFF)
+    assert np.array_equal(again[0][::-1], got[0]) and np.array_equal(again[1][::-1], got[1])
+
+
+@pytest.mark.parametrize("V", [30000, 500])
+def test_odd_rows(sb, V):
+    rng = np.random.default_rng(4)
+    x = rng.normal(size=(12, V)).astype(np.float32)
+    x[0] = -np.inf                                                      # nothing can be drawn
+    x[1] = np.nan
+    x[2] = -np.inf; x[2, V - 1] = -3e38                                 # one token, far down
+    x[3, 5] = np.inf                                                    # all of the mass
+    x[4, [3, V - 2]] = np.inf
+    x[5] = 0.0                                                          # all equal
+    x[6] = -0.0; x[6, ::2] = 0.0
+    x[7] = np.finfo(np.float32).min; x[7, 9] = np.finfo(np.float32).min / 2
+    x[8] = 1.0 + rng.integers(0, 3, V) * 2.0 ** -23                     # neighbours in the last bit
+    x[9] = np.linspace(3e38, -3e38, V)
+    x[10, : V // 2] = -np.inf
+    x[11] *= 1e-30
+    rows = place(x, "float32", 0, 0)
+    for u in (0.0, 0.3, 0.77, 0.99999994, 1.0, -1.0, np.nan):
+        for s in (dict(), dict(k=2), dict(p=0.9), dict(mp=0.1), dict(T=0.0), dict(T=1e-6), dict(T=1e6, p=0.5), dict(T=1e-38), dict(k=V - 1, p=0.3, mp=0.5)):
+            uu = np.full(12, u, np.float32)
+            got = run(sb, rows, uu, **s)
+            assert got[0][0] == got[0][1] == 0 and np.isneginf(got[1][:2]).all()
+            check(rows, uu, got, **s, least=0.4)
+
+
+@pytest.mark.parametrize("V,s", [(151936, dict(p=0.9)), (40000, dict(k=30000)), (151936, dict(k=20000, p=0.7)), (20000, dict(mp=0.999))])
+def test_crowded_rows(sb, V, s):
+    """More logits around the cut than any list of candidates would hold."""
+    rng = np.random.default_rng(5)
+    x = np.stack([rng.normal(size=V) * 1e-3, np.zeros(V), np.where(rng.random(V) < 0.5, 1.0, 1.0009765625), rng.normal(size=V) * 1e-7]).astype(np.float32)
+    x[3] += 5
+    u = rng.random(4).astype(np.float32)
+    rows = place(x, "float32", 0, 0)
+    check(rows, u, run(sb, rows, u, **s), **s, least=0.4)
+
+
+def test_numbers_spread_over_the_distribution(sb):
+    """1024 numbers on a grid draw every token as often as it is probable, up to the two ends of its stretch."""
+    rng = np.random.default_rng(6)
+    V = 97
+    row = (rng.normal(size=V) * 1.5).astype(np.float32)
+    u = ((np.arange(1024) + 0.5) / 1024).astype(np.float32)
+    rows = place(np.repeat(row[None], 1024, 0), "float32", 0, 0)
+    tok, lp = run(sb, rows, u)
+    assert (np.diff(tok) >= 0).all()
+    q = np.exp(row.astype(np.float64)); q /= q.sum()
+    assert np.abs(np.bincount(tok, minlength=V) - 1024 * q).max() <= 1.0 + 1e-6
+
+
+def test_replays_of_a_captured_draw_read_the_numbers_of_then(sb):
+    import torch
+    rng = np.random.default_rng(7)
+    B, V = 5, 33000
+    x = rng.normal(size=(B, V)).astype(np.float32) * 2
+    rows = place(x, "float32", 0, 0)
+    T, k, p = np.full(B, 0.8, np.float32), np.array([0, 40, 0, 40, 0], np.int32), np.array([1, 1, 0.9, 0.9, 0.2], np.float32)
+    u = torch.zeros(B, device="cuda")
+    ws = torch.empty(sb.spiral_sample_uniform_workspace_bytes(B, V), dtype=torch.uint8, device="cuda")
+    tok, lp = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty(B, device="cuda")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        sb.spiral_sample_uniform(rows, T, k, p, None, u, ws, tok, lp)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        sb.spiral_sample_uniform(rows, T, k, p, None, u, ws, tok, lp)
+    for r in range(4):
+        un = rng.random(B).astype(np.float32)
+        u.copy_(torch.from_numpy(un))
+        rows.copy_(torch.from_numpy(np.roll(x, r, axis=1)))
+        tok.fill_(-1)
+        g.replay()
+        torch.cuda.synchronize()
+        got = tok.cpu().numpy().copy(), lp.cpu().numpy().copy()
+        check(rows, un, got, T, k, p)
+        assert np.array_equal(run(sb, rows, un, T, k, p)[0], got[0])
