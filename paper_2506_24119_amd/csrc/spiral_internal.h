@@ -252,7 +252,7 @@ hipError_t launch_policy_grad(const GradArgs& a, int dtype, void* workspace, hip
 
 // AdamW over many tensors
 constexpr int kAdamwBlock = SPIRAL_ADAMW_BLOCK;
-constexpr int kAdamwParts = 1024;             // workgroups, and partial sums of the norm, at most
+constexpr int kAdamwParts = 2048;             // workgroups, and partial sums of the norm, at most
 constexpr float kE4m3Max = 448.f;
 constexpr float kAdamwTiny = 1e-30f;          // a block of 8-bit states whose largest value is no more holds zeros (448 over less may be infinite)
 struct AdamwRec {
@@ -269,8 +269,9 @@ struct AdamwArgs {
     // rest1 = 1 - beta1, rest2 = 1 - beta2 (in 32 bits 1 - 0.9f is 2e-7 off), keep = 1 - lr wd, step_size = lr / (1 - beta1^t), root_scale = (1 - beta2^t)^-1/2
     float beta1, rest1, beta2, rest2, eps, keep, step_size, root_scale, grad_scale, max_norm;
 };
-long long adamw_chunks(long long n);          // chunks that a tensor of n elements is cut into
-hipError_t launch_adamw(const AdamwArgs& a, hipStream_t s);
+int adamw_steps(long long elements);          // runs of 1,024 elements in a chunk, for tensors of so many in all
+long long adamw_chunks(long long n, int steps);      // chunks that a tensor of n elements is cut into
+hipError_t launch_adamw(const AdamwArgs& a, int steps, hipStream_t s);
 
 // ---------------------------------------------------------------------------------------------
 // device helpers

@@ -103,7 +103,7 @@ extern "C" int spiral_policy_gradient(const void* dev_logits, int dtype, long lo
 // AdamW
 // ---------------------------------------------------------------------------------------------
 struct spiral_adamw {
-    int n = 0;
+    int n = 0, steps = 0;
     long long chunks = 0;
     std::unique_ptr<AdamwRec[]> table;      // what the device holds a copy of
     char* mem = nullptr;
@@ -143,7 +143,7 @@ extern "C" int spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int 
         if (p) spans[n_spans++] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)n * size, written};
     };
     span(dev_mem, (long long)spiral_adamw_bytes(n_tensors), 1, true);
-    long long chunks = 0;
+    long long elements = 0, chunks = 0;
     for (int t = 0; t < n_tensors; ++t) {
         const spiral_adamw_tensor& x = host_tensors[t];
         const int ps = dtype_size(x.param_dtype), gs = dtype_size(x.grad_dtype);
@@ -167,9 +167,9 @@ extern "C" int spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int 
         span(x.dev_v, x.n, ss, true);
         span(x.dev_m_scale, blocks, 4, true);
         span(x.dev_v_scale, blocks, 4, true);
-        o->table[t] = {x.dev_param, x.dev_grad, x.dev_master, x.dev_m, x.dev_v, x.dev_m_scale, x.dev_v_scale, x.n, chunks,
+        o->table[t] = {x.dev_param, x.dev_grad, x.dev_master, x.dev_m, x.dev_v, x.dev_m_scale, x.dev_v_scale, x.n, 0,
                        x.param_dtype, x.grad_dtype, x.state_dtype, x.decay};
-        chunks += adamw_chunks(x.n);
+        elements += x.n;
     }
     std::sort(spans.get(), spans.get() + n_spans, [](const Span& a, const Span& b) { return a.lo < b.lo; });
     uintptr_t end = 0, written_end = 0;                          // of all spans so far, and of those that are written
@@ -179,6 +179,11 @@ extern "C" int spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int 
         if (spans[i].written) written_end = std::max(written_end, spans[i].hi);
     }
     o->n = n_tensors;
+    o->steps = adamw_steps(elements);
+    for (int t = 0; t < n_tensors; ++t) {
+        o->table[t].first_chunk = chunks;
+        chunks += adamw_chunks(o->table[t].n, o->steps);
+    }
     o->chunks = chunks;
     o->mem = (char*)dev_mem;
     const int rc = adamw_upload(o.get(), stream, "adamw_create");
@@ -222,7 +227,7 @@ extern "C" int spiral_adamw_step(spiral_adamw* o, double lr, double beta1, doubl
     a.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, step)));
     a.grad_scale = grad_scale;
     a.max_norm = max_norm;
-    return done(launch_adamw(a, (hipStream_t)stream), "adamw_step");
+    return done(launch_adamw(a, o->steps, (hipStream_t)stream), "adamw_step");
 }
 
 extern "C" void spiral_adamw_free(spiral_adamw* o) { delete o; }

@@ -255,3 +255,18 @@ def test_many_tensors(sb):
     opt, mem = build(sb, tensors)
     check_step(sb, opt, tensors, 2, max_norm=0.5)
     sb.spiral_adamw_free(opt)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_long_chunks(sb, bits):
+    """From 2^23 elements on a workgroup takes 4,096 of a tensor at a time: tensors that end in and behind every run of them, each kind of
+    parameter and gradient."""
+    rng = np.random.default_rng(9)
+    kinds = [("bfloat16", "bfloat16", True), ("float32", "float32", False), ("bfloat16", "float32", False), ("float16", "bfloat16", False)]
+    sizes = [2_200_001, 4095, 4096, 4097, 2_150_400, 5121, 8191, 2_100_003, 300, 2_050_050]
+    tensors = [Tensor(sb, rng, n, *kinds[i % 4], bits=bits, decay=i % 2 == 0, offset=i % 3) for i, n in enumerate(sizes)]
+    assert sum(t.n for t in tensors) > 1 << 23
+    opt, mem = build(sb, tensors)
+    for step in (1, 9):
+        check_step(sb, opt, tensors, step, max_norm=1.0)
+    sb.spiral_adamw_free(opt)
