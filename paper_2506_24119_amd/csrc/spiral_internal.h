@@ -247,6 +247,7 @@ struct GradArgs {
     float inv_t, clip_eps, scale;
     float* logp;
 };
+int policy_grad_slices(long long n_rows, int V, int dtype);      // workgroups of a row; 1: one launch, more: two
 size_t policy_grad_workspace_bytes(long long n_rows, int V);
 hipError_t launch_policy_grad(const GradArgs& a, int dtype, void* workspace, hipStream_t s);
 

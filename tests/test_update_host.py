@@ -143,3 +143,17 @@ def test_binding_checks_what_it_marshals():
         a.update(bad)
         with pytest.raises(ValueError):
             sb.spiral_adamw_tensor(**a)
+
+
+def test_rows_of_the_gradient_are_cut_where_there_are_few_long_ones(lib):
+    """The lines of the rule: 96 rows, 16,384 vectors of 16 bytes to a row, slices of 1,024 of them at least."""
+    slices = lib["_ZN6spiral18policy_grad_slicesExii"]
+    slices.restype, slices.argtypes = C.c_int, [C.c_longlong, C.c_int, C.c_int]
+    FP32, BF16, FP16 = sb.SPIRAL_DTYPE_FP32, sb.SPIRAL_DTYPE_BF16, sb.SPIRAL_DTYPE_FP16
+    assert slices(1, 65536, FP32) == 16 and slices(1, 65532, FP32) == 1 and slices(1, 131072, BF16) == 16 and slices(1, 131071, FP16) == 1
+    assert slices(96, 151936, BF16) == 10 and slices(97, 151936, BF16) == 1 and slices(5, 8209, FP32) == 1
+    for n in (1, 7, 96):
+        for V in (65536, 151936, 1 << 20, (1 << 31) - 1):
+            k = slices(n, V, FP32)
+            assert 2 <= k <= max(2, 1024 // n) and V // 4 // k >= 1024
+            assert sb.spiral_policy_gradient_workspace_bytes(n, V) >= n * k * 8 + n * 4
