@@ -5,35 +5,100 @@ namespace spiral {
 
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
-
 // larger float <=> larger key; -0 and +0 share a key
 __device__ __forceinline__ uint32_t order_key(float z) {
     const uint32_t b = __float_as_uint(z + 0.0f);
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k); }
 
-__device__ __forceinline__ float clean(float l) { return l == l ? l : -INFINITY; }      // an undefined logit is never drawn
-template <class T> __device__ __forceinline__ float logit_at(const T* row, uint32_t v);
-template <> __device__ __forceinline__ float logit_at(const float* row, uint32_t v) { return clean(row[v]); }
-template <> __device__ __forceinline__ float logit_at(const __bf16* row, uint32_t v) { return clean((float)row[v]); }
-template <> __device__ __forceinline__ float logit_at(const _Float16* row, uint32_t v) { return clean((float)row[v]); }
+__device__ __forceinline__ float clean(float l) { return fmaxf(l, -INFINITY); }      // an undefined logit is never drawn
+
+// 16 bytes of a row, aligned to an element only: the wide loads take any address
+template <class T> struct RowVec;
+template <> struct RowVec<float> { static constexpr int N = 4; typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct RowVec<__bf16> { static constexpr int N = 8; typedef __bf16 type __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct RowVec<_Float16> { static constexpr int N = 8; typedef _Float16 type __attribute__((ext_vector_type(8), aligned(2))); };
 
 __device__ __forceinline__ uint64_t shfl_down_u64(uint64_t v, int d) {
     const uint32_t lo = __shfl_down((uint32_t)v, d, 64), hi = __shfl_down((uint32_t)(v >> 32), d, 64);
     return ((uint64_t)hi << 32) | lo;
 }
+__device__ __forceinline__ double wave_total(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+__device__ __forceinline__ float wave_largest(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+// the sum over the lanes up to this one
+__device__ __forceinline__ double wave_scan(double v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const double o = __shfl_up(v, d, 64);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+// 2^(j / 64), j = 0 .. 63, evaluated by the host's compiler from the definition
+struct Exp2Table { double v[64]; };
+constexpr Exp2Table make_exp2_table() {
+    Exp2Table t = {};
+    for (int j = 0; j < 64; ++j) {                    // e^(j ln 2 / 64) by its series
+        const double x = j * (0.69314718055994530942 / 64.0);
+        double term = 1.0, sum = 0.0, lost = 0.0;
+        for (int n = 1; n < 30; ++n) {                // the small terms' rounding is carried along
+            const double y = term - lost, s = sum + y;
+            lost = (s - sum) - y;
+            sum = s;
+            term *= x / n;
+        }
+        t.v[j] = sum;
+    }
+    return t;
+}
+__device__ const Exp2Table kExp2 = make_exp2_table();
 
 // w = exp((l - m) / T) in 64 bits: the tokens follow from where u falls between sums of up to 10^5 of them, and an error of 1e-7 in those
-// would draw another token once in a few dozen rows.  The largest logit, +inf too, weighs 1.
+// would draw another token once in a few dozen rows.  With t = 64 (l - m) / (T ln 2), k the nearest integer and f = t - k: 2^(k / 64) from a table and
+// an exponent, 2^(f / 64) by four terms (|f ln 2 / 64| <= 0.0055: 4e-14 off).  Adding 1.5 2^52 rounds to the integer and leaves it in the lower word.
+// The largest logit, +inf too, weighs 1; without a temperature all others weigh 0.
+// p f + c with the constant where a scalar register holds it: as the accumulator of the two-address form it is moved there anew each time.
+__device__ __forceinline__ double fma_const(double p, double f, double c) {
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(p), "v"(f), "s"(c));
+    return r;
+}
 struct Weight {
-    double m, inv_t;
-    bool greedy;
-    __device__ __forceinline__ double operator()(float l) const {
-        if ((double)l == m) return 1.0;
-        return greedy ? 0.0 : exp(((double)l - m) * inv_t);
+    double m, c;                                      // c = 64 / (T ln 2)
+    const double* table;
+    bool greedy, infinite;
+    __device__ __forceinline__ Weight(float largest, float temperature, const double* table_)
+        : m(largest == INFINITY ? 0.0 : (double)largest), c(92.33248261689366 / (double)temperature), table(table_), greedy(temperature == 0.f),
+          infinite(largest == INFINITY) {}
+    // what takes the place of a logit where the largest is +inf, whose differences are undefined
+    __device__ __forceinline__ float tame(float l) const { return infinite ? l == INFINITY ? 0.f : -INFINITY : l; }
+    // of a row with a temperature and a finite maximum
+    __device__ __forceinline__ double plain(float l) const {
+        const double t = fmax(((double)l - m) * c, -80000.0), s = t + 6755399441055744.0, f = t - (s - 6755399441055744.0);
+        const int k = (int)(uint32_t)__double_as_longlong(s);
+        double p = 5.732851688640402e-10;            // (ln 2 / 64)^4 / 24, ^3 / 6, ^2 / 2, ^1
+        p = fma_const(p, f, 2.1173137155464774e-07);
+        p = fma_const(p, f, 5.864904955056169e-05);
+        p = fma_const(p, f, 0.010830424696249145);
+        p = fma(p, f, 1.0);
+        return ldexp(table[k & 63] * p, k >> 6);
     }
+    __device__ __forceinline__ double operator()(float l) const {
+        const float x = tame(l);
+        return (double)x == m ? 1.0 : greedy ? 0.0 : plain(x);
+    }
+    // log of a token's weight
+    __device__ __forceinline__ double log_of(float l, float temperature) const { return greedy ? 0.0 : ((double)tame(l) - m) / (double)temperature; }
 };
 
 struct Select {
@@ -63,39 +128,66 @@ __device__ __forceinline__ void pick_digit(const uint64_t* hist, int shift, Sele
     }
 }
 
-}  // namespace
+// the sum of 256 bins, in the first lane of the wave that calls this
+__device__ __forceinline__ uint64_t sum_of(const uint64_t* hist, int lane) {
+    uint64_t z = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z += hist[lane * 4 + i];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) z += shfl_down_u64(z, d);
+    return z;
+}
+__device__ __forceinline__ uint64_t share_of(double p, uint64_t z) {
+    const uint64_t target = (uint64_t)ceil(p * (double)z);
+    return target < 1 ? 1 : target > z ? z : target;
+}
+__device__ __forceinline__ double number_of(float u) { return (double)fminf(fmaxf(u, 0.f), 0.99999994f); }      // fmaxf: a NaN counts as 0
+
+struct RowSettings {
+    float temperature;
+    int top_k;
+    double top_p, min_p;
+    bool greedy;
+    __device__ __forceinline__ RowSettings(const DrawRows& rows, int r, int V) {
+        temperature = rows.temperature[r];
+        greedy = temperature == 0.f;
+        top_k = greedy || rows.top_k[r] >= V || rows.top_k[r] < 0 ? 0 : rows.top_k[r];
+        top_p = greedy ? 1.0 : rows.top_p[r];
+        min_p = greedy ? 0.0 : rows.min_p[r];
+    }
+};
+
+__device__ __forceinline__ void nothing_to_draw(const DrawArgs& a, int r) {
+    a.tokens[r] = 0;
+    if (a.logp) a.logp[r] = -INFINITY;
+}
 
 // A row by a workgroup, in as many sweeps of it as the cuts need: one for the maximum, four digits of the k-th largest key, four of the
 // key at which the mass reaches p, one for the sum of what is kept and a part of one for the token.
-template <class T>
-__global__ __launch_bounds__(kThreads) void draw_row_kernel(DrawArgs a, DrawRows rows) {
+template <class T, int THREADS>
+__device__ __forceinline__ void draw_row(const DrawArgs& a, const DrawRows& rows, int r, const double* table) {
+    constexpr int WAVES = THREADS / 64;
     __shared__ uint64_t hist[256];
     __shared__ Select sel;
-    __shared__ double s_sum[kWaves];
-    __shared__ float s_max[kWaves];
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ double s_sum[WAVES];
+    __shared__ float s_max[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T* row = (const T*)a.logits + (size_t)r * a.row_stride;
     const uint32_t V = a.V;
+    auto logit_at = [&](uint32_t v) { return clean((float)row[v]); };
 
     float m = -INFINITY;
-    for (uint32_t v = tid; v < V; v += kThreads) m = fmaxf(m, logit_at(row, v));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    for (uint32_t v = tid; v < V; v += THREADS) m = fmaxf(m, logit_at(v));
+    m = wave_largest(m);
     if (lane == 0) s_max[wave] = m;
     __syncthreads();
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_max[w]);
-    if (m == -INFINITY) {                           // nothing can be drawn
-        if (tid == 0) {
-            a.tokens[r] = 0;
-            if (a.logp) a.logp[r] = -INFINITY;
-        }
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, s_max[w]);
+    if (m == -INFINITY) {
+        if (tid == 0) nothing_to_draw(a, r);
         return;
     }
-    const float temperature = rows.temperature[r];
-    const bool greedy = temperature == 0.f;
-    const Weight weight = {(double)m, greedy ? 0.0 : 1.0 / (double)temperature, greedy};
-    const int top_k = greedy ? 0 : rows.top_k[r];
-    const double top_p = greedy ? 1.0 : rows.top_p[r], min_p = greedy ? 0.0 : rows.min_p[r];
+    const RowSettings set(rows, r, a.V);
+    const Weight weight(m, set.temperature, table);
     uint32_t floor_key = 0;
 
     auto descend = [&](auto&& amount, auto&& total_known) {
@@ -104,8 +196,8 @@ __global__ __launch_bounds__(kThreads) void draw_row_kernel(DrawArgs a, DrawRows
             if (tid < 256) hist[tid] = 0;
             __syncthreads();
             const uint32_t prefix = sel.prefix;
-            for (uint32_t v = tid; v < V; v += kThreads) {
-                const float l = logit_at(row, v);
+            for (uint32_t v = tid; v < V; v += THREADS) {
+                const float l = logit_at(v);
                 const uint32_t key = order_key(l);
                 if (key >= floor_key && (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8)))) {
                     const uint64_t x = amount(l);
@@ -114,7 +206,7 @@ __global__ __launch_bounds__(kThreads) void draw_row_kernel(DrawArgs a, DrawRows
             }
             __syncthreads();
             if (shift == 24) {
-                if (tid == 0) total_known();
+                if (wave == 0) total_known();
                 __syncthreads();
             }
             if (wave == 0) pick_digit(hist, shift, &sel, lane);
@@ -123,46 +215,42 @@ __global__ __launch_bounds__(kThreads) void draw_row_kernel(DrawArgs a, DrawRows
         floor_key = sel.prefix > floor_key ? sel.prefix : floor_key;
         __syncthreads();
     };
-    if (top_k > 0 && (uint32_t)top_k < V) {
-        if (tid == 0) { sel.prefix = 0; sel.remaining = (uint64_t)top_k; }
+    if (set.top_k) {
+        if (tid == 0) { sel.prefix = 0; sel.remaining = (uint64_t)set.top_k; }
         descend([](float) { return (uint64_t)1; }, [] {});
     }
-    if (top_p < 1.0) {
+    if (set.top_p < 1.0) {
         // integers add in any order: 2^-b of the largest weight, b as V of them leave room for
         const double unit = ldexp(1.0, 30 + __clz(V));
         if (tid == 0) { sel.prefix = 0; sel.remaining = 0; }
         descend([&](float l) { return (uint64_t)rint(weight(l) * unit); }, [&] {
-            uint64_t z = 0;
-            for (int i = 0; i < 256; ++i) z += hist[i];
-            const uint64_t target = (uint64_t)ceil(top_p * (double)z);
-            sel.remaining = target < 1 ? 1 : target > z ? z : target;
+            const uint64_t z = sum_of(hist, lane);
+            if (lane == 0) sel.remaining = share_of(set.top_p, z);
         });
     }
 
     auto kept = [&](float l) {
         if (order_key(l) < floor_key) return 0.0;
         const double w = weight(l);
-        return w >= min_p ? w : 0.0;
+        return w >= set.min_p ? w : 0.0;
     };
     // a wave has a run of neighbouring entries
-    const uint32_t run = ((V + kWaves - 1) / kWaves + 63) & ~63u;
+    const uint32_t run = ((V + WAVES - 1) / WAVES + 63) & ~63u;
     const uint32_t lo = min((uint32_t)wave * run, V), hi = min(lo + run, V);
     double sum = 0.0;
-    for (uint32_t v = lo + lane; v < hi; v += 64) sum += kept(logit_at(row, v));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    for (uint32_t v = lo + lane; v < hi; v += 64) sum += kept(logit_at(v));
+    sum = wave_total(sum);
     if (lane == 0) s_sum[wave] = sum;
     __syncthreads();
     double total = 0.0;
-    for (int w = 0; w < kWaves; ++w) total += s_sum[w];
-    const float u = greedy ? 0.f : a.uniform[r];
-    const double target = (double)fminf(fmaxf(u, 0.f), 0.99999994f) * total;      // fmaxf: a NaN counts as 0
+    for (int w = 0; w < WAVES; ++w) total += s_sum[w];
+    const double target = set.greedy ? 0.0 : number_of(a.uniform[r]) * total;
     double before = 0.0;
-    int mine = -1;
-    for (int w = 0, done = 0; w < kWaves && !done; ++w) {
+    int mine = 0;
+    for (int w = 0, done = 0; w < WAVES && !done; ++w) {
         if (s_sum[w] > 0.0) mine = w;               // rounding may leave none: then the last with anything in it
-        if (before + s_sum[w] > target) done = 1;
-        else if (w + 1 < kWaves) before += s_sum[w];
+        done = before + s_sum[w] > target;
+        before += s_sum[w];
     }
     if (wave != mine) return;
     uint32_t token = 0;
@@ -171,13 +259,8 @@ __global__ __launch_bounds__(kThreads) void draw_row_kernel(DrawArgs a, DrawRows
     for (int w = 0; w < mine; ++w) before += s_sum[w];
     for (uint32_t v0 = lo; v0 < hi && !found; v0 += 64) {
         const uint32_t v = v0 + lane;
-        const double w = v < hi ? kept(logit_at(row, v)) : 0.0;
-        double c = w;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const double o = __shfl_up(c, d, 64);
-            if (lane >= d) c += o;
-        }
+        const double w = v < hi ? kept(logit_at(v)) : 0.0;
+        const double c = wave_scan(w, lane);
         const uint64_t over = __builtin_amdgcn_ballot_w64(w > 0.0 && before + c > target), any = __builtin_amdgcn_ballot_w64(w > 0.0);
         if (over) { token = v0 + __builtin_ctzll(over); found = true; }
         else if (any) token = v0 + 63 - __builtin_clzll(any);
@@ -185,23 +268,653 @@ __global__ __launch_bounds__(kThreads) void draw_row_kernel(DrawArgs a, DrawRows
     }
     if (lane == 0) {
         a.tokens[r] = (int32_t)token;
-        if (a.logp) a.logp[r] = greedy ? 0.f : (float)(log(weight(logit_at(row, token))) - log(total));
+        if (a.logp) a.logp[r] = set.greedy ? 0.f : (float)(weight.log_of(logit_at(token), set.temperature) - log(total));
     }
 }
 
-size_t draw_workspace_bytes(int, int) { return 256; }
+// ---- long rows, in pieces -----------------------------------------------------------------------------------------------
+
+constexpr int kPiece = 2048;          // neighbouring entries of a wave: 32 a lane, all loaded at once
+constexpr int kMaxPieces = 256;       // of a row
+constexpr int kWgWaves = 8;           // waves of a workgroup
+constexpr int kSlice = kPiece * kWgWaves;
+constexpr int kBins = 1024, kPerNat = 32;          // bins over the 32 below the maximum of (l - m) / T, and the last for what lies further down
+constexpr int kCopies = 4;            // of a histogram: neighbouring lanes do not meet in one
+constexpr uint32_t kOne = 1u << 19;   // an entry in it; below, the sum of places of seven bits.  Room for all that lanes of one copy have:
+static_assert(kSlice / kCopies * 127 < (int)kOne && kSlice / kCopies < (1 << 13), "a copy's bin overflows");
+constexpr int kCap = 8192;            // candidates of a row
+constexpr int kTakeAll = 0, kTakeSome = 1, kTakeListed = 2, kTakeSlow = 3;
+
+// What the histogram decides of a row.  Cut by count, the border lies among the logits from k_list up to below k_keep (-inf both: not cut so); cut by mass, from
+// list up to below keep.  Those are the candidates; from keep on all are kept.
+struct DrawPlan {
+    float m;
+    int take;                         // kTakeAll: all are kept but for min-p's; Some: as above; Listed: all from `list` on are candidates; Slow: a workgroup does the row
+    float keep, list, k_keep, k_list;
+    uint32_t k_above;                 // entries from k_keep on
+    int pad;
+};
+// What a piece has: kept weights relative to exp(ref), and of a row cut by mass all weights and those in bins below lo.
+struct PieceSums { double kept, all, above; float ref; int pad; };
+
+// the piece's entries in index order: vector q of lane i starts at (64 q + i) N
+template <class T>
+struct Piece {
+    static constexpr int N = RowVec<T>::N, Q = kPiece / 64 / N;
+    typename RowVec<T>::type x[Q];
+    uint32_t first, V;
+    __device__ __forceinline__ Piece(const T* row, uint32_t start, uint32_t V_, int lane) : first(start + lane * N), V(V_) {
+        if (start + kPiece <= V) {                  // the same for the whole wave
+#pragma unroll
+            for (int q = 0; q < Q; ++q) x[q] = *(const typename RowVec<T>::type*)(row + first + q * 64 * N);
+            return;
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[q][e] = index(q, e) < V ? row[index(q, e)] : (T)-INFINITY;
+    }
+    __device__ __forceinline__ uint32_t index(int q, int e) const { return first + q * 64 * N + e; }
+    __device__ __forceinline__ bool whole() const { return __builtin_amdgcn_readfirstlane(first) + kPiece <= V; }
+    __device__ __forceinline__ float at(int q, int e) const { return clean((float)x[q][e]); }
+    __device__ __forceinline__ float largest() const {
+        float m = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int e = 0; e < N; ++e) m = fmaxf(m, (float)x[q][e]);
+        return m;
+    }
+};
+
+// monotone in l, and their floors whole numbers that floats hold exactly
+__device__ __forceinline__ float bin_scale(float temperature) { return (float)kPerNat / temperature; }
+__device__ __forceinline__ float bin_place(float l, float scale) { return fminf(fmaxf(l * scale, -4194304.f), 4194304.f); }
+__device__ __forceinline__ float bin_floor(float l, float scale) { return floorf(bin_place(l, scale)); }
+// the least logit whose floor is at least f (NaN, which none reaches: there is none), bit by bit of its key
+__device__ __forceinline__ float least_logit(float f, float scale) {
+    uint32_t most_below = 0;                           // keys up to it are below, or no logit's
+    const uint32_t bottom = order_key(-INFINITY), top = order_key(INFINITY);
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t key = most_below | (1u << bit);
+        if (key < bottom || (key <= top && bin_floor(key_value(key), scale) < f)) most_below = key;
+    }
+    return most_below >= top ? NAN : key_value(max(most_below + 1, bottom));
+}
+
+struct DrawSpace {                    // the workspace of a launch's rows
+    PieceSums* pieces;                // [rows][kMaxPieces]: n_pieces of them used
+    float* largest;                   // [rows][slices]
+    uint2* hist;                      // [rows][slices][kBins]: entries, and how far down in the bin they lie, in all
+    DrawPlan* plan;                   // [rows]
+    uint32_t* n_listed;               // [rows]
+    uint2* list;                      // [rows][kCap]: key, index
+    int slices, n_pieces;
+};
+
+// a piece whose entries are all kept, relative to its own maximum
+template <class T>
+__device__ __forceinline__ void sum_whole_piece(const Piece<T>& p, float temperature, const double* table, int lane, PieceSums* out) {
+    const float m = wave_largest(p.largest());
+    double sum = 0.0;
+    if (m != -INFINITY) {
+        const Weight weight(m, temperature, table);
+        if (weight.infinite || weight.greedy) {
+#pragma unroll
+            for (int q = 0; q < p.Q; ++q)
+#pragma unroll
+                for (int e = 0; e < p.N; ++e) sum += weight(p.at(q, e));
+        } else {
+#pragma unroll
+            for (int q = 0; q < p.Q; ++q)
+#pragma unroll
+                for (int e = 0; e < p.N; ++e) sum += weight.plain(p.at(q, e));
+        }
+        sum = wave_total(sum);
+    }
+    if (lane == 0) { out->kept = sum; out->ref = m; }
+}
+
+__device__ __forceinline__ void copy_table(double* s_table) {
+    if (threadIdx.x < 64) s_table[threadIdx.x] = kExp2.v[threadIdx.x];
+    __syncthreads();
+}
+
+}  // namespace
+
+template <class T>
+__global__ __launch_bounds__(1024) void draw_row_kernel(DrawArgs a, DrawRows rows) {
+    __shared__ double s_table[64];
+    copy_table(s_table);
+    draw_row<T, 1024>(a, rows, blockIdx.x, s_table);
+}
+
+// Batches without a cut: one sweep.
+template <class T>
+__global__ __launch_bounds__(kWgWaves * 64) void draw_sum_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
+    __shared__ double s_table[64];
+    const int r = blockIdx.y, lane = threadIdx.x & 63, i = blockIdx.x * kWgWaves + (threadIdx.x >> 6);
+    const Piece<T> p((const T*)a.logits + (size_t)r * a.row_stride, min((uint32_t)i * kPiece, (uint32_t)a.V), a.V, lane);
+    copy_table(s_table);
+    if (i < w.n_pieces) sum_whole_piece(p, rows.temperature[r], s_table, lane, &w.pieces[(size_t)r * kMaxPieces + i]);
+}
+
+// The maximum of a slice and, where the row is cut by count or mass, how many of its entries lie in which bin below it.
+template <class T>
+__global__ __launch_bounds__(kWgWaves * 64) void draw_count_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
+    __shared__ uint32_t h[kBins * kCopies];
+    __shared__ float s_max[kWgWaves];
+    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t first = (uint32_t)(blockIdx.x * kWgWaves + wave) * kPiece;
+    const Piece<T> p((const T*)a.logits + (size_t)r * a.row_stride, min(first, (uint32_t)a.V), a.V, lane);
+    const RowSettings set(rows, r, a.V);
+    const bool binned = set.top_k || set.top_p < 1.0;
+    if (binned)
+        for (int i = tid; i < kBins * kCopies; i += kWgWaves * 64) h[i] = 0;
+    float m = wave_largest(p.largest());
+    if (lane == 0) s_max[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWgWaves; ++i) m = fmaxf(m, s_max[i]);
+    const size_t seg = (size_t)r * w.slices + blockIdx.x;
+    if (tid == 0) w.largest[seg] = m;
+    if (!binned) return;
+    const float scale = bin_scale(set.temperature), top = bin_floor(m, scale);
+#pragma unroll
+    for (int q = 0; q < p.Q; ++q)
+#pragma unroll
+        for (int e = 0; e < p.N; ++e) {
+            const float y = bin_place(p.at(q, e), scale), f = floorf(y);
+            const int b = min((int)(top - f), kBins - 1);
+            const uint32_t down = (uint32_t)((f + 1.f - y) * 127.99f);          // of 128 parts of the bin
+            if (p.index(q, e) < p.V) atomicAdd(&h[b * kCopies + (lane & (kCopies - 1))], kOne | down);
+        }
+    __syncthreads();
+    for (int b = tid; b < kBins; b += kWgWaves * 64) {
+        uint2 n = make_uint2(0, 0);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const uint32_t x = h[b * kCopies + i];
+            n.x += x / kOne;
+            n.y += x % kOne;
+        }
+        w.hist[seg * kBins + b] = n;
+    }
+}
+
+// The row's histogram, and the logits between which its cuts fall.  By mass they are estimated, an entry by the mean place of its bin's: 2e-4 off at most, one
+// alone in its bin 1e-4.  The sums of the next sweep show whether the cut lies among the candidates.  (With whole bins for places a distribution of a few
+// likely tokens over a flat rest was 2e-2 off, and the candidates a third of the row.)
+__global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
+    __shared__ uint32_t s_count[kBins], s_down[kBins];
+    __shared__ double s_mass[kBins / 64], s_share, s_more;
+    __shared__ uint32_t s_wave[kBins / 64], s_above, s_upto;
+    __shared__ int s_lo, s_hi, s_cut;
+    const int r = blockIdx.x, b = threadIdx.x, lane = b & 63, wave = b >> 6;
+    const RowSettings set(rows, r, a.V);
+    static_assert(kMaxPieces / kWgWaves <= 64, "a lane has a slice");
+    const float mine = lane < w.slices ? w.largest[(size_t)r * w.slices + lane] : -INFINITY;
+    uint2 n8[8];                                                // the first slices' bins are on their way meanwhile
+    const uint2* hist = w.hist + (size_t)r * w.slices * kBins + b;
+    const bool binned = set.top_k || set.top_p < 1.0;
+    if (binned)
+#pragma unroll
+        for (int s = 0; s < 8; ++s) n8[s] = s < w.slices ? hist[(size_t)s * kBins] : make_uint2(0, 0);
+    const float m = wave_largest(mine);
+    DrawPlan plan = {m, kTakeAll, -INFINITY, -INFINITY, -INFINITY, -INFINITY, 0u, 0};
+    if (b == 0) w.n_listed[r] = 0;
+    if (m == -INFINITY || !binned) {
+        if (b == 0) w.plan[r] = plan;
+        return;
+    }
+    const float scale = bin_scale(set.temperature), top = bin_floor(m, scale);
+    s_count[b] = s_down[b] = 0;
+    if (b == 0) { s_lo = kBins; s_hi = s_cut = kBins - 1; }
+    __syncthreads();
+    const float down = top - bin_floor(mine, scale);
+    for (int s0 = 0; s0 < w.slices; s0 += 8) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const int to = (int)fminf((float)b + __shfl(down, s0 + s, 64), (float)(kBins - 1));
+            if (n8[s].x) { atomicAdd(&s_count[to], n8[s].x); atomicAdd(&s_down[to], n8[s].y); }
+        }
+#pragma unroll
+        for (int s = 0; s < 8; ++s) n8[s] = s0 + 8 + s < w.slices ? hist[(size_t)(s0 + 8 + s) * kBins] : make_uint2(0, 0);
+    }
+    __syncthreads();
+    const uint32_t n = s_count[b];
+    const double mid = n && b < kBins - 1 ? n * exp(-(b + (s_down[b] + 0.5 * n) / (128.0 * n)) * (1.0 / kPerNat)) : 0.0;
+    uint32_t count = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(count, d, 64);
+        if (lane >= d) count += o;
+    }
+    double mass = wave_scan(mid, lane);
+    if (lane == 63) { s_wave[wave] = count; s_mass[wave] = mass; }
+    __syncthreads();
+    double all = 0.0;
+    for (int i = 0; i < kBins / 64; ++i) {
+        if (i < wave) { count += s_wave[i]; mass += s_mass[i]; }
+        all += s_mass[i];
+    }
+    double off = 0.0;
+    if (set.top_k) {                                            // exactly one bin; of its mass, the share of its entries that count
+        if (count - n < (uint32_t)set.top_k && (uint32_t)set.top_k <= count) {
+            s_cut = b;
+            s_above = count - n;
+            s_upto = count;
+            s_share = mass - mid + mid * ((double)((uint32_t)set.top_k - (count - n)) / n);
+            s_more = mid;
+        }
+        __syncthreads();
+        all = s_share;
+        off = s_more;
+    }
+    const bool listed = set.top_k && s_upto <= kCap;
+    const int cut = s_cut;
+    if (set.top_p < 1.0 && !listed) {
+        const double target = set.top_p * all;
+        off += 3e-4 * target;
+        if (mass - mid < target - off && target - off <= mass) s_lo = b;
+        if (mass - mid < target + off && target + off <= mass) s_hi = b;
+        if (b == 0 && target - off <= 0.0) s_lo = 0;
+        __syncthreads();
+    }
+    if (wave != 0) return;
+    int lo = set.top_p < 1.0 && !listed ? s_lo : cut, hi = set.top_p < 1.0 && !listed ? s_hi : cut;
+    if (hi >= cut || lo > cut) hi = cut;                        // both borders in one run of bins
+    if (lo > cut && lo < kBins) lo = cut;
+    // lanes 0 to 3: keep, list, k_keep, k_list; a bin's entries are those from its floor on
+    const int bin = lane == 0 ? lo - 1 : lane == 1 ? hi : lane == 2 ? cut - 1 : cut;
+    float t = bin < 0 ? NAN : least_logit(top - (float)bin, scale);           // NaN: above every logit
+    if (bin == kBins - 1) t = set.top_k ? -INFINITY : -3.402823466e38f;      // all the rest; what weighs nothing is no candidate by mass
+    plan.keep = __shfl(t, 0, 64);
+    plan.list = __shfl(t, 1, 64);
+    if (set.top_k) {
+        plan.k_keep = __shfl(t, 2, 64);
+        plan.k_list = __shfl(t, 3, 64);
+        plan.k_above = s_above;
+    }
+    plan.take = lo >= kBins ? kTakeSlow : listed ? kTakeListed : kTakeSome;
+    if (lane == 0) w.plan[r] = plan;
+}
+
+// The second sweep: sums of what is kept for sure, piece by piece, and the list of candidates.
+template <class T>
+__global__ __launch_bounds__(kWgWaves * 64) void draw_cut_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
+    __shared__ double s_table[64];
+    const int r = blockIdx.y, lane = threadIdx.x & 63, i = blockIdx.x * kWgWaves + (threadIdx.x >> 6);
+    const Piece<T> p((const T*)a.logits + (size_t)r * a.row_stride, min((uint32_t)i * kPiece, (uint32_t)a.V), a.V, lane);
+    copy_table(s_table);
+    const DrawPlan plan = w.plan[r];
+    if (i >= w.n_pieces || plan.take == kTakeSlow || plan.m == -INFINITY) return;
+    const RowSettings set(rows, r, a.V);
+    PieceSums* out = &w.pieces[(size_t)r * kMaxPieces + i];
+    if (plan.take == kTakeAll && set.min_p == 0.0) {
+        sum_whole_piece(p, set.temperature, s_table, lane, out);
+        return;
+    }
+    const Weight weight(plan.m, set.temperature, s_table);
+    const bool odd = weight.infinite || weight.greedy;
+    double kept = 0.0, all = 0.0, above = 0.0;
+    uint32_t mine = 0;                                          // one bit an entry: a candidate
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int q = 0; q < p.Q; ++q)
+#pragma unroll
+            for (int e = 0; e < p.N; ++e) f(p.at(q, e), q * p.N + e);
+    };
+    const bool limited = set.min_p > 0.0, by_count = set.top_k != 0;
+    // what counts for the mass that top-p goes by; what is kept for sure; the candidates
+    auto some = [&](float l, int i, double x) {
+        const bool sure = l >= plan.keep;
+        above += sure ? x : 0.0;
+        all += x;
+        mine |= !sure && l >= plan.list ? 1u << i : 0u;
+    };
+    auto some_more = [&](float l, int i, double x) {
+        const bool sure = l >= plan.keep, counted = !by_count || l >= plan.k_keep;
+        above += sure ? x : 0.0;
+        kept += sure && x >= set.min_p ? x : 0.0;
+        all += counted ? x : 0.0;
+        mine |= (!sure && l >= plan.list) || (!counted && l >= plan.k_list) ? 1u << i : 0u;
+    };
+    if (plan.take == kTakeListed) each([&](float l, int i) { mine |= l >= plan.list ? 1u << i : 0u; });
+    else if (plan.take == kTakeAll) each([&](float l, int) { const double x = weight(l); kept += x >= set.min_p ? x : 0.0; });
+    else if (odd || limited || by_count) each([&](float l, int i) { some_more(l, i, weight(l)); });
+    else each([&](float l, int i) { some(l, i, weight.plain(l)); });
+    if (plan.take == kTakeSome) {
+        all = wave_total(all);
+        above = wave_total(above);
+    }
+    kept = wave_total(kept);
+    if (plan.take == kTakeSome && !limited) kept = above;
+    if (lane == 0) *out = {kept, all, above, plan.m, 0};
+    if (!p.whole())                                             // past the row's end there are none
+#pragma unroll
+        for (int q = 0; q < p.Q; ++q)
+#pragma unroll
+            for (int e = 0; e < p.N; ++e)
+                if (p.index(q, e) >= p.V) mine &= ~(1u << (q * p.N + e));
+    if (!__builtin_amdgcn_ballot_w64(mine != 0)) return;
+    uint32_t at = __popc(mine), n = at;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(at, d, 64);
+        if (lane >= d) at += o;
+    }
+    uint32_t base = 0;
+    if (lane == 63) base = atomicAdd(&w.n_listed[r], at);
+    at += __shfl(base, 63, 64) - n;
+#pragma unroll
+    for (int q = 0; q < p.Q; ++q)
+#pragma unroll
+        for (int e = 0; e < p.N; ++e)
+            if (mine & (1u << (q * p.N + e))) {
+                if (at < kCap) w.list[(size_t)r * kCap + at] = make_uint2(order_key(p.at(q, e)), p.index(q, e));
+                ++at;
+            }
+}
+
+// The end of a row: with CUTS the exact border among the candidates (a radix descent, as in draw_row) and their weights' place among the pieces; the piece in
+// which the number falls; the token in it.
+template <class T, bool CUTS>
+__global__ __launch_bounds__(CUTS ? 512 : 64) void draw_pick_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
+    constexpr int THREADS = CUTS ? 512 : 64;
+    extern __shared__ uint4 lds_raw[];
+    uint2* list = (uint2*)lds_raw;                              // [kCap]
+    __shared__ double s_table[64];
+    __shared__ uint64_t hist[CUTS ? 256 : 1];
+    __shared__ uint64_t s_cand[CUTS ? kMaxPieces : 1];
+    __shared__ Select sel;
+    __shared__ double s_all, s_above;
+    __shared__ uint64_t s_z, s_zk;
+    __shared__ uint32_t s_differ;
+    __shared__ bool s_found;
+    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    copy_table(s_table);
+    const RowSettings set(rows, r, a.V);
+    const T* row = (const T*)a.logits + (size_t)r * a.row_stride;
+    const PieceSums* pieces = w.pieces + (size_t)r * kMaxPieces;
+    constexpr int PER = kMaxPieces / 64;
+    double sum[PER];                                            // a lane has PER neighbouring pieces
+    float ref[PER];
+    float m = -INFINITY;
+    DrawPlan plan = {};
+    if (CUTS) {
+        plan = w.plan[r];
+        m = plan.m;
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int i = lane * PER + j;
+        ref[j] = i < w.n_pieces ? pieces[i].ref : -INFINITY;
+        sum[j] = i < w.n_pieces ? pieces[i].kept : 0.0;
+        if (!CUTS) m = fmaxf(m, ref[j]);
+    }
+    if (!CUTS) m = wave_largest(m);
+    if (m == -INFINITY) {
+        if (tid == 0) nothing_to_draw(a, r);
+        return;
+    }
+    const Weight weight(m, set.temperature, s_table);
+    uint32_t floor_key = 0;
+    constexpr double UNIT = 1125899906842624.0;                 // 2^50: kCap of them fit 64 bits
+    bool slow = false;
+    if constexpr (CUTS) {
+        const uint32_t n = w.n_listed[r];
+        slow = plan.take == kTakeSlow || ((plan.take == kTakeSome || plan.take == kTakeListed) && n > kCap);
+        const bool listed = !slow && (plan.take == kTakeSome || plan.take == kTakeListed);
+        if (listed) {
+            if (wave == 0) {
+                double all = 0.0, above = 0.0;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int i = lane * PER + j;
+                    if (i < w.n_pieces) { all += pieces[i].all; above += pieces[i].above; }
+                }
+                all = wave_total(all);
+                above = wave_total(above);
+                if (lane == 0) { s_all = all; s_above = above; }
+            }
+            if (tid == 0) { s_z = s_zk = 0; s_differ = 0; }
+            for (uint32_t i = tid; i < n; i += THREADS) list[i] = w.list[(size_t)r * kCap + i];
+            for (int i = tid; i < kMaxPieces; i += THREADS) s_cand[i] = 0;
+            __syncthreads();
+            // digits that all candidates share are not looked at
+            uint32_t differ = 0;
+            for (uint32_t i = tid; i < n; i += THREADS) differ |= list[i].x ^ list[0].x;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) differ |= __shfl_xor(differ, o, 64);
+            if (lane == 0 && differ) atomicOr(&s_differ, differ);
+            __syncthreads();
+            const uint32_t any = s_differ;
+            const int first = any >> 24 ? 24 : any >> 16 ? 16 : any >> 8 ? 8 : 0;
+            const uint32_t shared_bits = first < 24 ? list[0].x & ~((256u << first) - 1u) : 0u;
+            auto descend = [&](auto&& amount) {                 // sel.remaining is set
+                if (tid == 0) sel.prefix = shared_bits;
+                for (int shift = first; shift >= 0; shift -= 8) {
+                    if (tid < 256) hist[tid] = 0;
+                    __syncthreads();
+                    const uint32_t prefix = sel.prefix;
+                    for (uint32_t i = tid; i < n; i += THREADS) {
+                        const uint32_t key = list[i].x;
+                        if (key >= floor_key && (shift == first || (key >> (shift + 8)) == (prefix >> (shift + 8)))) {
+                            const uint64_t x = amount(key);
+                            if (x) atomicAdd((unsigned long long*)&hist[key >> shift & 255u], (unsigned long long)x);
+                        }
+                    }
+                    __syncthreads();
+                    if (wave == 0) pick_digit(hist, shift, &sel, lane);
+                    __syncthreads();
+                }
+                floor_key = sel.prefix > floor_key ? sel.prefix : floor_key;
+            };
+            auto mass = [&](uint32_t key) { return (uint64_t)rint(weight(key_value(key)) * UNIT); };
+            // only those below k_keep are counted: the others are in number known
+            const uint32_t sure_key = plan.take == kTakeListed || plan.k_keep != plan.k_keep ? 0xFFFFFFFFu : order_key(plan.k_keep);
+            if (set.top_k) {
+                if (tid == 0) sel.remaining = (uint64_t)set.top_k - (plan.take == kTakeListed ? 0u : plan.k_above);
+                descend([&](uint32_t key) { return key < sure_key ? (uint64_t)1 : (uint64_t)0; });
+            }
+            if (set.top_p < 1.0) {
+                // the mass of what the count leaves: all candidates', and of that what lies below k_keep (the rest is in s_all already)
+                uint64_t z = 0, zk = 0;
+                for (uint32_t i = tid; i < n; i += THREADS) {
+                    const uint32_t key = list[i].x;
+                    if (key < floor_key) continue;
+                    const uint64_t x = mass(key);
+                    z += x;
+                    if (set.top_k && key < sure_key) zk += x;
+                }
+#pragma unroll
+                for (int o = 32; o > 0; o >>= 1) { z += shfl_down_u64(z, o); zk += shfl_down_u64(zk, o); }
+                if (lane == 0) { atomicAdd((unsigned long long*)&s_z, (unsigned long long)z); atomicAdd((unsigned long long*)&s_zk, (unsigned long long)zk); }
+                __syncthreads();
+                if (tid == 0) {
+                    // how much of it the cut still needs; none, or more than there is: it does not lie among the candidates
+                    const double of = (plan.take == kTakeListed ? 0.0 : s_all) + (double)s_zk * (1.0 / UNIT), over = plan.take == kTakeListed ? 0.0 : s_above;
+                    const double need = ceil((set.top_p * of - over) * UNIT);
+                    sel.remaining = need >= 1.0 && need <= (double)s_z ? (uint64_t)need : 0;
+                    if (need > (double)s_z && over + (double)s_z * (1.0 / UNIT) >= of * (1.0 - 1e-12)) sel.remaining = s_z;      // by rounding alone
+                    s_found = sel.remaining != 0;
+                }
+                __syncthreads();
+                slow = !s_found;
+                if (!slow) {
+                    descend(mass);
+                    // below its run of candidates there is a gap down to those of the count
+                    slow = plan.take == kTakeSome && floor_key < order_key(plan.list);
+                }
+            }
+            if (!slow) {
+                for (uint32_t i = tid; i < n; i += THREADS) {
+                    const uint2 e = list[i];
+                    if (e.x < floor_key || weight(key_value(e.x)) < set.min_p) continue;
+                    atomicAdd((unsigned long long*)&s_cand[e.y / kPiece], (unsigned long long)mass(e.x));
+                }
+                __syncthreads();
+            }
+        }
+        if (slow) {
+            draw_row<T, THREADS>(a, rows, r, s_table);
+            return;
+        }
+        if (wave != 0) return;
+        if (listed)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) sum[j] += (double)s_cand[lane * PER + j] * (1.0 / UNIT);
+    }
+    // relative to the row's maximum: pieces whose entries are all kept have their own
+    double mine = 0.0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        if (ref[j] != m) sum[j] = sum[j] > 0.0 ? sum[j] * weight(ref[j]) : 0.0;
+        mine += sum[j];
+    }
+    const double upto = wave_scan(mine, lane), total = __shfl(upto, 63, 64);
+    const double target = set.greedy ? 0.0 : number_of(a.uniform[r]) * total;
+    // the first piece whose running sum exceeds the target, else the last that has anything
+    double c = upto - mine, before = 0.0;
+    int hit = -1, last = -1;
+    double hit_before = 0.0, last_before = 0.0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        if (sum[j] > 0.0) { last = lane * PER + j; last_before = c; }
+        const double next = c + sum[j];
+        if (hit < 0 && sum[j] > 0.0 && next > target) { hit = lane * PER + j; hit_before = c; }
+        c = next;
+    }
+    const double log_total = log(total);
+    const uint64_t hits = __builtin_amdgcn_ballot_w64(hit >= 0), lasts = __builtin_amdgcn_ballot_w64(last >= 0);
+    int piece;
+    if (hits) {
+        const int from = __builtin_ctzll(hits);
+        piece = __shfl(hit, from, 64); before = __shfl(hit_before, from, 64);
+    } else {
+        const int from = 63 - __builtin_clzll(lasts);
+        piece = __shfl(last, from, 64); before = __shfl(last_before, from, 64);
+    }
+    const Piece<T> p(row, (uint32_t)piece * kPiece, a.V, lane);
+    auto kept = [&](int q, int e) {
+        const float l = p.at(q, e);
+        const double x = !CUTS || order_key(l) >= floor_key ? weight(l) : 0.0;
+        return CUTS && x < set.min_p ? 0.0 : x;
+    };
+    double own[p.Q], to[p.Q];                                   // all runs of 64 N at once: their scans wait for each other's lanes together
+#pragma unroll
+    for (int q = 0; q < p.Q; ++q) {
+        own[q] = 0.0;
+#pragma unroll
+        for (int e = 0; e < p.N; ++e) own[q] += kept(q, e);
+        to[q] = own[q];
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+        for (int q = 0; q < p.Q; ++q) {
+            const double o = __shfl_up(to[q], d, 64);
+            if (lane >= d) to[q] += o;
+        }
+    uint32_t token = 0;
+    float logit = 0.f;
+    bool found = false;
+#pragma unroll
+    for (int q = 0; q < p.Q; ++q) {
+        const double run = __shfl(to[q], 63, 64);
+        const uint64_t over = __builtin_amdgcn_ballot_w64(own[q] > 0.0 && before + to[q] > target), any = __builtin_amdgcn_ballot_w64(own[q] > 0.0);
+        if (!found && any) {
+            const int from = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any);
+            double s = before + (to[q] - own[q]);               // in that lane: its first entry that exceeds, else its last with a weight
+            uint32_t best = 0;
+            float l = 0.f;
+            bool done = false;
+#pragma unroll
+            for (int e = 0; e < p.N; ++e) {
+                const double x = kept(q, e);
+                s += x;
+                if (!done && x > 0.0) { best = p.index(q, e); l = p.at(q, e); done = s > target; }
+            }
+            token = __shfl(best, from, 64);
+            logit = __shfl(l, from, 64);
+            found = over != 0;
+        }
+        before += run;
+    }
+    if (lane == 0) {
+        a.tokens[r] = (int32_t)token;
+        if (a.logp) a.logp[r] = set.greedy ? 0.f : (float)(weight.log_of(logit, set.temperature) - log_total);
+    }
+}
+
+namespace {
+bool in_pieces(int V) { return V >= 16384 && V <= kPiece * kMaxPieces; }
+size_t take(size_t& at, size_t bytes) {
+    const size_t o = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return o;
+}
+DrawSpace draw_space(uintptr_t base, int rows, int V, size_t* bytes) {
+    DrawSpace w;
+    w.n_pieces = (V + kPiece - 1) / kPiece;
+    w.slices = (V + kSlice - 1) / kSlice;
+    size_t at = 0;
+    w.pieces = (PieceSums*)(base + take(at, (size_t)rows * kMaxPieces * sizeof(PieceSums)));
+    w.largest = (float*)(base + take(at, (size_t)rows * w.slices * sizeof(float)));
+    w.hist = (uint2*)(base + take(at, (size_t)rows * w.slices * kBins * sizeof(uint2)));
+    w.plan = (DrawPlan*)(base + take(at, (size_t)rows * sizeof(DrawPlan)));
+    w.n_listed = (uint32_t*)(base + take(at, (size_t)rows * sizeof(uint32_t)));
+    w.list = (uint2*)(base + take(at, (size_t)rows * kCap * sizeof(uint2)));
+    *bytes = at;
+    return w;
+}
+
+template <class T>
+hipError_t launch_chunk(const DrawArgs& g, const DrawRows& rows, const DrawSpace& w, bool pieces, bool cuts, hipStream_t s) {
+    if (!pieces) {
+        hipLaunchKernelGGL(draw_row_kernel<T>, dim3(g.B), dim3(1024), 0, s, g, rows);
+        return hipGetLastError();
+    }
+    const dim3 grid(w.slices, g.B), threads(kWgWaves * 64);
+    if (!cuts) {
+        hipLaunchKernelGGL(draw_sum_kernel<T>, grid, threads, 0, s, g, rows, w);
+        hipLaunchKernelGGL((draw_pick_kernel<T, false>), dim3(g.B), dim3(64), 0, s, g, rows, w);
+        return hipGetLastError();
+    }
+    const int list_lds = kCap * sizeof(uint2);
+    hipLaunchKernelGGL(draw_count_kernel<T>, grid, threads, 0, s, g, rows, w);
+    hipLaunchKernelGGL(draw_plan_kernel, dim3(g.B), dim3(kBins), 0, s, g, rows, w);
+    hipLaunchKernelGGL(draw_cut_kernel<T>, grid, threads, 0, s, g, rows, w);
+    hipError_t e = hipFuncSetAttribute((const void*)draw_pick_kernel<T, true>, hipFuncAttributeMaxDynamicSharedMemorySize, list_lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((draw_pick_kernel<T, true>), dim3(g.B), dim3(512), list_lds, s, g, rows, w);
+    return hipGetLastError();
+}
+}  // namespace
+
+// rows are processed kDrawRows at a time (their settings travel by value), one chunk after the other on the stream
+size_t draw_workspace_bytes(int B, int V) {
+    if (!in_pieces(V)) return 256;
+    size_t bytes = 0;
+    draw_space(0, B < kDrawRows ? B : kDrawRows, V, &bytes);
+    return bytes;
+}
 
 hipError_t launch_draw(const DrawArgs& a, int dtype, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
-                       void*, hipStream_t s) {
+                       void* workspace, hipStream_t s) {
     const size_t size = dtype == SPIRAL_DTYPE_FP32 ? 4 : 2;
+    const bool pieces = in_pieces(a.V);
     for (int off = 0; off < a.B; off += kDrawRows) {
         DrawRows rows;
         const int n = a.B - off < kDrawRows ? a.B - off : kDrawRows;
+        bool cuts = false;
         for (int i = 0; i < n; ++i) {
             rows.temperature[i] = temperature ? temperature[off + i] : 1.f;
             rows.top_k[i] = top_k ? top_k[off + i] : 0;
             rows.top_p[i] = top_p ? top_p[off + i] : 1.f;
             rows.min_p[i] = min_p ? min_p[off + i] : 0.f;
+            cuts = cuts || (rows.temperature[i] > 0.f && ((rows.top_k[i] > 0 && rows.top_k[i] < a.V) || rows.top_p[i] < 1.f || rows.min_p[i] > 0.f));
         }
         DrawArgs g = a;
         g.B = n;
@@ -209,10 +922,10 @@ hipError_t launch_draw(const DrawArgs& a, int dtype, const float* temperature, c
         g.uniform = a.uniform + off;
         g.tokens = a.tokens + off;
         g.logp = a.logp ? a.logp + off : nullptr;
-        if (dtype == SPIRAL_DTYPE_FP32) hipLaunchKernelGGL(draw_row_kernel<float>, dim3(n), dim3(kThreads), 0, s, g, rows);
-        else if (dtype == SPIRAL_DTYPE_BF16) hipLaunchKernelGGL(draw_row_kernel<__bf16>, dim3(n), dim3(kThreads), 0, s, g, rows);
-        else hipLaunchKernelGGL(draw_row_kernel<_Float16>, dim3(n), dim3(kThreads), 0, s, g, rows);
-        const hipError_t e = hipGetLastError();
+        size_t bytes;
+        const DrawSpace w = draw_space((uintptr_t)workspace, n, a.V, &bytes);
+        const hipError_t e = dtype == SPIRAL_DTYPE_FP32 ? launch_chunk<float>(g, rows, w, pieces, cuts, s)
+                           : dtype == SPIRAL_DTYPE_BF16 ? launch_chunk<__bf16>(g, rows, w, pieces, cuts, s) : launch_chunk<_Float16>(g, rows, w, pieces, cuts, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
