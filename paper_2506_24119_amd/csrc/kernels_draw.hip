@@ -82,20 +82,34 @@ struct Weight {
           infinite(largest == INFINITY) {}
     // what takes the place of a logit where the largest is +inf, whose differences are undefined
     __device__ __forceinline__ float tame(float l) const { return infinite ? l == INFINITY ? 0.f : -INFINITY : l; }
-    // of a row with a temperature and a finite maximum
-    __device__ __forceinline__ double plain(float l) const {
-        const double t = fmax(((double)l - m) * c, -80000.0), s = t + 6755399441055744.0, f = t - (s - 6755399441055744.0);
-        const int k = (int)(uint32_t)__double_as_longlong(s);
-        double p = 5.732851688640402e-10;            // (ln 2 / 64)^4 / 24, ^3 / 6, ^2 / 2, ^1
-        p = fma_const(p, f, 2.1173137155464774e-07);
-        p = fma_const(p, f, 5.864904955056169e-05);
-        p = fma_const(p, f, 0.010830424696249145);
-        p = fma(p, f, 1.0);
-        return ldexp(table[k & 63] * p, k >> 6);
+    // of a row with a temperature and a finite maximum, N at a time, so that neither a table's entry nor a product is waited for; an undefined logit
+    // weighs nothing (the maximum drops it).  The difference comes first: l c - m c in one operation is off by m c's rounding, which for logits of 1e38 or temperatures
+    // of 1e-30 is larger than any exponent.
+    template <int N> __device__ __forceinline__ void plain(const float (&l)[N], double (&w)[N]) const {
+        double f[N], e[N];
+        int k[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const double t = fmax(((double)l[i] - m) * c, -80000.0), s = t + 6755399441055744.0;
+            f[i] = t - (s - 6755399441055744.0);
+            k[i] = (int)(uint32_t)__double_as_longlong(s);
+            e[i] = table[k[i] & 63];
+        }
+        if (N > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = fma_const(5.732851688640402e-10, f[i], 2.1173137155464774e-07);            // (ln 2 / 64)^4 / 24, ^3 / 6, ^2 / 2, ^1
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = fma_const(w[i], f[i], 5.864904955056169e-05);
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = fma_const(w[i], f[i], 0.010830424696249145);
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = ldexp(e[i] * fma(w[i], f[i], 1.0), k[i] >> 6);
     }
     __device__ __forceinline__ double operator()(float l) const {
-        const float x = tame(l);
-        return (double)x == m ? 1.0 : greedy ? 0.0 : plain(x);
+        const float x[1] = {tame(l)};
+        double w[1];
+        plain(x, w);
+        return (double)x[0] == m ? 1.0 : greedy ? 0.0 : w[0];
     }
     // log of a token's weight
     __device__ __forceinline__ double log_of(float l, float temperature) const { return greedy ? 0.0 : ((double)tame(l) - m) / (double)temperature; }
@@ -283,6 +297,7 @@ constexpr int kCopies = 4;            // of a histogram: neighbouring lanes do n
 constexpr uint32_t kOne = 1u << 19;   // an entry in it; below, the sum of places of seven bits.  Room for all that lanes of one copy have:
 static_assert(kSlice / kCopies * 127 < (int)kOne && kSlice / kCopies < (1 << 13), "a copy's bin overflows");
 constexpr int kCap = 8192;            // candidates of a row
+constexpr int kApart = 64;            // words between the counters of rows: atomics of different rows do not queue for one cache line
 constexpr int kTakeAll = 0, kTakeSome = 1, kTakeListed = 2, kTakeSlow = 3;
 
 // What the histogram decides of a row.  Cut by count, the border lies among the logits from k_list up to below k_keep (-inf both: not cut so); cut by mass, from
@@ -331,15 +346,19 @@ struct Piece {
 __device__ __forceinline__ float bin_scale(float temperature) { return (float)kPerNat / temperature; }
 __device__ __forceinline__ float bin_place(float l, float scale) { return fminf(fmaxf(l * scale, -4194304.f), 4194304.f); }
 __device__ __forceinline__ float bin_floor(float l, float scale) { return floorf(bin_place(l, scale)); }
-// the least logit whose floor is at least f (NaN, which none reaches: there is none), bit by bit of its key
-__device__ __forceinline__ float least_logit(float f, float scale) {
-    uint32_t most_below = 0;                           // keys up to it are below, or no logit's
+// the least logit whose floor is at least f (NaN, which none reaches: there is none), for every 16 lanes of a wave one f: four bits of its key at a time, lane i
+// of the 16 tries the last key of the i-th range
+__device__ __forceinline__ float least_logit(float f, float scale, int lane) {
     const uint32_t bottom = order_key(-INFINITY), top = order_key(INFINITY);
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t key = most_below | (1u << bit);
-        if (key < bottom || (key <= top && bin_floor(key_value(key), scale) < f)) most_below = key;
+    auto reaches = [&](uint32_t key) { return key >= bottom && (key > top || bin_floor(key_value(key), scale) >= f); };
+    uint32_t at = 0;
+#pragma unroll
+    for (int shift = 28; shift >= 0; shift -= 4) {
+        const uint32_t last = at + ((uint32_t)(lane & 15) << shift) + ((1u << shift) - 1u);
+        const uint32_t hit = (uint32_t)(__builtin_amdgcn_ballot_w64(reaches(last)) >> (lane & 48)) & 0xFFFFu;
+        at += (uint32_t)__builtin_ctz(hit) << shift;           // the last range's reaches always
     }
-    return most_below >= top ? NAN : key_value(max(most_below + 1, bottom));
+    return at > top ? NAN : key_value(at);
 }
 
 struct DrawSpace {                    // the workspace of a launch's rows
@@ -347,10 +366,28 @@ struct DrawSpace {                    // the workspace of a launch's rows
     float* largest;                   // [rows][slices]
     uint2* hist;                      // [rows][slices][kBins]: entries, and how far down in the bin they lie, in all
     DrawPlan* plan;                   // [rows]
-    uint32_t* n_listed;               // [rows]
+    uint32_t* n_listed;               // [rows][kApart]
     uint2* list;                      // [rows][kCap]: key, index
     int slices, n_pieces;
 };
+
+// f(four logits, the first's number) for a lane's entries.  The values, and what has been added so far (settle), are opaque to the compiler, which would convert
+// all 32 ahead, for every branch that may need them, and add them when all are there: 222 registers for what takes 80, and two waves a SIMD for six.
+template <class V> __device__ __forceinline__ void settle(V& v) { asm volatile("" : "+v"(v)); }
+template <class T, class F>
+__device__ __forceinline__ void for_each_four(const Piece<T>& p, F&& f) {
+#pragma unroll
+    for (int i = 0; i < p.Q * p.N; i += 4) {
+        float l[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            l[j] = (float)p.x[(i + j) / p.N][(i + j) % p.N];
+            asm volatile("" : "+v"(l[j]));
+        }
+        f(l, i);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 
 // a piece whose entries are all kept, relative to its own maximum
 template <class T>
@@ -359,17 +396,19 @@ __device__ __forceinline__ void sum_whole_piece(const Piece<T>& p, float tempera
     double sum = 0.0;
     if (m != -INFINITY) {
         const Weight weight(m, temperature, table);
-        if (weight.infinite || weight.greedy) {
+        double x[4];
+        if (weight.infinite || weight.greedy)
+            for_each_four(p, [&](const float (&l)[4], int) {
 #pragma unroll
-            for (int q = 0; q < p.Q; ++q)
-#pragma unroll
-                for (int e = 0; e < p.N; ++e) sum += weight(p.at(q, e));
-        } else {
-#pragma unroll
-            for (int q = 0; q < p.Q; ++q)
-#pragma unroll
-                for (int e = 0; e < p.N; ++e) sum += weight.plain(p.at(q, e));
-        }
+                for (int j = 0; j < 4; ++j) sum += weight(clean(l[j]));
+                settle(sum);
+            });
+        else
+            for_each_four(p, [&](const float (&l)[4], int) {
+                weight.plain(l, x);
+                sum += (x[0] + x[1]) + (x[2] + x[3]);
+                settle(sum);
+            });
         sum = wave_total(sum);
     }
     if (lane == 0) { out->kept = sum; out->ref = m; }
@@ -462,7 +501,7 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
         for (int s = 0; s < 8; ++s) n8[s] = s < w.slices ? hist[(size_t)s * kBins] : make_uint2(0, 0);
     const float m = wave_largest(mine);
     DrawPlan plan = {m, kTakeAll, -INFINITY, -INFINITY, -INFINITY, -INFINITY, 0u, 0};
-    if (b == 0) w.n_listed[r] = 0;
+    if (b == 0) w.n_listed[(size_t)r * kApart] = 0;
     if (m == -INFINITY || !binned) {
         if (b == 0) w.plan[r] = plan;
         return;
@@ -525,15 +564,16 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
     int lo = set.top_p < 1.0 && !listed ? s_lo : cut, hi = set.top_p < 1.0 && !listed ? s_hi : cut;
     if (hi >= cut || lo > cut) hi = cut;                        // both borders in one run of bins
     if (lo > cut && lo < kBins) lo = cut;
-    // lanes 0 to 3: keep, list, k_keep, k_list; a bin's entries are those from its floor on
-    const int bin = lane == 0 ? lo - 1 : lane == 1 ? hi : lane == 2 ? cut - 1 : cut;
-    float t = bin < 0 ? NAN : least_logit(top - (float)bin, scale);           // NaN: above every logit
+    // 16 lanes each: keep, list, k_keep, k_list; a bin's entries are those from its floor on
+    const int bin = lane < 16 ? lo - 1 : lane < 32 ? hi : lane < 48 ? cut - 1 : cut;
+    float t = least_logit(bin < 0 ? NAN : top - (float)bin, scale, lane);
+    if (bin < 0) t = NAN;                                       // above every logit
     if (bin == kBins - 1) t = set.top_k ? -INFINITY : -3.402823466e38f;      // all the rest; what weighs nothing is no candidate by mass
     plan.keep = __shfl(t, 0, 64);
-    plan.list = __shfl(t, 1, 64);
+    plan.list = __shfl(t, 16, 64);
     if (set.top_k) {
-        plan.k_keep = __shfl(t, 2, 64);
-        plan.k_list = __shfl(t, 3, 64);
+        plan.k_keep = __shfl(t, 32, 64);
+        plan.k_list = __shfl(t, 48, 64);
         plan.k_above = s_above;
     }
     plan.take = lo >= kBins ? kTakeSlow : listed ? kTakeListed : kTakeSome;
@@ -542,10 +582,11 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
 
 // The second sweep: sums of what is kept for sure, piece by piece, and the list of candidates.
 template <class T>
-__global__ __launch_bounds__(kWgWaves * 64) void draw_cut_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
+__global__ __launch_bounds__(kWgWaves * 64, 5) void draw_cut_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
     __shared__ double s_table[64];
     const int r = blockIdx.y, lane = threadIdx.x & 63, i = blockIdx.x * kWgWaves + (threadIdx.x >> 6);
-    const Piece<T> p((const T*)a.logits + (size_t)r * a.row_stride, min((uint32_t)i * kPiece, (uint32_t)a.V), a.V, lane);
+    const T* row = (const T*)a.logits + (size_t)r * a.row_stride;
+    const Piece<T> p(row, min((uint32_t)i * kPiece, (uint32_t)a.V), a.V, lane);
     copy_table(s_table);
     const DrawPlan plan = w.plan[r];
     if (i >= w.n_pieces || plan.take == kTakeSlow || plan.m == -INFINITY) return;
@@ -559,31 +600,49 @@ __global__ __launch_bounds__(kWgWaves * 64) void draw_cut_kernel(DrawArgs a, Dra
     const bool odd = weight.infinite || weight.greedy;
     double kept = 0.0, all = 0.0, above = 0.0;
     uint32_t mine = 0;                                          // one bit an entry: a candidate
-    auto each = [&](auto&& f) {
-#pragma unroll
-        for (int q = 0; q < p.Q; ++q)
-#pragma unroll
-            for (int e = 0; e < p.N; ++e) f(p.at(q, e), q * p.N + e);
-    };
     const bool limited = set.min_p > 0.0, by_count = set.top_k != 0;
-    // what counts for the mass that top-p goes by; what is kept for sure; the candidates
-    auto some = [&](float l, int i, double x) {
-        const bool sure = l >= plan.keep;
-        above += sure ? x : 0.0;
-        all += x;
-        mine |= !sure && l >= plan.list ? 1u << i : 0u;
+    // `all`: what counts for the mass that top-p goes by; `kept`, where min-p is at work, and `above`: what is kept for sure; and the candidates
+    auto each = [&](auto&& f) {
+        for_each_four(p, [&](const float (&l)[4], int i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f(l[j], i + j, weight(clean(l[j])));
+        });
     };
-    auto some_more = [&](float l, int i, double x) {
-        const bool sure = l >= plan.keep, counted = !by_count || l >= plan.k_keep;
-        above += sure ? x : 0.0;
-        kept += sure && x >= set.min_p ? x : 0.0;
-        all += counted ? x : 0.0;
-        mine |= (!sure && l >= plan.list) || (!counted && l >= plan.k_list) ? 1u << i : 0u;
-    };
-    if (plan.take == kTakeListed) each([&](float l, int i) { mine |= l >= plan.list ? 1u << i : 0u; });
-    else if (plan.take == kTakeAll) each([&](float l, int) { const double x = weight(l); kept += x >= set.min_p ? x : 0.0; });
-    else if (odd || limited || by_count) each([&](float l, int i) { some_more(l, i, weight(l)); });
-    else each([&](float l, int i) { some(l, i, weight.plain(l)); });
+    if (plan.take == kTakeListed) {
+        for_each_four(p, [&](const float (&l)[4], int i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine |= l[j] >= plan.list ? 1u << (i + j) : 0u;
+            settle(mine);
+        });
+    } else if (plan.take == kTakeAll) {
+        each([&](float, int, double x) { kept += x >= set.min_p ? x : 0.0; settle(kept); });
+    } else if (odd || limited || by_count) {
+        each([&](float l, int i, double x) {
+            const bool sure = l >= plan.keep, counted = !by_count || l >= plan.k_keep;
+            above += sure ? x : 0.0;
+            kept += sure && x >= set.min_p ? x : 0.0;
+            all += counted ? x : 0.0;
+            mine |= (!sure && l >= plan.list) || (!counted && l >= plan.k_list) ? 1u << i : 0u;
+            settle(all); settle(above); settle(kept); settle(mine);
+        });
+    } else {
+        double x[4];
+        for_each_four(p, [&](const float (&l)[4], int i) {
+            weight.plain(l, x);
+            all += (x[0] + x[1]) + (x[2] + x[3]);
+            settle(all);
+            // of a distribution with few likely tokens most are below the candidates
+            if (!__builtin_amdgcn_ballot_w64(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= plan.list)) return;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool sure = l[j] >= plan.keep;
+                x[j] = sure ? x[j] : 0.0;
+                mine |= !sure && l[j] >= plan.list ? 1u << (i + j) : 0u;
+            }
+            above += (x[0] + x[1]) + (x[2] + x[3]);
+            settle(above); settle(mine);
+        });
+    }
     if (plan.take == kTakeSome) {
         all = wave_total(all);
         above = wave_total(above);
@@ -605,23 +664,21 @@ __global__ __launch_bounds__(kWgWaves * 64) void draw_cut_kernel(DrawArgs a, Dra
         if (lane >= d) at += o;
     }
     uint32_t base = 0;
-    if (lane == 63) base = atomicAdd(&w.n_listed[r], at);
+    if (lane == 63) base = atomicAdd(&w.n_listed[(size_t)r * kApart], at);
     at += __shfl(base, 63, 64) - n;
-#pragma unroll
-    for (int q = 0; q < p.Q; ++q)
-#pragma unroll
-        for (int e = 0; e < p.N; ++e)
-            if (mine & (1u << (q * p.N + e))) {
-                if (at < kCap) w.list[(size_t)r * kCap + at] = make_uint2(order_key(p.at(q, e)), p.index(q, e));
-                ++at;
-            }
+    // a lane has few, in any of 32 places: it reads them again rather than ask for each place
+    for (; mine && at < kCap; mine &= mine - 1, ++at) {
+        const int i = __builtin_ctz(mine);
+        const uint32_t v = p.first + i / p.N * 64 * p.N + i % p.N;
+        w.list[(size_t)r * kCap + at] = make_uint2(order_key(clean((float)row[v])), v);
+    }
 }
 
 // The end of a row: with CUTS the exact border among the candidates (a radix descent, as in draw_row) and their weights' place among the pieces; the piece in
 // which the number falls; the token in it.
 template <class T, bool CUTS>
-__global__ __launch_bounds__(CUTS ? 512 : 64) void draw_pick_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
-    constexpr int THREADS = CUTS ? 512 : 64;
+__global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a, DrawRows rows, DrawSpace w) {
+    constexpr int THREADS = CUTS ? 512 : 256;
     extern __shared__ uint4 lds_raw[];
     uint2* list = (uint2*)lds_raw;                              // [kCap]
     __shared__ double s_table[64];
@@ -663,7 +720,7 @@ __global__ __launch_bounds__(CUTS ? 512 : 64) void draw_pick_kernel(DrawArgs a, 
     constexpr double UNIT = 1125899906842624.0;                 // 2^50: kCap of them fit 64 bits
     bool slow = false;
     if constexpr (CUTS) {
-        const uint32_t n = w.n_listed[r];
+        const uint32_t n = w.n_listed[(size_t)r * kApart];
         slow = plan.take == kTakeSlow || ((plan.take == kTakeSome || plan.take == kTakeListed) && n > kCap);
         const bool listed = !slow && (plan.take == kTakeSome || plan.take == kTakeListed);
         if (listed) {
@@ -761,7 +818,7 @@ __global__ __launch_bounds__(CUTS ? 512 : 64) void draw_pick_kernel(DrawArgs a, 
             draw_row<T, THREADS>(a, rows, r, s_table);
             return;
         }
-        if (wave != 0) return;
+        if (wave >= 4) { __syncthreads(); return; }             // the barrier of the four waves below
         if (listed)
 #pragma unroll
             for (int j = 0; j < PER; ++j) sum[j] += (double)s_cand[lane * PER + j] * (1.0 / UNIT);
@@ -793,56 +850,71 @@ __global__ __launch_bounds__(CUTS ? 512 : 64) void draw_pick_kernel(DrawArgs a, 
         const int from = __builtin_ctzll(hits);
         piece = __shfl(hit, from, 64); before = __shfl(hit_before, from, 64);
     } else {
-        const int from = 63 - __builtin_clzll(lasts);
-        piece = __shfl(last, from, 64); before = __shfl(last_before, from, 64);
+        const int from = lasts ? 63 - __builtin_clzll(lasts) : 0;
+        piece = max(__shfl(last, from, 64), 0); before = __shfl(last_before, from, 64);
     }
-    const Piece<T> p(row, (uint32_t)piece * kPiece, a.V, lane);
-    auto kept = [&](int q, int e) {
-        const float l = p.at(q, e);
-        const double x = !CUTS || order_key(l) >= floor_key ? weight(l) : 0.0;
-        return CUTS && x < set.min_p ? 0.0 : x;
-    };
-    double own[p.Q], to[p.Q];                                   // all runs of 64 N at once: their scans wait for each other's lanes together
+    // the piece by four waves, RUNS runs of 64 N entries each, whose scans wait for each other's lanes together
+    constexpr int N = RowVec<T>::N, RUNS = kPiece / 64 / N / 4;
+    __shared__ double s_run[4 * RUNS];
+    const uint32_t start = (uint32_t)piece * kPiece + wave * RUNS * 64 * N + lane * N;
+    typename RowVec<T>::type x[RUNS];
+    double own[RUNS], to[RUNS];
 #pragma unroll
-    for (int q = 0; q < p.Q; ++q) {
+    for (int q = 0; q < RUNS; ++q) {
+        const uint32_t v = start + q * 64 * N;
+        if (v + N <= (uint32_t)a.V) x[q] = *(const typename RowVec<T>::type*)(row + v);
+        else
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[q][e] = v + e < (uint32_t)a.V ? row[v + e] : (T)-INFINITY;
+    }
+    auto kept = [&](float l) {
+        const double w = !CUTS || order_key(l) >= floor_key ? weight(l) : 0.0;
+        return CUTS && w < set.min_p ? 0.0 : w;
+    };
+#pragma unroll
+    for (int q = 0; q < RUNS; ++q) {
         own[q] = 0.0;
 #pragma unroll
-        for (int e = 0; e < p.N; ++e) own[q] += kept(q, e);
+        for (int e = 0; e < N; ++e) own[q] += kept(clean((float)x[q][e]));
         to[q] = own[q];
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
 #pragma unroll
-        for (int q = 0; q < p.Q; ++q) {
+        for (int q = 0; q < RUNS; ++q) {
             const double o = __shfl_up(to[q], d, 64);
             if (lane >= d) to[q] += o;
         }
-    uint32_t token = 0;
-    float logit = 0.f;
-    bool found = false;
 #pragma unroll
-    for (int q = 0; q < p.Q; ++q) {
-        const double run = __shfl(to[q], 63, 64);
-        const uint64_t over = __builtin_amdgcn_ballot_w64(own[q] > 0.0 && before + to[q] > target), any = __builtin_amdgcn_ballot_w64(own[q] > 0.0);
-        if (!found && any) {
-            const int from = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any);
-            double s = before + (to[q] - own[q]);               // in that lane: its first entry that exceeds, else its last with a weight
-            uint32_t best = 0;
-            float l = 0.f;
-            bool done = false;
-#pragma unroll
-            for (int e = 0; e < p.N; ++e) {
-                const double x = kept(q, e);
-                s += x;
-                if (!done && x > 0.0) { best = p.index(q, e); l = p.at(q, e); done = s > target; }
-            }
-            token = __shfl(best, from, 64);
-            logit = __shfl(l, from, 64);
-            found = over != 0;
+    for (int q = 0; q < RUNS; ++q)
+        if (lane == 63) s_run[wave * RUNS + q] = to[q];
+    __syncthreads();
+    int run = -1;
+    double run_before = 0.0;
+    for (int i = 0, found = 0; i < 4 * RUNS && !found; ++i) {    // the first whose end exceeds, else the last that has anything
+        if (s_run[i] > 0.0) {
+            run = i;
+            run_before = before;
+            found = before + s_run[i] > target;
         }
-        before += run;
+        before += s_run[i];
     }
-    if (lane == 0) {
+#pragma unroll
+    for (int q = 0; q < RUNS; ++q) {
+        if (run != wave * RUNS + q) continue;
+        const uint64_t over = __builtin_amdgcn_ballot_w64(own[q] > 0.0 && run_before + to[q] > target), any = __builtin_amdgcn_ballot_w64(own[q] > 0.0);
+        if (lane != (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any))) continue;
+        double s = run_before + (to[q] - own[q]);               // in that lane: its first entry that exceeds, else its last with a weight
+        uint32_t token = 0;
+        float logit = 0.f;
+        bool done = false;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float l = clean((float)x[q][e]);
+            const double w = kept(l);
+            s += w;
+            if (!done && w > 0.0) { token = start + q * 64 * N + e; logit = l; done = s > target; }
+        }
         a.tokens[r] = (int32_t)token;
         if (a.logp) a.logp[r] = set.greedy ? 0.f : (float)(weight.log_of(logit, set.temperature) - log_total);
     }
@@ -864,7 +936,7 @@ DrawSpace draw_space(uintptr_t base, int rows, int V, size_t* bytes) {
     w.largest = (float*)(base + take(at, (size_t)rows * w.slices * sizeof(float)));
     w.hist = (uint2*)(base + take(at, (size_t)rows * w.slices * kBins * sizeof(uint2)));
     w.plan = (DrawPlan*)(base + take(at, (size_t)rows * sizeof(DrawPlan)));
-    w.n_listed = (uint32_t*)(base + take(at, (size_t)rows * sizeof(uint32_t)));
+    w.n_listed = (uint32_t*)(base + take(at, (size_t)rows * kApart * sizeof(uint32_t)));
     w.list = (uint2*)(base + take(at, (size_t)rows * kCap * sizeof(uint2)));
     *bytes = at;
     return w;
@@ -879,7 +951,7 @@ hipError_t launch_chunk(const DrawArgs& g, const DrawRows& rows, const DrawSpace
     const dim3 grid(w.slices, g.B), threads(kWgWaves * 64);
     if (!cuts) {
         hipLaunchKernelGGL(draw_sum_kernel<T>, grid, threads, 0, s, g, rows, w);
-        hipLaunchKernelGGL((draw_pick_kernel<T, false>), dim3(g.B), dim3(64), 0, s, g, rows, w);
+        hipLaunchKernelGGL((draw_pick_kernel<T, false>), dim3(g.B), dim3(256), 0, s, g, rows, w);
         return hipGetLastError();
     }
     const int list_lds = kCap * sizeof(uint2);
