@@ -120,11 +120,18 @@ struct Select {
     uint64_t remaining;    // how much (count or mass) must still be covered from the top of the current digit
 };
 
-// Among 256 bins, walking from bin 255 down, the one in which the running total first reaches `remaining`.  By one wave.
+// Among 256 bins, walking from bin 255 down, the one in which the running total first reaches `remaining`.  By one wave.  The sum over COPIES of them,
+// kCopyBins apart.
+constexpr int kCopyBins = 260;         // the copies of a bin lie in different banks
+template <int COPIES>
 __device__ __forceinline__ void pick_digit(const uint64_t* hist, int shift, Select* sel, int lane) {
-    uint64_t b[4], mine = 0;
+    uint64_t b[4] = {}, mine = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { b[i] = hist[lane * 4 + i]; mine += b[i]; }
+    for (int c = 0; c < COPIES; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] += hist[c * kCopyBins + lane * 4 + i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine += b[i];
     uint64_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -223,7 +230,7 @@ __device__ __forceinline__ void draw_row(const DrawArgs& a, const DrawRows& rows
                 if (wave == 0) total_known();
                 __syncthreads();
             }
-            if (wave == 0) pick_digit(hist, shift, &sel, lane);
+            if (wave == 0) pick_digit<1>(hist, shift, &sel, lane);
         }
         __syncthreads();
         floor_key = sel.prefix > floor_key ? sel.prefix : floor_key;
@@ -522,7 +529,7 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
     }
     __syncthreads();
     const uint32_t n = s_count[b];
-    const double mid = n && b < kBins - 1 ? n * exp(-(b + (s_down[b] + 0.5 * n) / (128.0 * n)) * (1.0 / kPerNat)) : 0.0;
+    const double mid = n && b < kBins - 1 ? (double)((float)n * expf(-((float)b + ((float)s_down[b] / (float)n + 0.5f) * (1.f / 128.f)) * (1.f / kPerNat))) : 0.0;
     uint32_t count = n;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -681,8 +688,10 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
     constexpr int THREADS = CUTS ? 512 : 256;
     extern __shared__ uint4 lds_raw[];
     uint2* list = (uint2*)lds_raw;                              // [kCap]
+    uint64_t* mass = (uint64_t*)(list + kCap);                  // [kCap], 2^-50 of the largest weight
+    constexpr int kDigitCopies = 8;
     __shared__ double s_table[64];
-    __shared__ uint64_t hist[CUTS ? 256 : 1];
+    __shared__ uint64_t hist[CUTS ? kDigitCopies * kCopyBins : 1];
     __shared__ uint64_t s_cand[CUTS ? kMaxPieces : 1];
     __shared__ Select sel;
     __shared__ double s_all, s_above;
@@ -733,47 +742,55 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
                 }
                 all = wave_total(all);
                 above = wave_total(above);
-                if (lane == 0) { s_all = all; s_above = above; }
+                if (lane == 0) { s_all = all; s_above = above; s_z = s_zk = 0; s_differ = 0; }
             }
-            if (tid == 0) { s_z = s_zk = 0; s_differ = 0; }
-            for (uint32_t i = tid; i < n; i += THREADS) list[i] = w.list[(size_t)r * kCap + i];
             for (int i = tid; i < kMaxPieces; i += THREADS) s_cand[i] = 0;
             __syncthreads();
-            // digits that all candidates share are not looked at
+            const uint2* from = w.list + (size_t)r * kCap;
+            const uint32_t key0 = from[0].x;
             uint32_t differ = 0;
-            for (uint32_t i = tid; i < n; i += THREADS) differ |= list[i].x ^ list[0].x;
+            for (uint32_t i = tid; i < n; i += THREADS) {
+                const uint2 e = from[i];
+                list[i] = e;
+                mass[i] = (uint64_t)rint(weight(key_value(e.x)) * UNIT);
+                differ |= e.x ^ key0;
+            }
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) differ |= __shfl_xor(differ, o, 64);
             if (lane == 0 && differ) atomicOr(&s_differ, differ);
             __syncthreads();
             const uint32_t any = s_differ;
-            const int first = any >> 24 ? 24 : any >> 16 ? 16 : any >> 8 ? 8 : 0;
-            const uint32_t shared_bits = first < 24 ? list[0].x & ~((256u << first) - 1u) : 0u;
+            // digits that all candidates share are not looked at (16-bit logits: two of four)
+            uint32_t shared_digits = 0;
+            for (int shift = 0; shift < 32; shift += 8)
+                if ((any >> shift & 255u) == 0) shared_digits |= key0 & (255u << shift);
             auto descend = [&](auto&& amount) {                 // sel.remaining is set
-                if (tid == 0) sel.prefix = shared_bits;
-                for (int shift = first; shift >= 0; shift -= 8) {
-                    if (tid < 256) hist[tid] = 0;
+                if (tid == 0) sel.prefix = shared_digits;
+                for (int shift = 24; shift >= 0; shift -= 8) {
+                    if ((any >> shift & 255u) == 0) continue;
+                    for (int i = tid; i < kDigitCopies * kCopyBins; i += THREADS) hist[i] = 0;
                     __syncthreads();
                     const uint32_t prefix = sel.prefix;
                     for (uint32_t i = tid; i < n; i += THREADS) {
                         const uint32_t key = list[i].x;
-                        if (key >= floor_key && (shift == first || (key >> (shift + 8)) == (prefix >> (shift + 8)))) {
-                            const uint64_t x = amount(key);
-                            if (x) atomicAdd((unsigned long long*)&hist[key >> shift & 255u], (unsigned long long)x);
+                        if (key >= floor_key && (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8)))) {
+                            const uint64_t x = amount(key, i);
+                            if (x) atomicAdd((unsigned long long*)&hist[(lane & (kDigitCopies - 1)) * kCopyBins + (key >> shift & 255u)], (unsigned long long)x);
                         }
                     }
                     __syncthreads();
-                    if (wave == 0) pick_digit(hist, shift, &sel, lane);
+                    if (wave == 0) pick_digit<kDigitCopies>(hist, shift, &sel, lane);
                     __syncthreads();
                 }
+                __syncthreads();
                 floor_key = sel.prefix > floor_key ? sel.prefix : floor_key;
+                __syncthreads();
             };
-            auto mass = [&](uint32_t key) { return (uint64_t)rint(weight(key_value(key)) * UNIT); };
             // only those below k_keep are counted: the others are in number known
             const uint32_t sure_key = plan.take == kTakeListed || plan.k_keep != plan.k_keep ? 0xFFFFFFFFu : order_key(plan.k_keep);
             if (set.top_k) {
                 if (tid == 0) sel.remaining = (uint64_t)set.top_k - (plan.take == kTakeListed ? 0u : plan.k_above);
-                descend([&](uint32_t key) { return key < sure_key ? (uint64_t)1 : (uint64_t)0; });
+                descend([&](uint32_t key, uint32_t) { return key < sure_key ? (uint64_t)1 : (uint64_t)0; });
             }
             if (set.top_p < 1.0) {
                 // the mass of what the count leaves: all candidates', and of that what lies below k_keep (the rest is in s_all already)
@@ -781,9 +798,8 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
                 for (uint32_t i = tid; i < n; i += THREADS) {
                     const uint32_t key = list[i].x;
                     if (key < floor_key) continue;
-                    const uint64_t x = mass(key);
-                    z += x;
-                    if (set.top_k && key < sure_key) zk += x;
+                    z += mass[i];
+                    if (set.top_k && key < sure_key) zk += mass[i];
                 }
 #pragma unroll
                 for (int o = 32; o > 0; o >>= 1) { z += shfl_down_u64(z, o); zk += shfl_down_u64(zk, o); }
@@ -800,17 +816,28 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
                 __syncthreads();
                 slow = !s_found;
                 if (!slow) {
-                    descend(mass);
+                    descend([&](uint32_t, uint32_t i) { return mass[i]; });
                     // below its run of candidates there is a gap down to those of the count
                     slow = plan.take == kTakeSome && floor_key < order_key(plan.list);
                 }
             }
             if (!slow) {
-                for (uint32_t i = tid; i < n; i += THREADS) {
+                // A thread has neighbours of the list, which come from one piece mostly: it adds them up before it adds to the piece's sum.  (Neighbouring lanes on
+                // neighbouring entries would all wait for one sum.)
+                const uint32_t per = (n + THREADS - 1) / THREADS, first = tid * per, end = min(first + per, n);
+                uint32_t piece = 0;
+                uint64_t x = 0;
+                for (uint32_t i = first; i < end; ++i) {
                     const uint2 e = list[i];
-                    if (e.x < floor_key || weight(key_value(e.x)) < set.min_p) continue;
-                    atomicAdd((unsigned long long*)&s_cand[e.y / kPiece], (unsigned long long)mass(e.x));
+                    if (e.x < floor_key || (set.min_p > 0.0 && weight(key_value(e.x)) < set.min_p)) continue;
+                    if (e.y / kPiece != piece) {
+                        if (x) atomicAdd((unsigned long long*)&s_cand[piece], (unsigned long long)x);
+                        piece = e.y / kPiece;
+                        x = 0;
+                    }
+                    x += mass[i];
                 }
+                if (x) atomicAdd((unsigned long long*)&s_cand[piece], (unsigned long long)x);
                 __syncthreads();
             }
         }
@@ -954,7 +981,7 @@ hipError_t launch_chunk(const DrawArgs& g, const DrawRows& rows, const DrawSpace
         hipLaunchKernelGGL((draw_pick_kernel<T, false>), dim3(g.B), dim3(256), 0, s, g, rows, w);
         return hipGetLastError();
     }
-    const int list_lds = kCap * sizeof(uint2);
+    const int list_lds = kCap * (sizeof(uint2) + sizeof(uint64_t));          // and 23 KB of its own: one workgroup a compute unit, which has one row at most
     hipLaunchKernelGGL(draw_count_kernel<T>, grid, threads, 0, s, g, rows, w);
     hipLaunchKernelGGL(draw_plan_kernel, dim3(g.B), dim3(kBins), 0, s, g, rows, w);
     hipLaunchKernelGGL(draw_cut_kernel<T>, grid, threads, 0, s, g, rows, w);
