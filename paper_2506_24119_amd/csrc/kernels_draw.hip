@@ -20,28 +20,44 @@ template <> struct RowVec<float> { static constexpr int N = 4; typedef float typ
 template <> struct RowVec<__bf16> { static constexpr int N = 8; typedef __bf16 type __attribute__((ext_vector_type(8), aligned(2))); };
 template <> struct RowVec<_Float16> { static constexpr int N = 8; typedef _Float16 type __attribute__((ext_vector_type(8), aligned(2))); };
 
-__device__ __forceinline__ uint64_t shfl_down_u64(uint64_t v, int d) {
-    const uint32_t lo = __shfl_down((uint32_t)v, d, 64), hi = __shfl_down((uint32_t)(v >> 32), d, 64);
-    return ((uint64_t)hi << 32) | lo;
+// Sums and maxima over a wave without a trip through LDS (an exchange of lanes there takes a hundred cycles, and a sum of 64 bits needs two for each of its six
+// steps): within rows of 16 lanes by shifts, then the last lane of a row to the next row and that of the second to the third and fourth.  All lanes are active.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t x, uint32_t none) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, CTRL, ROWS, 0xF, false);
 }
-__device__ __forceinline__ double wave_total(double v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t moved(uint64_t x) {
+    return ((uint64_t)moved<CTRL, ROWS>((uint32_t)(x >> 32), 0u) << 32) | moved<CTRL, ROWS>((uint32_t)x, 0u);
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double x) {
+    return __longlong_as_double((long long)moved<CTRL, ROWS>((uint64_t)__double_as_longlong(x)));
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t x) { return moved<CTRL, ROWS>(x, 0u); }
+// the sum over the lanes up to this one
+template <class V> __device__ __forceinline__ V wave_scan(V v) {
+    v += moved<0x111, 0xF>(v);
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);
+    v += moved<0x143, 0xC>(v);
     return v;
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ uint64_t last_lane(uint64_t v) { return ((uint64_t)last_lane((uint32_t)(v >> 32)) << 32) | last_lane((uint32_t)v); }
+__device__ __forceinline__ double last_lane(double v) { return __longlong_as_double((long long)last_lane((uint64_t)__double_as_longlong(v))); }
+template <class V> __device__ __forceinline__ V wave_total(V v) { return last_lane(wave_scan(v)); }
+template <int CTRL, int ROWS> __device__ __forceinline__ float larger(float v) {
+    const uint32_t x = __float_as_uint(v);
+    return fmaxf(v, __uint_as_float(moved<CTRL, ROWS>(x, x)));
 }
 __device__ __forceinline__ float wave_largest(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
-}
-// the sum over the lanes up to this one
-__device__ __forceinline__ double wave_scan(double v, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double o = __shfl_up(v, d, 64);
-        if (lane >= d) v += o;
-    }
-    return v;
+    v = larger<0x111, 0xF>(v);
+    v = larger<0x112, 0xF>(v);
+    v = larger<0x114, 0xF>(v);
+    v = larger<0x118, 0xF>(v);
+    v = larger<0x142, 0xA>(v);
+    v = larger<0x143, 0xC>(v);
+    return __uint_as_float(last_lane(__float_as_uint(v)));
 }
 
 // 2^(j / 64), j = 0 .. 63, evaluated by the host's compiler from the definition
@@ -125,44 +141,40 @@ struct Select {
 constexpr int kCopyBins = 260;         // the copies of a bin lie in different banks
 template <int COPIES>
 __device__ __forceinline__ void pick_digit(const uint64_t* hist, int shift, Select* sel, int lane) {
+    const int top = 255 - 4 * lane;                  // a lane has four bins down from here
     uint64_t b[4] = {}, mine = 0;
 #pragma unroll
     for (int c = 0; c < COPIES; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] += hist[c * kCopyBins + lane * 4 + i];
+        for (int i = 0; i < 4; ++i) b[i] += hist[c * kCopyBins + top - i];
 #pragma unroll
     for (int i = 0; i < 4; ++i) mine += b[i];
-    uint64_t incl = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = shfl_down_u64(incl, d);
-        if (lane + d < 64) incl += o;
-    }
+    const uint64_t incl = wave_scan(mine);
     uint64_t acc = incl - mine;
     const uint64_t need = sel->remaining;
     if (acc < need && need <= incl) {               // exactly one lane
 #pragma unroll
-        for (int i = 3; i >= 0; --i) {
-            if (acc + b[i] >= need) { sel->prefix |= (uint32_t)(lane * 4 + i) << shift; sel->remaining = need - acc; break; }
+        for (int i = 0; i < 4; ++i) {
+            if (acc + b[i] >= need) { sel->prefix |= (uint32_t)(top - i) << shift; sel->remaining = need - acc; break; }
             acc += b[i];
         }
     }
 }
 
-// the sum of 256 bins, in the first lane of the wave that calls this
+// the sum of 256 bins, by a wave
 __device__ __forceinline__ uint64_t sum_of(const uint64_t* hist, int lane) {
     uint64_t z = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) z += hist[lane * 4 + i];
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) z += shfl_down_u64(z, d);
-    return z;
+    return wave_total(z);
 }
 __device__ __forceinline__ uint64_t share_of(double p, uint64_t z) {
     const uint64_t target = (uint64_t)ceil(p * (double)z);
     return target < 1 ? 1 : target > z ? z : target;
 }
 __device__ __forceinline__ double number_of(float u) { return (double)fminf(fmaxf(u, 0.f), 0.99999994f); }      // fmaxf: a NaN counts as 0
+
+constexpr int kCached = 16384;         // entries of a row that fit LDS (64 KB)
 
 struct RowSettings {
     float temperature;
@@ -185,8 +197,9 @@ __device__ __forceinline__ void nothing_to_draw(const DrawArgs& a, int r) {
 
 // A row by a workgroup, in as many sweeps of it as the cuts need: one for the maximum, four digits of the k-th largest key, four of the
 // key at which the mass reaches p, one for the sum of what is kept and a part of one for the token.
+// cache: or null, LDS for the row (short ones), which is then read once.
 template <class T, int THREADS>
-__device__ __forceinline__ void draw_row(const DrawArgs& a, const DrawRows& rows, int r, const double* table) {
+__device__ __forceinline__ void draw_row(const DrawArgs& a, const DrawRows& rows, int r, const double* table, float* cache) {
     constexpr int WAVES = THREADS / 64;
     __shared__ uint64_t hist[256];
     __shared__ Select sel;
@@ -195,10 +208,14 @@ __device__ __forceinline__ void draw_row(const DrawArgs& a, const DrawRows& rows
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T* row = (const T*)a.logits + (size_t)r * a.row_stride;
     const uint32_t V = a.V;
-    auto logit_at = [&](uint32_t v) { return clean((float)row[v]); };
+    auto logit_at = [&](uint32_t v) { return cache ? cache[v] : clean((float)row[v]); };
 
     float m = -INFINITY;
-    for (uint32_t v = tid; v < V; v += THREADS) m = fmaxf(m, logit_at(v));
+    for (uint32_t v = tid; v < V; v += THREADS) {
+        const float l = clean((float)row[v]);
+        if (cache) cache[v] = l;
+        m = fmaxf(m, l);
+    }
     m = wave_largest(m);
     if (lane == 0) s_max[wave] = m;
     __syncthreads();
@@ -281,11 +298,11 @@ __device__ __forceinline__ void draw_row(const DrawArgs& a, const DrawRows& rows
     for (uint32_t v0 = lo; v0 < hi && !found; v0 += 64) {
         const uint32_t v = v0 + lane;
         const double w = v < hi ? kept(logit_at(v)) : 0.0;
-        const double c = wave_scan(w, lane);
+        const double c = wave_scan(w);
         const uint64_t over = __builtin_amdgcn_ballot_w64(w > 0.0 && before + c > target), any = __builtin_amdgcn_ballot_w64(w > 0.0);
         if (over) { token = v0 + __builtin_ctzll(over); found = true; }
         else if (any) token = v0 + 63 - __builtin_clzll(any);
-        before += __shfl(c, 63, 64);
+        before += last_lane(c);
     }
     if (lane == 0) {
         a.tokens[r] = (int32_t)token;
@@ -430,9 +447,10 @@ __device__ __forceinline__ void copy_table(double* s_table) {
 
 template <class T>
 __global__ __launch_bounds__(1024) void draw_row_kernel(DrawArgs a, DrawRows rows) {
+    extern __shared__ uint4 lds_raw[];
     __shared__ double s_table[64];
     copy_table(s_table);
-    draw_row<T, 1024>(a, rows, blockIdx.x, s_table);
+    draw_row<T, 1024>(a, rows, blockIdx.x, s_table, a.V <= kCached ? (float*)lds_raw : nullptr);
 }
 
 // Batches without a cut: one sweep.
@@ -530,13 +548,8 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
     __syncthreads();
     const uint32_t n = s_count[b];
     const double mid = n && b < kBins - 1 ? (double)((float)n * expf(-((float)b + ((float)s_down[b] / (float)n + 0.5f) * (1.f / 128.f)) * (1.f / kPerNat))) : 0.0;
-    uint32_t count = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = __shfl_up(count, d, 64);
-        if (lane >= d) count += o;
-    }
-    double mass = wave_scan(mid, lane);
+    uint32_t count = wave_scan(n);
+    double mass = wave_scan(mid);
     if (lane == 63) { s_wave[wave] = count; s_mass[wave] = mass; }
     __syncthreads();
     double all = 0.0;
@@ -610,10 +623,18 @@ __global__ __launch_bounds__(kWgWaves * 64, 5) void draw_cut_kernel(DrawArgs a, 
     const bool limited = set.min_p > 0.0, by_count = set.top_k != 0;
     // `all`: what counts for the mass that top-p goes by; `kept`, where min-p is at work, and `above`: what is kept for sure; and the candidates
     auto each = [&](auto&& f) {
-        for_each_four(p, [&](const float (&l)[4], int i) {
+        double x[4];
+        if (odd)
+            for_each_four(p, [&](const float (&l)[4], int i) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f(l[j], i + j, weight(clean(l[j])));
-        });
+                for (int j = 0; j < 4; ++j) x[j] = weight(clean(l[j]));
+                f(l, i, x);
+            });
+        else
+            for_each_four(p, [&](const float (&l)[4], int i) {
+                weight.plain(l, x);
+                f(l, i, x);
+            });
     };
     if (plan.take == kTakeListed) {
         for_each_four(p, [&](const float (&l)[4], int i) {
@@ -622,14 +643,22 @@ __global__ __launch_bounds__(kWgWaves * 64, 5) void draw_cut_kernel(DrawArgs a, 
             settle(mine);
         });
     } else if (plan.take == kTakeAll) {
-        each([&](float, int, double x) { kept += x >= set.min_p ? x : 0.0; settle(kept); });
+        each([&](const float (&)[4], int, double (&x)[4]) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = x[j] >= set.min_p ? x[j] : 0.0;
+            kept += (x[0] + x[1]) + (x[2] + x[3]);
+            settle(kept);
+        });
     } else if (odd || limited || by_count) {
-        each([&](float l, int i, double x) {
-            const bool sure = l >= plan.keep, counted = !by_count || l >= plan.k_keep;
-            above += sure ? x : 0.0;
-            kept += sure && x >= set.min_p ? x : 0.0;
-            all += counted ? x : 0.0;
-            mine |= (!sure && l >= plan.list) || (!counted && l >= plan.k_list) ? 1u << i : 0u;
+        each([&](const float (&l)[4], int i, double (&x)[4]) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool sure = l[j] >= plan.keep, counted = !by_count || l[j] >= plan.k_keep;
+                above += sure ? x[j] : 0.0;
+                kept += sure && x[j] >= set.min_p ? x[j] : 0.0;
+                all += counted ? x[j] : 0.0;
+                mine |= (!sure && l[j] >= plan.list) || (!counted && l[j] >= plan.k_list) ? 1u << (i + j) : 0u;
+            }
             settle(all); settle(above); settle(kept); settle(mine);
         });
     } else {
@@ -664,15 +693,10 @@ __global__ __launch_bounds__(kWgWaves * 64, 5) void draw_cut_kernel(DrawArgs a, 
             for (int e = 0; e < p.N; ++e)
                 if (p.index(q, e) >= p.V) mine &= ~(1u << (q * p.N + e));
     if (!__builtin_amdgcn_ballot_w64(mine != 0)) return;
-    uint32_t at = __popc(mine), n = at;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = __shfl_up(at, d, 64);
-        if (lane >= d) at += o;
-    }
-    uint32_t base = 0;
+    const uint32_t n = __popc(mine);
+    uint32_t at = wave_scan(n), base = 0;
     if (lane == 63) base = atomicAdd(&w.n_listed[(size_t)r * kApart], at);
-    at += __shfl(base, 63, 64) - n;
+    at += last_lane(base) - n;
     // a lane has few, in any of 32 places: it reads them again rather than ask for each place
     for (; mine && at < kCap; mine &= mine - 1, ++at) {
         const int i = __builtin_ctz(mine);
@@ -801,8 +825,8 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
                     z += mass[i];
                     if (set.top_k && key < sure_key) zk += mass[i];
                 }
-#pragma unroll
-                for (int o = 32; o > 0; o >>= 1) { z += shfl_down_u64(z, o); zk += shfl_down_u64(zk, o); }
+                z = wave_total(z);
+                zk = wave_total(zk);
                 if (lane == 0) { atomicAdd((unsigned long long*)&s_z, (unsigned long long)z); atomicAdd((unsigned long long*)&s_zk, (unsigned long long)zk); }
                 __syncthreads();
                 if (tid == 0) {
@@ -842,7 +866,7 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
             }
         }
         if (slow) {
-            draw_row<T, THREADS>(a, rows, r, s_table);
+            draw_row<T, THREADS>(a, rows, r, s_table, nullptr);
             return;
         }
         if (wave >= 4) { __syncthreads(); return; }             // the barrier of the four waves below
@@ -857,7 +881,7 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
         if (ref[j] != m) sum[j] = sum[j] > 0.0 ? sum[j] * weight(ref[j]) : 0.0;
         mine += sum[j];
     }
-    const double upto = wave_scan(mine, lane), total = __shfl(upto, 63, 64);
+    const double upto = wave_scan(mine), total = last_lane(upto);
     const double target = set.greedy ? 0.0 : number_of(a.uniform[r]) * total;
     // the first piece whose running sum exceeds the target, else the last that has anything
     double c = upto - mine, before = 0.0;
@@ -880,7 +904,7 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
         const int from = lasts ? 63 - __builtin_clzll(lasts) : 0;
         piece = max(__shfl(last, from, 64), 0); before = __shfl(last_before, from, 64);
     }
-    // the piece by four waves, RUNS runs of 64 N entries each, whose scans wait for each other's lanes together
+    // the piece by four waves, RUNS runs of 64 N entries each
     constexpr int N = RowVec<T>::N, RUNS = kPiece / 64 / N / 4;
     __shared__ double s_run[4 * RUNS];
     const uint32_t start = (uint32_t)piece * kPiece + wave * RUNS * 64 * N + lane * N;
@@ -903,15 +927,8 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
         own[q] = 0.0;
 #pragma unroll
         for (int e = 0; e < N; ++e) own[q] += kept(clean((float)x[q][e]));
-        to[q] = own[q];
+        to[q] = wave_scan(own[q]);
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-        for (int q = 0; q < RUNS; ++q) {
-            const double o = __shfl_up(to[q], d, 64);
-            if (lane >= d) to[q] += o;
-        }
 #pragma unroll
     for (int q = 0; q < RUNS; ++q)
         if (lane == 63) s_run[wave * RUNS + q] = to[q];
@@ -948,7 +965,7 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
 }
 
 namespace {
-bool in_pieces(int V) { return V >= 16384 && V <= kPiece * kMaxPieces; }
+bool in_pieces(int V) { return V >= kCached && V <= kPiece * kMaxPieces; }
 size_t take(size_t& at, size_t bytes) {
     const size_t o = at;
     at += (bytes + 255) & ~(size_t)255;
@@ -972,7 +989,7 @@ DrawSpace draw_space(uintptr_t base, int rows, int V, size_t* bytes) {
 template <class T>
 hipError_t launch_chunk(const DrawArgs& g, const DrawRows& rows, const DrawSpace& w, bool pieces, bool cuts, hipStream_t s) {
     if (!pieces) {
-        hipLaunchKernelGGL(draw_row_kernel<T>, dim3(g.B), dim3(1024), 0, s, g, rows);
+        hipLaunchKernelGGL(draw_row_kernel<T>, dim3(g.B), dim3(1024), g.V <= kCached ? (unsigned)(g.V * sizeof(float)) : 0, s, g, rows);
         return hipGetLastError();
     }
     const dim3 grid(w.slices, g.B), threads(kWgWaves * 64);
