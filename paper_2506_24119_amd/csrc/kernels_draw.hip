@@ -319,7 +319,7 @@ constexpr int kSlice = kPiece * kWgWaves;
 constexpr int kBins = 1024, kPerNat = 32;          // bins over the 32 below the maximum of (l - m) / T, and the last for what lies further down
 constexpr int kCopies = 4;            // of a histogram: neighbouring lanes do not meet in one
 constexpr uint32_t kOne = 1u << 19;   // an entry in it; below, the sum of places of seven bits.  Room for all that lanes of one copy have:
-static_assert(kSlice / kCopies * 127 < (int)kOne && kSlice / kCopies < (1 << 13), "a copy's bin overflows");
+static_assert(kSlice / kCopies * 127 < (int)kOne && kSlice / kCopies < (1 << 13) && kSlice < (1 << 16), "a bin overflows");
 constexpr int kCap = 8192;            // candidates of a row
 constexpr int kApart = 64;            // words between the counters of rows: atomics of different rows do not queue for one cache line
 constexpr int kTakeAll = 0, kTakeSome = 1, kTakeListed = 2, kTakeSlow = 3;
@@ -388,7 +388,7 @@ __device__ __forceinline__ float least_logit(float f, float scale, int lane) {
 struct DrawSpace {                    // the workspace of a launch's rows
     PieceSums* pieces;                // [rows][kMaxPieces]: n_pieces of them used
     float* largest;                   // [rows][slices]
-    uint2* hist;                      // [rows][slices][kBins]: entries, and how far down in the bin they lie, in all
+    uint32_t* hist;                   // [rows][slices][kBins]: entries, and below their number 512 times the mean of their places
     DrawPlan* plan;                   // [rows]
     uint32_t* n_listed;               // [rows][kApart]
     uint2* list;                      // [rows][kCap]: key, index
@@ -502,7 +502,7 @@ __global__ __launch_bounds__(kWgWaves * 64) void draw_count_kernel(DrawArgs a, D
             n.x += x / kOne;
             n.y += x % kOne;
         }
-        w.hist[seg * kBins + b] = n;
+        w.hist[seg * kBins + b] = n.x ? n.x << 16 | n.y * 512 / n.x : 0u;
     }
 }
 
@@ -518,12 +518,15 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
     const RowSettings set(rows, r, a.V);
     static_assert(kMaxPieces / kWgWaves <= 64, "a lane has a slice");
     const float mine = lane < w.slices ? w.largest[(size_t)r * w.slices + lane] : -INFINITY;
-    uint2 n8[8];                                                // the first slices' bins are on their way meanwhile
-    const uint2* hist = w.hist + (size_t)r * w.slices * kBins + b;
+    uint32_t n8[8], next8[8];                                   // the first slices' bins are on their way meanwhile
+    const uint32_t* hist = w.hist + (size_t)r * w.slices * kBins + b;
     const bool binned = set.top_k || set.top_p < 1.0;
     if (binned)
 #pragma unroll
-        for (int s = 0; s < 8; ++s) n8[s] = s < w.slices ? hist[(size_t)s * kBins] : make_uint2(0, 0);
+        for (int s = 0; s < 8; ++s) {
+            n8[s] = s < w.slices ? hist[(size_t)s * kBins] : 0u;
+            next8[s] = 8 + s < w.slices ? hist[(size_t)(8 + s) * kBins] : 0u;
+        }
     const float m = wave_largest(mine);
     DrawPlan plan = {m, kTakeAll, -INFINITY, -INFINITY, -INFINITY, -INFINITY, 0u, 0};
     if (b == 0) w.n_listed[(size_t)r * kApart] = 0;
@@ -540,14 +543,20 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
             const int to = (int)fminf((float)b + __shfl(down, s0 + s, 64), (float)(kBins - 1));
-            if (n8[s].x) { atomicAdd(&s_count[to], n8[s].x); atomicAdd(&s_down[to], n8[s].y); }
+            if (n8[s]) {
+                atomicAdd(&s_count[to], n8[s] >> 16);
+                atomicAdd(&s_down[to], (n8[s] >> 16) * (n8[s] & 0xFFFFu) >> 5);          // 16 times the places' sum
+            }
         }
 #pragma unroll
-        for (int s = 0; s < 8; ++s) n8[s] = s0 + 8 + s < w.slices ? hist[(size_t)(s0 + 8 + s) * kBins] : make_uint2(0, 0);
+        for (int s = 0; s < 8; ++s) {
+            n8[s] = next8[s];
+            next8[s] = s0 + 16 + s < w.slices ? hist[(size_t)(s0 + 16 + s) * kBins] : 0u;
+        }
     }
     __syncthreads();
     const uint32_t n = s_count[b];
-    const double mid = n && b < kBins - 1 ? (double)((float)n * expf(-((float)b + ((float)s_down[b] / (float)n + 0.5f) * (1.f / 128.f)) * (1.f / kPerNat))) : 0.0;
+    const double mid = n && b < kBins - 1 ? (double)((float)n * expf(-((float)b + ((float)s_down[b] / (float)n * (1.f / 16.f) + 0.5f) * (1.f / 128.f)) * (1.f / kPerNat))) : 0.0;
     uint32_t count = wave_scan(n);
     double mass = wave_scan(mid);
     if (lane == 63) { s_wave[wave] = count; s_mass[wave] = mass; }
@@ -732,9 +741,15 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
     float ref[PER];
     float m = -INFINITY;
     DrawPlan plan = {};
+    constexpr int AHEAD = CUTS ? 4 : 1;                         // entries of the list, read before it is known whether there are so many
+    uint2 ahead[AHEAD], first_entry = {};
+    const uint2* from = w.list + (size_t)r * kCap;
     if (CUTS) {
         plan = w.plan[r];
         m = plan.m;
+        first_entry = from[0];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) ahead[j] = from[tid + j * THREADS];
     }
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -770,15 +785,17 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
             }
             for (int i = tid; i < kMaxPieces; i += THREADS) s_cand[i] = 0;
             __syncthreads();
-            const uint2* from = w.list + (size_t)r * kCap;
-            const uint32_t key0 = from[0].x;
+            const uint32_t key0 = first_entry.x;
             uint32_t differ = 0;
-            for (uint32_t i = tid; i < n; i += THREADS) {
-                const uint2 e = from[i];
+            auto enter = [&](uint32_t i, uint2 e) {
                 list[i] = e;
                 mass[i] = (uint64_t)rint(weight(key_value(e.x)) * UNIT);
                 differ |= e.x ^ key0;
-            }
+            };
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                if (tid + j * THREADS < n) enter(tid + j * THREADS, ahead[j]);
+            for (uint32_t i = tid + AHEAD * THREADS; i < n; i += THREADS) enter(i, from[i]);
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) differ |= __shfl_xor(differ, o, 64);
             if (lane == 0 && differ) atomicOr(&s_differ, differ);
@@ -978,7 +995,7 @@ DrawSpace draw_space(uintptr_t base, int rows, int V, size_t* bytes) {
     size_t at = 0;
     w.pieces = (PieceSums*)(base + take(at, (size_t)rows * kMaxPieces * sizeof(PieceSums)));
     w.largest = (float*)(base + take(at, (size_t)rows * w.slices * sizeof(float)));
-    w.hist = (uint2*)(base + take(at, (size_t)rows * w.slices * kBins * sizeof(uint2)));
+    w.hist = (uint32_t*)(base + take(at, (size_t)rows * w.slices * kBins * sizeof(uint32_t)));
     w.plan = (DrawPlan*)(base + take(at, (size_t)rows * sizeof(DrawPlan)));
     w.n_listed = (uint32_t*)(base + take(at, (size_t)rows * kApart * sizeof(uint32_t)));
     w.list = (uint2*)(base + take(at, (size_t)rows * kCap * sizeof(uint2)));
