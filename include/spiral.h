@@ -351,7 +351,7 @@ int spiral_sample_uniform(const void* dev_logits, int logits_dtype, long long ro
  * dev_workspace: 256-byte aligned, spiral_policy_gradient_workspace_bytes(n_rows, V) bytes (0 for invalid sizes), contents undefined before
  * and after; calls that share it must be ordered on one stream.
  * Errors: INVALID_ARG (null or misaligned pointer, n_rows or V < 1, more than 2^31 - 1 rows, unknown type, a stride < V,
- * overlapping buffers, temperature not positive and finite, clip_eps negative or not finite, scale not finite, workspace too small), HIP. */
+ * overlapping buffers, temperature below 1e-30 or not finite, clip_eps negative or not finite, scale not finite, workspace too small), HIP. */
 size_t spiral_policy_gradient_workspace_bytes(long long n_rows, int V);
 int spiral_policy_gradient(const void* dev_logits, int dtype, long long row_stride, long long n_rows, int V,
                            const int32_t* dev_targets, const float* dev_logp_old, const float* dev_advantage,
@@ -386,7 +386,7 @@ typedef struct spiral_adamw_tensor {
 /* spiral_adamw_create copies the table into the caller's device memory (dev_mem, spiral_adamw_bytes(n_tensors) bytes, 0 on a bad count; 256-byte
  * aligned), enqueued on `stream`; it must stay valid as long as the object, and nothing else is kept.  Tensors are aligned to their elements.
  * No buffer that a step writes may overlap another buffer of the table; gradients are only read.  spiral_adamw_set_grads exchanges the
- * gradients' addresses (host_dev_grads [n_tensors], same sizes and types) for the steps enqueued on `stream` after it.
+ * gradients' addresses (host_dev_grads [n_tensors], same sizes and types, under the same rules) for the steps enqueued on `stream` after it.
  * Errors: INVALID_ARG (null or misaligned pointer, unknown or impossible types, n < 1, overlap), HIP; NOT_LOADED (null object). */
 size_t spiral_adamw_bytes(int n_tensors);
 int  spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int n_tensors, void* dev_mem, size_t bytes, void* stream,
@@ -394,8 +394,9 @@ int  spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int n_tensors,
 int  spiral_adamw_set_grads(spiral_adamw* o, const void* const* host_dev_grads, void* stream);
 /* step >= 1 is the number of this step (a captured call that is replayed keeps it, as it keeps lr and the others).
  * max_norm == 0: gradients are not clipped.  dev_norm (fp32 [1] or NULL) receives N.  Where N is computed (max_norm > 0 or
- * dev_norm given) and is not finite in fp32, the step changes no parameter and no state.  Steps of one object must be ordered on one stream.
- * Errors: NOT_LOADED, INVALID_ARG (betas outside [0, 1), eps <= 0, a negative or not finite lr, weight_decay or max_norm, a grad_scale
+ * dev_norm given) and is not finite in fp32, the step changes no parameter and no state; where it is not computed, a gradient that is
+ * not finite leaves its element undefined, and of 8-bit states its block.  Steps of one object must be ordered on one stream.
+ * Errors: NOT_LOADED, INVALID_ARG (betas outside [0, 1), eps outside [1e-30, 1e30], a negative or not finite lr, weight_decay or max_norm, a grad_scale
  * that is not finite, step < 1, misaligned dev_norm), HIP. */
 int  spiral_adamw_step(spiral_adamw* o, double lr, double beta1, double beta2, double eps, double weight_decay, int step,
                        float grad_scale, float max_norm, float* dev_norm, void* stream);

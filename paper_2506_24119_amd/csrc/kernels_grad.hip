@@ -48,7 +48,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ float policy_slope(const GradArgs& a, long long row, float logp) {
     const float A = a.advantage[row];
     float d = logp == logp ? A : NAN;
-    if (a.logp_old) {
+    if (a.logp_old && A != 0.f) {                      // no advantage, no slope: not that of an infinite ratio either
         const float r = expf(logp - a.logp_old[row]);
         const float rc = fminf(fmaxf(r, 1.f - a.clip_eps), 1.f + a.clip_eps);
         d = r * A <= rc * A ? r * A : r * A > rc * A ? 0.f : NAN;
@@ -276,7 +276,7 @@ size_t policy_grad_workspace_bytes(long long n_rows, int V) {
 }
 
 template <class T>
-static hipError_t launch_rows(const GradArgs& a, int slices, void* workspace, hipStream_t s) {
+static hipError_t launch_some(const GradArgs& a, int slices, void* workspace, hipStream_t s) {
     const uint32_t n_vec = (uint32_t)a.V / RowVec<T>::N;
     if (slices > 1) {
         const uint32_t per = (n_vec + slices - 1) / slices;
@@ -299,6 +299,26 @@ static hipError_t launch_rows(const GradArgs& a, int slices, void* workspace, hi
     else if (n_vec <= 1024 * 8 || !WIDE) hipLaunchKernelGGL((policy_grad_kernel<T, 1024, 8, 8>), grid, dim3(1024), 0, s, a);
     else hipLaunchKernelGGL((policy_grad_kernel<T, 1024, WIDE ? 20 : 8, WIDE ? 4 : 8>), grid, dim3(1024), 0, s, a);
     return hipGetLastError();
+}
+
+// A launch has at most 2^32 threads: 2^20 rows at a time.
+template <class T>
+static hipError_t launch_rows(const GradArgs& a, int slices, void* workspace, hipStream_t s) {
+    constexpr long long MOST = 1ll << 20;
+    for (long long r = 0; r < a.n_rows; r += MOST) {
+        GradArgs g = a;
+        g.n_rows = a.n_rows - r < MOST ? a.n_rows - r : MOST;
+        g.logits = (const T*)a.logits + r * a.row_stride;
+        g.grad = (T*)a.grad + r * a.grad_stride;
+        g.targets += r;
+        if (g.logp_old) g.logp_old += r;
+        g.advantage += r;
+        if (g.mask) g.mask += r;
+        g.logp += r;
+        const hipError_t e = launch_some<T>(g, slices, workspace, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_policy_grad(const GradArgs& a, int dtype, void* workspace, hipStream_t s) {

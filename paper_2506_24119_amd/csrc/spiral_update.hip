@@ -82,7 +82,7 @@ extern "C" int spiral_policy_gradient(const void* dev_logits, int dtype, long lo
     if (!aligned(dev_logits, size) || !aligned(dev_grad, size) || !aligned(dev_targets, 4) || !aligned(dev_logp_old, 4) ||
         !aligned(dev_advantage, 4) || !aligned(dev_mask, 4) || !aligned(dev_logp, 4))
         return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: misaligned buffer");
-    if (!(temperature > 0.f) || !std::isfinite(temperature)) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: temperature must be finite and > 0");
+    if (!(temperature >= 1e-30f) || !std::isfinite(temperature)) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: temperature must be finite and at least 1e-30");
     if (!(clip_eps >= 0.f) || !std::isfinite(clip_eps) || !std::isfinite(scale)) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: bad clip parameter or scale");
     const uintptr_t l0 = (uintptr_t)dev_logits, l1 = l0 + (((uintptr_t)(n_rows - 1) * row_stride) + V) * size;
     const uintptr_t g0 = (uintptr_t)dev_grad, g1 = g0 + (((uintptr_t)(n_rows - 1) * grad_stride) + V) * size;
@@ -102,10 +102,13 @@ extern "C" int spiral_policy_gradient(const void* dev_logits, int dtype, long lo
 // ---------------------------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------------------------
+struct Span { uintptr_t lo, hi; bool written; };
 struct spiral_adamw {
     int n = 0, steps = 0;
     long long chunks = 0;
     std::unique_ptr<AdamwRec[]> table;      // what the device holds a copy of
+    std::unique_ptr<Span[]> written;        // [n_written], in order and apart from each other: what a step writes
+    size_t n_written = 0;
     char* mem = nullptr;
 };
 
@@ -133,7 +136,6 @@ extern "C" int spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int 
     if (!dev_mem || !aligned(dev_mem, 256) || bytes < spiral_adamw_bytes(n_tensors))
         return fail(SPIRAL_ERR_INVALID_ARG, "adamw_create: memory is null, not 256-byte aligned or less than %zu bytes", spiral_adamw_bytes(n_tensors));
     std::unique_ptr<spiral_adamw> o(new (std::nothrow) spiral_adamw());
-    struct Span { uintptr_t lo, hi; bool written; };
     const size_t most = (size_t)n_tensors * 7 + 1;
     std::unique_ptr<Span[]> spans(new (std::nothrow) Span[most]);
     if (o) o->table.reset(new (std::nothrow) AdamwRec[n_tensors]);
@@ -178,6 +180,9 @@ extern "C" int spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int 
         end = std::max(end, spans[i].hi);
         if (spans[i].written) written_end = std::max(written_end, spans[i].hi);
     }
+    for (size_t i = 0; i < n_spans; ++i)
+        if (spans[i].written) spans[o->n_written++] = spans[i];
+    o->written = std::move(spans);
     o->n = n_tensors;
     o->steps = adamw_steps(elements);
     for (int t = 0; t < n_tensors; ++t) {
@@ -198,6 +203,10 @@ extern "C" int spiral_adamw_set_grads(spiral_adamw* o, const void* const* host_d
     for (int t = 0; t < o->n; ++t) {
         if (!host_dev_grads[t] || !aligned(host_dev_grads[t], dtype_size(o->table[t].grad_dtype)))
             return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: gradient %d is null or misaligned", t);
+        const uintptr_t lo = (uintptr_t)host_dev_grads[t], hi = lo + (uintptr_t)o->table[t].n * dtype_size(o->table[t].grad_dtype);
+        const Span* end = o->written.get() + o->n_written;
+        const Span* next = std::upper_bound((const Span*)o->written.get(), end, lo, [](uintptr_t v, const Span& s) { return v < s.hi; });      // the first that ends behind lo
+        if (next != end && next->lo < hi) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: gradient %d overlaps a buffer that is written", t);
     }
     for (int t = 0; t < o->n; ++t) o->table[t].grad = host_dev_grads[t];
     return adamw_upload(o, stream, "adamw_set_grads");
@@ -209,7 +218,7 @@ extern "C" int spiral_adamw_step(spiral_adamw* o, double lr, double beta1, doubl
     if (!(lr >= 0.0) || !std::isfinite(lr) || !(weight_decay >= 0.0) || !std::isfinite(weight_decay))
         return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: lr and weight_decay must be finite and >= 0");
     if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: betas must be in [0, 1)");
-    if (!(eps > 0.0) || !std::isfinite(eps)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: eps must be finite and > 0");
+    if (!(eps >= 1e-30) || !(eps <= 1e30)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: eps must be in [1e-30, 1e30]");
     if (!(max_norm >= 0.f) || !std::isfinite(max_norm) || !std::isfinite(grad_scale)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: bad max_norm or grad_scale");
     if (step < 1) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: steps are counted from 1");
     if (!aligned(dev_norm, 4)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: misaligned norm");

@@ -215,3 +215,37 @@ def test_captured_gradient_replays(sb, n):
         call(again)
         torch.cuda.synchronize()
         assert torch.equal(got, again) and torch.equal(lp, logp)
+
+
+def test_more_rows_than_a_launch_takes(sb):
+    """2^20 rows of three logits, and five more."""
+    import torch
+    n, V = (1 << 20) + 5, 3
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn((n, V), generator=g)
+    y = torch.randint(0, V, (n,), generator=g, dtype=torch.int32)
+    adv = torch.randn(n, generator=g)
+    mask = (torch.rand(n, generator=g) < 0.7).int()
+    logp, grad = torch.empty(n, device="cuda"), torch.full((n, V), 9.0, device="cuda")
+    ws = torch.empty(sb.spiral_policy_gradient_workspace_bytes(n, V), dtype=torch.uint8, device="cuda")
+    sb.spiral_policy_gradient(x.cuda(), y.cuda(), None, adv.cuda(), mask.cuda(), 1.0, 0.0, 1.0, logp, grad, ws)
+    ls = torch.log_softmax(x.double(), -1)
+    want = -(adv * mask).double()[:, None] * (torch.nn.functional.one_hot(y.long(), V) - ls.exp())
+    assert (logp.cpu().double() - ls.gather(1, y.long()[:, None])[:, 0] * mask).abs().max().item() <= EPS * (8 * 6 + 2 * 12 + 64)
+    assert (grad.cpu().double() - want).abs().max().item() <= 6 * 3 * EPS * (8 * 6 + 2 * 12 + 64)
+
+
+def test_no_advantage_no_gradient_whatever_the_ratio(sb):
+    import torch
+    n, V = 4, 50
+    rng = np.random.default_rng(11)
+    x = rng.normal(size=(n, V)).astype(np.float32)
+    y = np.arange(n, dtype=np.int32)
+    old = np.array([-1000.0, -np.inf, -3.0, 0.0], np.float32)             # ratios without end, and ordinary ones
+    whole, rows = matrix(n, V, "float32", 0, 0)
+    rows.copy_(torch.from_numpy(x))
+    _, grad = matrix(n, V, "float32", 0, 0)
+    run(sb, rows, y, old, np.zeros(n, np.float32), None, 1.0, 0.2, 1.0, grad)
+    assert (grad == 0).all()
+    run(sb, rows, y, old, np.ones(n, np.float32), None, 1.0, 0.2, 1.0, grad)
+    assert (grad[:2] == 0).all() and (grad[2:] != 0).any()                # clipped from above

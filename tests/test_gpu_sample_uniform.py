@@ -177,3 +177,46 @@ def test_replays_of_a_captured_draw_read_the_numbers_of_then(sb):
         got = tok.cpu().numpy().copy(), lp.cpu().numpy().copy()
         check(rows, un, got, T, k, p)
         assert np.array_equal(run(sb, rows, un, T, k, p)[0], got[0])
+
+
+@pytest.mark.parametrize("V", [524288, 524289, 600007])
+def test_rows_of_many_pieces_and_of_too_many(sb, V):
+    """256 pieces are the most; longer rows are a workgroup's."""
+    rng = np.random.default_rng(12)
+    x = (rng.normal(size=(3, V)) * np.array([[0.7], [1.5], [3.0]])).astype(np.float32)
+    rows = place(x, "float32", 0, 0)
+    for s in (dict(), dict(k=100, p=0.9), dict(p=0.95, T=0.7), dict(k=V // 4, p=0.8), dict(mp=0.02), dict(T=0.0)):
+        u = np.array([0.999, 0.2, 0.5], np.float32)
+        # 2 of 3: the oracle by itself says which are too near (one, at V = 524,288 under the third setting: 9.07e-10 from the cut)
+        check(rows, u, run(sb, rows, u, **s), **s, least=0.6)
+
+
+@pytest.mark.parametrize("V", [151936, 40000])
+def test_cuts_by_count_and_mass_that_lie_apart(sb, V):
+    """Counts far below, at and above the mass's border, in rows from flat to sharp, and ones where a few tokens have nearly everything."""
+    rng = np.random.default_rng(13)
+    B = 40
+    x = (rng.normal(size=(B, V)) * rng.uniform(0.3, 3, size=(B, 1))).astype(np.float32)
+    for i in range(0, B, 4):
+        x[i, rng.integers(0, V, 2)] += rng.uniform(6, 14)
+    k = np.exp(rng.uniform(np.log(2), np.log(V - 1), B)).astype(np.int32)
+    p = rng.choice([0.05, 0.5, 0.9, 0.999], size=B).astype(np.float32)
+    mp = rng.choice([0.0, 0.0, 1e-4, 0.1], size=B).astype(np.float32)
+    T = rng.choice([0.5, 1.0, 2.0], size=B).astype(np.float32)
+    u = rng.random(B).astype(np.float32)
+    for dtype in ("float32", "bfloat16"):
+        rows = place(x, dtype, 0, 0)
+        check(rows, u, run(sb, rows, u, T, k, p, mp), T, k, p, mp)
+
+
+def test_a_full_batch_and_the_calls_that_read_its_tokens(sb):
+    """1,024 rows, the most there are; the tokens are indices that an embedding may be read by."""
+    rng = np.random.default_rng(14)
+    B, V = 1024, 2000
+    x = rng.normal(size=(B, V)).astype(np.float32)
+    x[5] = -np.inf
+    u = rng.random(B).astype(np.float32)
+    rows = place(x, "float16", 0, 0)
+    got = run(sb, rows, u, p=0.9)
+    check(rows, u, got, p=0.9)
+    assert (got[0] >= 0).all() and (got[0] < V).all()

@@ -157,3 +157,8 @@ def test_rows_of_the_gradient_are_cut_where_there_are_few_long_ones(lib):
             k = slices(n, V, FP32)
             assert 2 <= k <= max(2, 1024 // n) and V // 4 // k >= 1024
             assert sb.spiral_policy_gradient_workspace_bytes(n, V) >= n * k * 8 + n * 4
+
+
+@pytest.mark.parametrize("T", [0.0, 1e-31, 1e-39])
+def test_gradient_refuses_temperatures_whose_inverse_is_infinite(lib, T):
+    refused(grad(lib, T=T), sb.SPIRAL_ERR_INVALID_ARG, "temperature")
