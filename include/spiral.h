@@ -6,7 +6,9 @@
  * (Sec. 3 "Self-play"; Alg. 1, generation step) with the actor's sampling
  * settings (hyper-parameter table, App. D: temperature 1.0, top-p 1.0, top-k -1,
  * i.e. an untruncated categorical), plus the role-conditioned advantage
- * estimation baseline (Sec. 3, RAE equation; Alg. 1, policy-optimisation loop).
+ * estimation baseline (Sec. 3, RAE equation; Alg. 1, policy-optimisation loop), and
+ * what closes an update of the policy: a draw with its log-probability, the gradient
+ * of the objective in the logits, AdamW.
  *
  * General rules
  *  - Every function returns SPIRAL_OK (0) or a negative SPIRAL_ERR_* code; it
@@ -18,7 +20,7 @@
  *    frees device memory and never synchronises the stream; all device work is
  *    enqueued on the stream that is passed in (`stream` is a hipStream_t, NULL =
  *    the default stream).  Host arrays are consumed before the call returns.
- *  - Opaque host objects (model, pool, RAE state) are created and freed by the
+ *  - Opaque host objects (model, pool, optimiser, RAE state) are created and freed by the
  *    library.  Calls on the same object must not overlap.
  *  - A failed call leaves sequence lengths and page tables unchanged: the sequences' lengths, their page lists
  *    and the free list are host-side state that is advanced only after every launch of the call was accepted

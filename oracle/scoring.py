@@ -15,7 +15,7 @@ epochs, i.e. the clipped importance-ratio surrogate.  Written out:
 
 A_t is the advantage of the player who produced token t (the caller expands the per-trajectory,
 per-role RAE advantages to tokens); mask_t selects generated tokens (prompt and observation tokens
-carry no gradient).  Everything is float64.  Backward pass and optimiser are outside this build.
+carry no gradient).  Everything is float64.  The objective's gradient in the logits and the optimiser's step are in update.py.
 """
 from __future__ import annotations
 

@@ -3,8 +3,8 @@
 // Bound by memory: 28 bytes an element for bf16 weights with fp32 masters and states, 12 + 4 with 8-bit states, of which the norm's sweep reads the
 // gradient's 2 once more.  A workgroup walks chunks of 4,096 elements of whatever tensor they fall in; all of a chunk's loads (4 runs of 4
 // neighbouring elements a thread) are in flight before the first is used, four workgroups a compute unit (128 registers, no spill; five
-// spill and gain 1% with 32-bit states, lose as much with 8-bit ones; chunks of 2,048 with eight: 9% and 5% slower).  Over 303 M elements, bf16 with masters: 1,680 us with 32-bit
-// states (103 + 1,570: 5.4 TB/s, where a copy of 4 GiB moves 4.8), 1,031 us with 8-bit states.  What brought them there from 10,279 and 5,624 us: wide loads of any alignment, all
+// spill and gain 1% with 32-bit states, lose as much with 8-bit ones; chunks of 2,048 with eight: 9% and 5% slower).  Over 303 M elements, bf16 with masters: 1,673 us with 32-bit
+// states (102 in the norm and 5.4 TB/s in the step, where a copy of 4 GiB moves 4.8), 1,012 us with 8-bit states.  What brought them there from 10,279 and 5,624 us: wide loads of any alignment, all
 // ahead (2,005, 2,026); as many workgroups as fit (1,779, 1,627); streaming loads and stores that nothing else evicts the gradients for (1,685, 1,502); records by scalar loads instead of
 // two dependent vector loads a chunk (8 bits: 1,108); chunks of four runs (1,670, 1,058).
 #include "spiral_internal.h"
