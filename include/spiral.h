@@ -327,9 +327,9 @@ int spiral_sample_truncated_ws(const float* dev_logits, int B, int V, float temp
  * off, off.  dev_uniform: fp32 [B], read when the kernels run: a captured call that is replayed draws from what stands there then.
  * dev_out_tokens: int32 [B]; dev_out_logp: fp32 [B] or NULL.  dev_workspace: 256-byte aligned,
  * spiral_sample_uniform_workspace_bytes(B, V) bytes (0 for an invalid B or V), contents undefined before and after; calls that share it
- * must be ordered on one stream.
+ * must be ordered on one stream.  Outputs and workspace may overlap neither each other nor an input (the logits' range ends with the last row's V).
  * Errors: INVALID_ARG (null or misaligned pointer, B outside [1, SPIRAL_MAX_BATCH], V < 1, unknown type, row_stride < V, temperature
- * negative or not finite, top_p outside (0, 1], min_p outside [0, 1], workspace too small), HIP. */
+ * negative or not finite, top_p outside (0, 1], min_p outside [0, 1], workspace too small, overlapping buffers), HIP. */
 size_t spiral_sample_uniform_workspace_bytes(int B, int V);
 int spiral_sample_uniform(const void* dev_logits, int logits_dtype, long long row_stride, int B, int V,
                           const float* host_temperature, const int32_t* host_top_k, const float* host_top_p,

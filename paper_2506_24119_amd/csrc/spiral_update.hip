@@ -26,6 +26,17 @@ static int dtype_size(int dtype) {          // of logits, parameters and gradien
 }
 static bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
+// Of a call's buffers none that is written may be another one too: workgroups would read what others have already written.
+struct Span { uintptr_t lo, hi; bool written; };
+static Span span_of(const void* p, size_t bytes, bool written) { return {(uintptr_t)p, (uintptr_t)p + (p ? bytes : 0), written}; }
+static uintptr_t matrix_bytes(long long rows, long long stride, int V, int size) { return ((uintptr_t)(rows - 1) * stride + V) * size; }
+static bool any_overlap(const Span* s, int n) {
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; j < i; ++j)
+            if ((s[i].written || s[j].written) && s[i].lo < s[j].hi && s[j].lo < s[i].hi) return true;
+    return false;
+}
+
 // ---------------------------------------------------------------------------------------------
 // draw
 // ---------------------------------------------------------------------------------------------
@@ -56,6 +67,10 @@ extern "C" int spiral_sample_uniform(const void* dev_logits, int logits_dtype, l
         if (host_min_p && !(host_min_p[i] >= 0.f && host_min_p[i] <= 1.f))
             return fail(SPIRAL_ERR_INVALID_ARG, "sample_uniform: min_p of row %d must be in [0, 1] (0 disables)", i);
     }
+    const size_t per_row = (size_t)B * 4;
+    const Span spans[] = {span_of(dev_logits, matrix_bytes(B, row_stride, V, size), false), span_of(dev_uniform, per_row, false),
+                          span_of(dev_out_tokens, per_row, true), span_of(dev_out_logp, per_row, true), span_of(dev_workspace, need, true)};
+    if (any_overlap(spans, 5)) return fail(SPIRAL_ERR_INVALID_ARG, "sample_uniform: a buffer that is written overlaps another");
     DrawArgs a = {};
     a.logits = dev_logits; a.row_stride = row_stride; a.B = B; a.V = V;
     a.uniform = dev_uniform; a.tokens = dev_out_tokens; a.logp = dev_out_logp;
@@ -102,7 +117,6 @@ extern "C" int spiral_policy_gradient(const void* dev_logits, int dtype, long lo
 // ---------------------------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------------------------
-struct Span { uintptr_t lo, hi; bool written; };
 struct spiral_adamw {
     int n = 0, steps = 0;
     long long chunks = 0;

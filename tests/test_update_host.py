@@ -162,3 +162,15 @@ def test_rows_of_the_gradient_are_cut_where_there_are_few_long_ones(lib):
 @pytest.mark.parametrize("T", [0.0, 1e-31, 1e-39])
 def test_gradient_refuses_temperatures_whose_inverse_is_infinite(lib, T):
     refused(grad(lib, T=T), sb.SPIRAL_ERR_INVALID_ARG, "temperature")
+
+
+Q = 1 << 31                      # far from P
+
+
+@pytest.mark.parametrize("change", [
+    dict(logp=P), dict(logp=P + 12), dict(u=P + (1 << 8) - 12, logp=P + (1 << 8)), dict(out=Q, logp=Q + 12), dict(out=Q + 1596, logp=None), dict(logits=P, u=Q, out=P + 1596, logp=None),
+    dict(ws=P), dict(ws=Q), dict(out=2 * Q + 252), dict(logp=2 * Q)])
+def test_draw_refuses_outputs_that_are_read(lib, change):
+    a = dict(logits=Q, u=P, out=P + 4096, logp=P + 8192, ws=2 * Q)
+    a.update(change)
+    refused(draw(lib, **a), sb.SPIRAL_ERR_INVALID_ARG, "overlaps")
