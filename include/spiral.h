@@ -349,6 +349,7 @@ int spiral_sample_uniform(const void* dev_logits, int logits_dtype, long long ro
  * or more; the gradient is rounded once, to the logits' type.  Results repeat bit for bit.
  * dev_logits [n_rows, V], rows row_stride apart, dev_grad [n_rows, V], rows grad_stride apart, both of `dtype` (SPIRAL_DTYPE_FP32, _BF16,
  * _FP16) and aligned to an element; the gradient may be written in place (same pointer, same stride) but not overlap the logits in another way.
+ * Nothing else that is written (dev_grad, dev_logp, the workspace) may overlap another buffer; a matrix counts from its first row's start to its last one's end.
  * dev_targets int32, dev_logp_old fp32 or NULL, dev_advantage fp32, dev_mask int32 or NULL, dev_logp fp32: [n_rows] each.
  * dev_workspace: 256-byte aligned, spiral_policy_gradient_workspace_bytes(n_rows, V) bytes (0 for invalid sizes), contents undefined before
  * and after; calls that share it must be ordered on one stream.

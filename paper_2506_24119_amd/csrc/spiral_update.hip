@@ -99,13 +99,17 @@ extern "C" int spiral_policy_gradient(const void* dev_logits, int dtype, long lo
         return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: misaligned buffer");
     if (!(temperature >= 1e-30f) || !std::isfinite(temperature)) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: temperature must be finite and at least 1e-30");
     if (!(clip_eps >= 0.f) || !std::isfinite(clip_eps) || !std::isfinite(scale)) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: bad clip parameter or scale");
-    const uintptr_t l0 = (uintptr_t)dev_logits, l1 = l0 + (((uintptr_t)(n_rows - 1) * row_stride) + V) * size;
-    const uintptr_t g0 = (uintptr_t)dev_grad, g1 = g0 + (((uintptr_t)(n_rows - 1) * grad_stride) + V) * size;
-    if (l0 < g1 && g0 < l1 && !(l0 == g0 && row_stride == grad_stride))
-        return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: the gradient overlaps the logits without being in place");
+    const size_t in_bytes = matrix_bytes(n_rows, row_stride, V, size), out_bytes = matrix_bytes(n_rows, grad_stride, V, size), per_row = (size_t)n_rows * 4;
+    const bool in_place = dev_grad == dev_logits && row_stride == grad_stride;
+    const Span matrices[] = {span_of(dev_logits, in_bytes, false), span_of(dev_grad, out_bytes, true)};
+    if (!in_place && any_overlap(matrices, 2)) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: the gradient overlaps the logits without being in place");
     const size_t need = policy_grad_workspace_bytes(n_rows, V);
     if (!dev_workspace || !aligned(dev_workspace, 256)) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: workspace is null or not 256-byte aligned");
     if (workspace_bytes < need) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    const Span spans[] = {span_of(in_place ? nullptr : dev_logits, in_bytes, false), span_of(dev_grad, out_bytes, true), span_of(dev_targets, per_row, false),
+                          span_of(dev_logp_old, per_row, false), span_of(dev_advantage, per_row, false), span_of(dev_mask, per_row, false),
+                          span_of(dev_logp, per_row, true), span_of(dev_workspace, need, true)};
+    if (any_overlap(spans, 8)) return fail(SPIRAL_ERR_INVALID_ARG, "policy_gradient: a buffer that is written overlaps another");
     GradArgs a = {};
     a.logits = dev_logits; a.row_stride = row_stride; a.grad = dev_grad; a.grad_stride = grad_stride;
     a.n_rows = n_rows; a.V = V;

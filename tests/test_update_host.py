@@ -174,3 +174,12 @@ def test_draw_refuses_outputs_that_are_read(lib, change):
     a = dict(logits=Q, u=P, out=P + 4096, logp=P + 8192, ws=2 * Q)
     a.update(change)
     refused(draw(lib, **a), sb.SPIRAL_ERR_INVALID_ARG, "overlaps")
+
+
+@pytest.mark.parametrize("change", [
+    dict(logp=P), dict(t=Q, logp=Q), dict(adv=Q, logp=Q + 28), dict(mask=Q, logp=Q + 16), dict(logp=2 * Q + 1500), dict(old=2 * Q), dict(t=2 * Q + 1596), dict(logits=2 * Q, logp=2 * Q + 4),
+    dict(ws=P), dict(ws=Q, logp=Q), dict(ws=2 * Q), dict(ws=2 * Q + 1536), dict(logits=3 * Q, ws=3 * Q + 256), dict(logp=3 * Q + 100, logits=3 * Q)])
+def test_gradient_refuses_outputs_that_are_read(lib, change):
+    a = dict(logits=3 * Q + 4096, t=P, old=P, adv=P, mask=P, logp=P + 4096, grad=2 * Q, ws=4 * Q)
+    a.update(change)
+    refused(grad(lib, **a), sb.SPIRAL_ERR_INVALID_ARG, "overlaps")
