@@ -215,16 +215,22 @@ extern "C" int spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int 
     return SPIRAL_OK;
 }
 
+// whether a step writes any of these bytes
+static bool overwritten(const spiral_adamw* o, const void* p, uintptr_t bytes) {
+    const uintptr_t lo = (uintptr_t)p;
+    const Span* end = o->written.get() + o->n_written;
+    const Span* next = std::upper_bound((const Span*)o->written.get(), end, lo, [](uintptr_t v, const Span& s) { return v < s.hi; });      // the first that ends behind lo
+    return next != end && next->lo < lo + bytes;
+}
+
 extern "C" int spiral_adamw_set_grads(spiral_adamw* o, const void* const* host_dev_grads, void* stream) {
     if (!o) return fail(SPIRAL_ERR_NOT_LOADED, "adamw_set_grads: null object");
     if (!host_dev_grads) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: null array");
     for (int t = 0; t < o->n; ++t) {
         if (!host_dev_grads[t] || !aligned(host_dev_grads[t], dtype_size(o->table[t].grad_dtype)))
             return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: gradient %d is null or misaligned", t);
-        const uintptr_t lo = (uintptr_t)host_dev_grads[t], hi = lo + (uintptr_t)o->table[t].n * dtype_size(o->table[t].grad_dtype);
-        const Span* end = o->written.get() + o->n_written;
-        const Span* next = std::upper_bound((const Span*)o->written.get(), end, lo, [](uintptr_t v, const Span& s) { return v < s.hi; });      // the first that ends behind lo
-        if (next != end && next->lo < hi) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: gradient %d overlaps a buffer that is written", t);
+        if (overwritten(o, host_dev_grads[t], (uintptr_t)o->table[t].n * dtype_size(o->table[t].grad_dtype)))
+            return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: gradient %d overlaps a buffer that is written", t);
     }
     for (int t = 0; t < o->n; ++t) o->table[t].grad = host_dev_grads[t];
     return adamw_upload(o, stream, "adamw_set_grads");
@@ -240,6 +246,14 @@ extern "C" int spiral_adamw_step(spiral_adamw* o, double lr, double beta1, doubl
     if (!(max_norm >= 0.f) || !std::isfinite(max_norm) || !std::isfinite(grad_scale)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: bad max_norm or grad_scale");
     if (step < 1) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: steps are counted from 1");
     if (!aligned(dev_norm, 4)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: misaligned norm");
+    if (dev_norm) {                                  // also none of the gradients, which other workgroups still read when it is written
+        bool meets = overwritten(o, dev_norm, 4);
+        for (int t = 0; t < o->n && !meets; ++t) {
+            const uintptr_t lo = (uintptr_t)o->table[t].grad, hi = lo + (uintptr_t)o->table[t].n * dtype_size(o->table[t].grad_dtype);
+            meets = (uintptr_t)dev_norm < hi && lo < (uintptr_t)dev_norm + 4;
+        }
+        if (meets) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: the norm overlaps a buffer of the table");
+    }
     AdamwArgs a = {};
     a.table = (const AdamwRec*)o->mem;
     a.n_tensors = o->n;

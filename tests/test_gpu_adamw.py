@@ -303,3 +303,28 @@ def test_refusals_of_a_made_optimiser(sb):
     assert all(torch.equal(g.whole.view(torch.uint8), b) for t, bs in zip(tensors, before) for g, b in zip(t.guards(), bs))
     check_step(sb, opt, tensors, 1, max_norm=1.0)
     sb.spiral_adamw_free(opt)
+
+
+def test_a_norm_inside_the_tables_buffers_is_refused(sb):
+    import torch
+    rng = np.random.default_rng(11)
+    tensors = [Tensor(sb, rng, n, bits=b) for n, b in ((1000, 32), (600, 8))]
+    opt, mem = build(sb, tensors)
+    before = [[g.whole.clone().view(torch.uint8) for g in t.guards()] for t in tensors]
+    t0, t1 = tensors
+    for buf in (t0.param.t, t0.master.t, t0.m.t, t0.v.t, t0.grad.t, t1.grad.t, mem):
+        words = buf.view(torch.uint8)
+        at = -words.data_ptr() % 4
+        for o in (at, at + (len(words) - at - 4) // 4 * 4):
+            with pytest.raises(sb.SpiralError) as e:
+                sb.spiral_adamw_step(opt, 1e-3, 0.9, 0.95, 1e-8, 0.0, 1, dev_norm=words[o:o + 4].view(torch.float32))
+            assert e.value.code == sb.SPIRAL_ERR_INVALID_ARG and "overlaps" in str(e.value)
+    grads = [t0.grad.t.clone(), t1.grad.t]
+    sb.spiral_adamw_set_grads(opt, grads)                                   # the table's gradients are those that it has now
+    with pytest.raises(sb.SpiralError):
+        sb.spiral_adamw_step(opt, 1e-3, 0.9, 0.95, 1e-8, 0.0, 1, dev_norm=grads[0].view(torch.float32)[7:8])
+    sb.spiral_adamw_set_grads(opt, [t0.grad.t, t1.grad.t])
+    torch.cuda.synchronize()
+    assert all(torch.equal(g.whole.view(torch.uint8), b) for t, bs in zip(tensors, before) for g, b in zip(t.guards(), bs))
+    check_step(sb, opt, tensors, 1, max_norm=1.0)
+    sb.spiral_adamw_free(opt)
