@@ -99,3 +99,84 @@ def test_an_update_of_the_policy(bits):
     assert moved > 0.05                                                    # and not those of the old ones
     sb.spiral_adamw_free(opt)
     s.close()
+
+
+def test_updates_on_two_streams_at_once():
+    """Each stream has its buffers and workspaces; together, captured and replayed in turn they give what each gives alone, bit for bit."""
+    import torch
+    from paper_2506_24119_amd import binding as sb
+    dev = torch.device("cuda")
+    gen = torch.Generator(device="cuda").manual_seed(81)
+
+    class Work:
+        def __init__(self, B, V, dtype, bits):
+            n = 70_000 + B
+            self.x = (torch.randn((B, V), device=dev, generator=gen) * 3).to(dtype)
+            self.u, self.adv = torch.rand(B, device=dev, generator=gen), torch.randn(B, device=dev, generator=gen)
+            self.tok, self.old, self.lp = torch.zeros(B, dtype=torch.int32, device=dev), torch.zeros(B, device=dev), torch.zeros(B, device=dev)
+            self.grad = torch.zeros_like(self.x)
+            self.ws = torch.zeros(sb.spiral_sample_uniform_workspace_bytes(B, V), dtype=torch.uint8, device=dev)
+            self.gws = torch.zeros(sb.spiral_policy_gradient_workspace_bytes(B, V), dtype=torch.uint8, device=dev)
+            state = torch.float32 if bits == 32 else torch.float8_e4m3fn
+            self.p, self.m, self.v = torch.randn(n, device=dev, generator=gen), torch.zeros(n, device=dev).to(state), torch.zeros(n, device=dev).to(state)
+            sc = {} if bits == 32 else {k: torch.zeros(-(-n // sb.SPIRAL_ADAMW_BLOCK), device=dev) for k in ("m_scale", "v_scale")}
+            self.g = torch.randn(n, device=dev, generator=gen).bfloat16()
+            recs = [sb.spiral_adamw_tensor(self.p, self.g, self.m, self.v, **sc)]
+            self.keep = sc
+            self.mem = torch.zeros(sb.spiral_adamw_bytes(recs), dtype=torch.uint8, device=dev)
+            self.opt = sb.spiral_adamw_create(recs, self.mem)
+            self.norm = torch.zeros(1, device=dev)
+            self.states = [self.p, self.m, self.v, *sc.values()]
+            self.first = [t.clone() for t in self.states]
+
+        def start(self):
+            for t, f in zip(self.states, self.first):
+                t.view(torch.uint8).copy_(f.view(torch.uint8))
+            for t in (self.tok, self.old, self.lp, self.grad, self.norm):
+                t.zero_()
+
+        def run(self):
+            sb.spiral_sample_uniform(self.x, 0.8, 300, 0.9, 0.001, self.u, self.ws, self.tok, self.old)
+            sb.spiral_policy_gradient(self.x, self.tok, self.old, self.adv, None, 0.8, 0.2, 0.5, self.lp, self.grad, self.gws)
+            sb.spiral_adamw_step(self.opt, 1e-2, 0.9, 0.95, 1e-8, 0.01, 1, max_norm=1.0, dev_norm=self.norm)
+
+        def results(self):
+            return [t.clone().view(torch.uint8) for t in (self.tok, self.old, self.lp, self.grad, self.norm, *self.states)]
+
+    works = [Work(5, 151936, torch.bfloat16, 32), Work(33, 50257, torch.float32, 8)]
+    alone = []
+    for w in works:
+        for _ in range(3):
+            w.run()
+        torch.cuda.synchronize()
+        alone.append(w.results())
+        assert (w.old < 0).any() and w.norm.item() > 0
+    same = lambda: all(torch.equal(a, b) for w, r in zip(works, alone) for a, b in zip(w.results(), r))  # noqa: E731
+    streams = [torch.cuda.Stream() for _ in works]
+    for w in works:
+        w.start()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for w, st in zip(works, streams):
+            with torch.cuda.stream(st):
+                w.run()
+    torch.cuda.synchronize()
+    assert same()
+    graphs = []
+    for w, st in zip(works, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            w.run()
+        graphs.append(g)
+    for _ in range(2):
+        for w in works:
+            w.start()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for g, st in zip(graphs, streams):
+                with torch.cuda.stream(st):
+                    g.replay()
+        torch.cuda.synchronize()
+        assert same()
+    for w in works:
+        sb.spiral_adamw_free(w.opt)
