@@ -338,7 +338,7 @@ struct DrawPlan {
     int take;                         // kTakeAll: all are kept but for min-p's; Some: as above; Listed: all from `list` on are candidates; Slow: a workgroup does the row
     float keep, list, k_keep, k_list;
     uint32_t k_above;                 // entries from k_keep on
-    int pad;
+    int k_last;                       // the count's border lies in the last bin or below the candidates
 };
 // What a piece has: kept weights relative to exp(ref), and of a row cut by mass all weights and those in bins below lo.
 struct PieceSums { double kept, all, above; float ref; int pad; };
@@ -604,13 +604,16 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
     const int bin = lane < 16 ? lo - 1 : lane < 32 ? hi : lane < 48 ? cut - 1 : cut;
     float t = least_logit(bin < 0 ? NAN : top - (float)bin, scale, lane);
     if (bin < 0) t = NAN;                                       // above every logit
-    if (bin == kBins - 1) t = set.top_k ? -INFINITY : -3.402823466e38f;      // all the rest; what weighs nothing is no candidate by mass
+    // The last bin's candidates end where weights are 0 in 64 bits too, so that a mask's -inf or lowest number is none: kept or not, such an entry is never drawn.
+    // (Where 30 of 151,936 are allowed and 50 are asked for, 64 rows: 48 us, and 1,008 with all of them as candidates, which the list does not hold.)
+    if (bin == kBins - 1) t = fmaxf(m - 1000.f * set.temperature, -3.402823466e38f);
     plan.keep = __shfl(t, 0, 64);
     plan.list = __shfl(t, 16, 64);
     if (set.top_k) {
         plan.k_keep = __shfl(t, 32, 64);
         plan.k_list = __shfl(t, 48, 64);
         plan.k_above = s_above;
+        plan.k_last = cut == kBins - 1;
     }
     plan.take = lo >= kBins ? kTakeSlow : listed ? kTakeListed : kTakeSome;
     if (lane == 0) w.plan[r] = plan;
@@ -736,7 +739,7 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
     __shared__ Select sel;
     __shared__ double s_all, s_above;
     __shared__ uint64_t s_z, s_zk;
-    __shared__ uint32_t s_differ;
+    __shared__ uint32_t s_differ, s_below;
     __shared__ bool s_found;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     copy_table(s_table);
@@ -788,7 +791,7 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
                 }
                 all = wave_total(all);
                 above = wave_total(above);
-                if (lane == 0) { s_all = all; s_above = above; s_z = s_zk = 0; s_differ = 0; }
+                if (lane == 0) { s_all = all; s_above = above; s_z = s_zk = 0; s_differ = s_below = 0; }
             }
             for (int i = tid; i < kMaxPieces; i += THREADS) s_cand[i] = 0;
             __syncthreads();
@@ -836,8 +839,19 @@ __global__ __launch_bounds__(CUTS ? 512 : 256) void draw_pick_kernel(DrawArgs a,
             };
             // only those below k_keep are counted: the others are in number known
             const uint32_t sure_key = plan.take == kTakeListed || plan.k_keep != plan.k_keep ? 0xFFFFFFFFu : order_key(plan.k_keep);
-            if (set.top_k) {
-                if (tid == 0) sel.remaining = (uint64_t)set.top_k - (plan.take == kTakeListed ? 0u : plan.k_above);
+            // A count that reaches past all candidates of the last bin cuts nothing that weighs anything.
+            const uint32_t to_count = set.top_k - (plan.take == kTakeListed ? 0u : plan.k_above);
+            bool counts = set.top_k != 0;
+            if (counts && plan.k_last) {
+                uint32_t below = 0;
+                for (uint32_t i = tid; i < n; i += THREADS) below += list[i].x < sure_key ? 1u : 0u;
+                below = wave_total(below);
+                if (lane == 0 && below) atomicAdd(&s_below, below);
+                __syncthreads();
+                counts = to_count <= s_below;
+            }
+            if (counts) {
+                if (tid == 0) sel.remaining = to_count;
                 descend([&](uint32_t key, uint32_t) { return key < sure_key ? (uint64_t)1 : (uint64_t)0; });
             }
             if (set.top_p < 1.0) {

@@ -220,3 +220,21 @@ def test_a_full_batch_and_the_calls_that_read_its_tokens(sb):
     got = run(sb, rows, u, p=0.9)
     check(rows, u, got, p=0.9)
     assert (got[0] >= 0).all() and (got[0] < V).all()
+
+
+@pytest.mark.parametrize("V,dtype", [(16384, "float32"), (20001, "bfloat16"), (151936, "float16")])
+@pytest.mark.parametrize("fill", [0xA5, 0xFF, 0x00])
+def test_counts_that_reach_the_undefined_logits(sb, V, dtype, fill):
+    """Undefined logits count as -inf also where a cut by count has more to keep than there are others; what the workspace held before is nothing to it."""
+    rng = np.random.default_rng(V)
+    B, n = 8, [1, 3, 10, 49, 10, 10, 500, 2]
+    x = np.full((B, V), np.nan, np.float32)
+    x[4, rng.random(V) < 0.2] = -np.inf
+    x[5, : V // 2] = -np.inf
+    for i in range(B):
+        x[i, rng.choice(V, n[i], replace=False)] = rng.normal(size=n[i]) * 2
+    x[7, rng.choice(V, 40, replace=False)] = -3e4                         # far below, weights of nothing
+    u = rng.random(B).astype(np.float32)
+    rows = place(x, dtype, 0, 0)
+    for s in (dict(k=50), dict(k=50, p=0.9), dict(k=V - 1, p=0.7, T=0.8), dict(k=50, mp=0.1), dict(k=30, T=0.5)):
+        check(rows, u, run(sb, rows, u, fill=fill, **s), **s, least=1.0)
