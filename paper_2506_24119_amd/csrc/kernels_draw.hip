@@ -6,6 +6,8 @@
 // that counts entries in bins (draw_count_kernel, 18.3 us), the bins between which the cuts fall (draw_plan_kernel, 8.9), a sweep that sums what is kept for sure and lists the
 // entries of those bins (draw_cut_kernel, 26.5), and the exact border among them (draw_pick_kernel, 15.6).  Counts are 32-bit LDS additions; 64-bit masses in the
 // histogram would take 46 us.  Lines, both sides measured: 16,000 and 17,000 logits with top-p, one row 29 and 24 us, 16 rows 35 and 29; uncut 14 to 17 and 13.
+#include <type_traits>
+
 #include "spiral_internal.h"
 
 namespace spiral {
@@ -202,13 +204,137 @@ __device__ __forceinline__ void nothing_to_draw(const DrawArgs& a, int r) {
     if (a.logp) a.logp[r] = -INFINITY;
 }
 
-// A row by a workgroup, in as many sweeps of it as the cuts need: one for the maximum, four digits of the k-th largest key, four of the
-// key at which the mass reaches p, one for the sum of what is kept and a part of one for the token.
+constexpr int kBins = 1024, kPerNat = 32;          // bins over the 32 below the maximum of (l - m) / T, and the last for what lies further down
+// monotone in l, and their floors whole numbers that floats hold exactly
+__device__ __forceinline__ float bin_scale(float temperature) { return (float)kPerNat / temperature; }
+__device__ __forceinline__ float bin_place(float l, float scale) { return fminf(fmaxf(l * scale, -4194304.f), 4194304.f); }
+__device__ __forceinline__ float bin_floor(float l, float scale) { return floorf(bin_place(l, scale)); }
+__device__ __forceinline__ int bin_of(float l, float top, float scale) { return min((int)(top - bin_floor(l, scale)), kBins - 1); }
+// Where the last bin's candidates end: below, weights are 0 in 64 bits too, so that a mask's -inf or lowest number is none.  Kept or not, such an entry is never drawn.
+// (Where 30 of 151,936 are allowed and 50 are asked for, 64 rows: 48 us, and 1,008 with all of them as candidates, which the list does not hold.)
+__device__ __forceinline__ float least_candidate(float m, float temperature) { return fmaxf(m - 1000.f * temperature, -3.402823466e38f); }
+
+// The cuts of a row that lies in LDS, in two or three sweeps: counts and masses of its bins, then the entries of the bin in which a border falls, each by a thread
+// that adds up those above it (up to a thread each; more, e.g. equal logits, are left to the descent below).  The masses are the integers that the descent
+// adds, so the border is the same.  128 rows of 16,000 fp32 logits, top-k 300 and top-p 0.95: 43 us by eight sweeps of the descent, 29 so; 2,039 of them 15.2 and 12.8 (one
+// cut of 600: 7.9 and 8.2).
+struct RowBins {
+    uint64_t mass[kBins];             // of bins, then of listed entries
+    uint32_t count[kBins];            // of bins, then keys
+    uint64_t wave_mass[kBins / 64], above_mass, kept_mass;
+    uint32_t wave_count[kBins / 64], above, n, border;
+    int bin;
+};
+struct NoBins { uint64_t mass[256]; };
+struct Cuts { uint32_t floor_key; bool by_count, by_mass; };      // and which of them are done
+__device__ __forceinline__ Cuts cut_by_bins(RowBins& s, const float* cache, uint32_t V, float m, const Weight& weight, const RowSettings& set, double unit) {
+    constexpr int THREADS = kBins;    // a bin a thread
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool by_mass = set.top_p < 1.0;
+    auto amount = [&](float l) { return (uint64_t)rint(weight(l) * unit); };
+    Cuts cuts = {0u, !set.top_k, !by_mass};
+    s.count[tid] = 0;
+    s.mass[tid] = 0;
+    if (tid == 0) s.n = s.border = 0;
+    __syncthreads();
+    const float scale = bin_scale(set.temperature), top = bin_floor(m, scale);
+    for (uint32_t v = tid; v < V; v += THREADS) {
+        const float l = cache[v];
+        const int b = bin_of(l, top, scale);
+        if (set.top_k) atomicAdd(&s.count[b], 1u);
+        if (by_mass) {
+            const uint64_t x = amount(l);
+            if (x) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)x);
+        }
+    }
+    __syncthreads();
+    const uint32_t n = s.count[tid];
+    const uint64_t q = s.mass[tid];
+    uint32_t n_upto = wave_scan(n);
+    uint64_t q_upto = wave_scan(q), all = 0;
+    if (lane == 63) { s.wave_count[wave] = n_upto; s.wave_mass[wave] = q_upto; }
+    __syncthreads();
+    for (int i = 0; i < THREADS / 64; ++i) {
+        if (i < wave) { n_upto += s.wave_count[i]; q_upto += s.wave_mass[i]; }
+        all += s.wave_mass[i];
+    }
+    uint64_t target = 0;
+    auto find_mass = [&] {                           // exactly one bin
+        if (q_upto - q < target && target <= q_upto) { s.bin = tid; s.above_mass = q_upto - q; }
+    };
+    if (set.top_k) {
+        if (n_upto - n < (uint32_t)set.top_k && (uint32_t)set.top_k <= n_upto) { s.bin = tid; s.above = n_upto - n; s.above_mass = q_upto - q; }
+    } else {
+        target = share_of(set.top_p, all);
+        find_mass();
+    }
+    uint32_t key = 0, upto_n = 0, over_n = 0;        // of this thread's entry of the list: how much from it on, and above it
+    uint64_t upto_q = 0, over_q = 0;
+    bool mine = false;
+    auto listed = [&] {                              // the bin's entries; false: more than threads
+        __syncthreads();
+        const int bin = s.bin;
+        const float least = bin == kBins - 1 ? least_candidate(m, set.temperature) : -INFINITY;
+        for (uint32_t v = tid; v < V; v += THREADS) {
+            const float l = cache[v];
+            if (l < least || bin_of(l, top, scale) != bin) continue;
+            const uint32_t at = atomicAdd(&s.n, 1u);
+            if (at < (uint32_t)THREADS) s.count[at] = order_key(l);
+        }
+        __syncthreads();
+        const uint32_t entries = s.n;
+        if (entries > (uint32_t)THREADS) return false;
+        mine = (uint32_t)tid < entries;
+        if (mine) {
+            key = s.count[tid];
+            s.mass[tid] = by_mass ? amount(key_value(key)) : 0;
+        }
+        __syncthreads();
+        if (mine) {
+            upto_n = over_n = 0;
+            upto_q = over_q = 0;
+            for (uint32_t j = 0; j < entries; ++j) {
+                const uint32_t k = s.count[j];
+                const uint64_t x = s.mass[j];
+                upto_n += k >= key;
+                over_n += k > key;
+                upto_q += k >= key ? x : 0;
+                over_q += k > key ? x : 0;
+            }
+        }
+        return true;
+    };
+    if (!listed()) return cuts;
+    if (set.top_k) {
+        const uint32_t need = (uint32_t)set.top_k - s.above;
+        const bool reaches = need <= s.n;            // else it lies where nothing weighs anything
+        if (mine && over_n < need && need <= upto_n) { s.border = key; s.kept_mass = upto_q; }          // equal ones write the same
+        __syncthreads();
+        cuts = {s.border, true, !by_mass};
+        if (!by_mass) return cuts;
+        target = share_of(set.top_p, reaches ? s.above_mass + s.kept_mass : all);
+        if (target <= s.above_mass) {                // in a bin above
+            __syncthreads();
+            find_mass();
+            if (tid == 0) s.n = 0;
+            if (!listed()) return cuts;
+        }
+    }
+    const uint64_t need = target - s.above_mass;
+    if (mine && over_q < need && need <= upto_q) s.border = key;
+    __syncthreads();
+    return {s.border, true, true};
+}
+
+// A row by a workgroup, in as many sweeps of it as the cuts need: one for the maximum, those of cut_by_bins or four digits of the k-th largest key and four of
+// the key at which the mass reaches p, one for the sum of what is kept and a part of one for the token.
 // cache: or null, LDS for the row (short ones), which is then read once.
 template <class T, int THREADS>
 __device__ __forceinline__ void draw_row(const DrawArgs& a, const DrawRows& rows, int r, const double* table, float* cache) {
     constexpr int WAVES = THREADS / 64;
-    __shared__ uint64_t hist[256];
+    constexpr bool BINS = THREADS == kBins;
+    __shared__ std::conditional_t<BINS, RowBins, NoBins> bins;
+    uint64_t* hist = bins.mass;
     __shared__ Select sel;
     __shared__ double s_sum[WAVES];
     __shared__ float s_max[WAVES];
@@ -260,13 +386,19 @@ __device__ __forceinline__ void draw_row(const DrawArgs& a, const DrawRows& rows
         floor_key = sel.prefix > floor_key ? sel.prefix : floor_key;
         __syncthreads();
     };
-    if (set.top_k) {
+    // integers add in any order: 2^-b of the largest weight, b as V of them leave room for
+    const double unit = ldexp(1.0, 30 + __clz(V));
+    Cuts cuts = {0u, !set.top_k, !(set.top_p < 1.0)};
+    if constexpr (BINS)
+        if (cache && !(cuts.by_count && cuts.by_mass)) {
+            cuts = cut_by_bins(bins, cache, V, m, weight, set, unit);
+            floor_key = cuts.floor_key;
+        }
+    if (!cuts.by_count) {
         if (tid == 0) { sel.prefix = 0; sel.remaining = (uint64_t)set.top_k; }
         descend([](float) { return (uint64_t)1; }, [] {});
     }
-    if (set.top_p < 1.0) {
-        // integers add in any order: 2^-b of the largest weight, b as V of them leave room for
-        const double unit = ldexp(1.0, 30 + __clz(V));
+    if (!cuts.by_mass) {
         if (tid == 0) { sel.prefix = 0; sel.remaining = 0; }
         descend([&](float l) { return (uint64_t)rint(weight(l) * unit); }, [&] {
             const uint64_t z = sum_of(hist, lane);
@@ -323,7 +455,6 @@ constexpr int kPiece = 2048;          // neighbouring entries of a wave: 32 a la
 constexpr int kMaxPieces = 256;       // of a row
 constexpr int kWgWaves = 8;           // waves of a workgroup
 constexpr int kSlice = kPiece * kWgWaves;
-constexpr int kBins = 1024, kPerNat = 32;          // bins over the 32 below the maximum of (l - m) / T, and the last for what lies further down
 constexpr int kCopies = 4;            // of a histogram: neighbouring lanes do not meet in one
 constexpr uint32_t kOne = 1u << 19;   // an entry in it; below, the sum of places of seven bits.  Room for all that lanes of one copy have:
 static_assert(kSlice / kCopies * 127 < (int)kOne && kSlice / kCopies < (1 << 13) && kSlice < (1 << 16), "a bin overflows");
@@ -373,10 +504,6 @@ struct Piece {
     }
 };
 
-// monotone in l, and their floors whole numbers that floats hold exactly
-__device__ __forceinline__ float bin_scale(float temperature) { return (float)kPerNat / temperature; }
-__device__ __forceinline__ float bin_place(float l, float scale) { return fminf(fmaxf(l * scale, -4194304.f), 4194304.f); }
-__device__ __forceinline__ float bin_floor(float l, float scale) { return floorf(bin_place(l, scale)); }
 // the least logit whose floor is at least f (NaN, which none reaches: there is none), for every 16 lanes of a wave one f: four bits of its key at a time, lane i
 // of the 16 tries the last key of the i-th range
 __device__ __forceinline__ float least_logit(float f, float scale, int lane) {
@@ -607,9 +734,7 @@ __global__ __launch_bounds__(kBins) void draw_plan_kernel(DrawArgs a, DrawRows r
     const int bin = lane < 16 ? lo - 1 : lane < 32 ? hi : lane < 48 ? cut - 1 : cut;
     float t = least_logit(bin < 0 ? NAN : top - (float)bin, scale, lane);
     if (bin < 0) t = NAN;                                       // above every logit
-    // The last bin's candidates end where weights are 0 in 64 bits too, so that a mask's -inf or lowest number is none: kept or not, such an entry is never drawn.
-    // (Where 30 of 151,936 are allowed and 50 are asked for, 64 rows: 48 us, and 1,008 with all of them as candidates, which the list does not hold.)
-    if (bin == kBins - 1) t = fmaxf(m - 1000.f * set.temperature, -3.402823466e38f);
+    if (bin == kBins - 1) t = least_candidate(m, set.temperature);
     plan.keep = __shfl(t, 0, 64);
     plan.list = __shfl(t, 16, 64);
     if (set.top_k) {

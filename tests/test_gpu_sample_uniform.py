@@ -238,3 +238,30 @@ def test_counts_that_reach_the_undefined_logits(sb, V, dtype, fill):
     rows = place(x, dtype, 0, 0)
     for s in (dict(k=50), dict(k=50, p=0.9), dict(k=V - 1, p=0.7, T=0.8), dict(k=50, mp=0.1), dict(k=30, T=0.5)):
         check(rows, u, run(sb, rows, u, fill=fill, **s), **s, least=1.0)
+
+
+@pytest.mark.parametrize("V,dtype", [(16383, "float32"), (9001, "bfloat16"), (2039, "float16"), (1025, "float32"), (1024, "bfloat16"), (130, "float32")])
+def test_short_rows_whose_borders_lie_anywhere(sb, V, dtype):
+    """Borders in the first bins and the last, between two, among equal entries (more of them than a workgroup has threads), above and below masked ones."""
+    rng = np.random.default_rng(V + 1)
+    B = 14
+    low = {"float32": -3.4028235e38, "bfloat16": -3.3895314e38, "float16": -65504.0}[dtype]
+    for s in (dict(k=50), dict(k=V - 1), dict(k=V // 2, p=0.5), dict(p=0.01), dict(p=0.999), dict(k=V // 3, p=0.9999, T=0.7), dict(k=50, p=0.9, mp=0.02), dict(k=2, p=0.99),
+              dict(p=0.9, T=0.05), dict(k=40, T=30.0), dict(k=V // 2, p=0.6, T=1e-6), dict(p=0.3, T=1e4)):
+        x = (rng.normal(size=(B, V)) * 2).astype(np.float32)
+        x[1] = np.round(x[1])                                              # a few values for all
+        x[2] = 1.5
+        x[3, rng.random(V) < 0.98] = -np.inf
+        x[4, rng.random(V) < 0.98] = low
+        x[5, rng.random(V) < 0.98] = np.nan
+        x[6, rng.choice(V, V // 4, replace=False)] = 9.25                  # the largest, many of them
+        x[7] -= 5e4 if dtype == "float16" else 1e6
+        x[8, rng.choice(V, 3, replace=False)] = np.inf
+        x[9] = np.where(rng.random(V) < 0.5, 4.0, -4.0)
+        x[10] = np.linspace(-20, 20, V)
+        x[11, 1:] = -np.inf
+        x[12] *= 0.01
+        x[13] = np.nan
+        u = rng.random(B).astype(np.float32)
+        rows = place(x, dtype, 3, 1)
+        check(rows, u, run(sb, rows, u, **s), **s, least=0.6)
