@@ -390,10 +390,13 @@ typedef struct spiral_adamw_tensor {
  * aligned), enqueued on `stream`; it must stay valid as long as the object, and nothing else is kept.  Tensors are aligned to their elements.
  * No buffer that a step writes may overlap another buffer of the table; gradients are only read.  spiral_adamw_set_grads exchanges the
  * gradients' addresses (host_dev_grads [n_tensors], same sizes and types, under the same rules) for the steps enqueued on `stream` after it.
+ * It cannot see how many addresses there are nor what lies behind them: fewer than n_tensors, or a buffer of fewer elements or another type, is undefined.
+ * spiral_adamw_check_grads says what spiral_adamw_set_grads would refuse, and a count n other than n_tensors; it enqueues nothing.
  * Errors: INVALID_ARG (null or misaligned pointer, unknown or impossible types, n < 1, overlap), HIP; NOT_LOADED (null object). */
 size_t spiral_adamw_bytes(int n_tensors);
 int  spiral_adamw_create(const spiral_adamw_tensor* host_tensors, int n_tensors, void* dev_mem, size_t bytes, void* stream,
                          spiral_adamw** out);
+int  spiral_adamw_check_grads(const spiral_adamw* o, const void* const* host_dev_grads, int n);
 int  spiral_adamw_set_grads(spiral_adamw* o, const void* const* host_dev_grads, void* stream);
 /* step >= 1 is the number of this step (a captured call that is replayed keeps it, as it keeps lr and the others).
  * max_norm == 0: gradients are not clipped.  dev_norm (fp32 [1] or NULL) receives N.  Where N is computed (max_norm > 0 or

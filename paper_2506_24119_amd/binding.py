@@ -38,7 +38,7 @@ EXPORTS = [
     "spiral_decode_step_static", "spiral_static_workspace_bytes", "spiral_probe_stream_read",
     "spiral_sample_truncated_ws", "spiral_sample_truncated_workspace_bytes",
     "spiral_sample_uniform", "spiral_sample_uniform_workspace_bytes", "spiral_policy_gradient", "spiral_policy_gradient_workspace_bytes",
-    "spiral_adamw_bytes", "spiral_adamw_create", "spiral_adamw_set_grads", "spiral_adamw_step", "spiral_adamw_free",
+    "spiral_adamw_bytes", "spiral_adamw_create", "spiral_adamw_check_grads", "spiral_adamw_set_grads", "spiral_adamw_step", "spiral_adamw_free",
 ]
 
 
@@ -156,6 +156,8 @@ def load_library(path: Optional[str] = None):
     lib.spiral_adamw_bytes.argtypes = [C.c_int]
     lib.spiral_adamw_create.restype = C.c_int
     lib.spiral_adamw_create.argtypes = [C.POINTER(spiral_adamw_tensor_t), C.c_int, vp, C.c_size_t, vp, C.POINTER(vp)]
+    lib.spiral_adamw_check_grads.restype = C.c_int
+    lib.spiral_adamw_check_grads.argtypes = [vp, C.POINTER(C.c_void_p), C.c_int]
     lib.spiral_adamw_set_grads.restype = C.c_int
     lib.spiral_adamw_set_grads.argtypes = [vp, C.POINTER(C.c_void_p), vp]
     lib.spiral_adamw_step.restype = C.c_int
@@ -504,17 +506,30 @@ def spiral_adamw_bytes(tensors) -> int:
     return int(load_library().spiral_adamw_bytes(len(tensors)))
 
 
+_adamw_grads = {}                # of every optimiser: elements and type of each record's gradient, which the library's call is given addresses of alone
+
+
 def spiral_adamw_create(tensors: Sequence[spiral_adamw_tensor_t], dev_mem, stream=None) -> int:
     arr = (spiral_adamw_tensor_t * len(tensors))(*tensors)
     out = C.c_void_p()
-    _check(load_library().spiral_adamw_create(arr, len(tensors), _ptr(dev_mem), dev_mem.numel() * dev_mem.element_size(), _stream_handle(stream),
-                                              C.byref(out)))
+    _check(load_library().spiral_adamw_create(arr, len(tensors), _ptr(dev_mem), 0 if dev_mem is None else dev_mem.numel() * dev_mem.element_size(),
+                                              _stream_handle(stream), C.byref(out)))
+    _adamw_grads[out.value] = [(t.n, t.grad_dtype) for t in tensors]
     return out.value
 
 
 def spiral_adamw_set_grads(opt: int, grads, stream=None):
     """grads: one contiguous tensor of the record's size and type per record."""
-    arr = (C.c_void_p * len(grads))(*[g.data_ptr() for g in grads])
+    wanted = _adamw_grads.get(opt)
+    if wanted is None:
+        raise ValueError("gradients: no optimiser that spiral_adamw_create made, or one that is freed")
+    if len(grads) != len(wanted):
+        raise ValueError(f"gradients: {len(wanted)} are needed, one per record, got {len(grads)}")
+    arr = (C.c_void_p * len(grads))(*[_ptr(g) for g in grads])
+    _check(load_library().spiral_adamw_check_grads(opt, arr, len(grads)))
+    for i, (g, (n, dtype)) in enumerate(zip(grads, wanted)):
+        if g.numel() != n or _dtype(g) != dtype or not g.is_contiguous():
+            raise ValueError(f"gradient {i}: {n} contiguous elements of the record's type are needed, got {tuple(g.shape)} of {g.dtype}, strides {g.stride()}")
     _check(load_library().spiral_adamw_set_grads(opt, arr, _stream_handle(stream)))
 
 
@@ -525,6 +540,7 @@ def spiral_adamw_step(opt: int, lr: float, beta1: float, beta2: float, eps: floa
 
 
 def spiral_adamw_free(opt: int):
+    _adamw_grads.pop(opt, None)
     load_library().spiral_adamw_free(opt)
 
 

@@ -223,15 +223,27 @@ static bool overwritten(const spiral_adamw* o, const void* p, uintptr_t bytes) {
     return next != end && next->lo < lo + bytes;
 }
 
-extern "C" int spiral_adamw_set_grads(spiral_adamw* o, const void* const* host_dev_grads, void* stream) {
-    if (!o) return fail(SPIRAL_ERR_NOT_LOADED, "adamw_set_grads: null object");
-    if (!host_dev_grads) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: null array");
+static int check_grads(const spiral_adamw* o, const void* const* host_dev_grads, const char* who) {
+    if (!o) return fail(SPIRAL_ERR_NOT_LOADED, "%s: null object", who);
+    if (!host_dev_grads) return fail(SPIRAL_ERR_INVALID_ARG, "%s: null array", who);
     for (int t = 0; t < o->n; ++t) {
         if (!host_dev_grads[t] || !aligned(host_dev_grads[t], dtype_size(o->table[t].grad_dtype)))
-            return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: gradient %d is null or misaligned", t);
+            return fail(SPIRAL_ERR_INVALID_ARG, "%s: gradient %d is null or misaligned", who, t);
         if (overwritten(o, host_dev_grads[t], (uintptr_t)o->table[t].n * dtype_size(o->table[t].grad_dtype)))
-            return fail(SPIRAL_ERR_INVALID_ARG, "adamw_set_grads: gradient %d overlaps a buffer that is written", t);
+            return fail(SPIRAL_ERR_INVALID_ARG, "%s: gradient %d overlaps a buffer that is written", who, t);
     }
+    return SPIRAL_OK;
+}
+
+extern "C" int spiral_adamw_check_grads(const spiral_adamw* o, const void* const* host_dev_grads, int n) {
+    if (!o) return fail(SPIRAL_ERR_NOT_LOADED, "adamw_check_grads: null object");
+    if (n != o->n) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_check_grads: %d gradients for %d tensors", n, o->n);
+    return check_grads(o, host_dev_grads, "adamw_check_grads");
+}
+
+extern "C" int spiral_adamw_set_grads(spiral_adamw* o, const void* const* host_dev_grads, void* stream) {
+    const int rc = check_grads(o, host_dev_grads, "adamw_set_grads");
+    if (rc) return rc;
     for (int t = 0; t < o->n; ++t) o->table[t].grad = host_dev_grads[t];
     return adamw_upload(o, stream, "adamw_set_grads");
 }
