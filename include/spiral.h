@@ -365,7 +365,7 @@ int spiral_policy_gradient(const void* dev_logits, int dtype, long long row_stri
  * One step over all tensors of a model at once, e.g. the weights that spiral_model_load was given (a repacked model is repacked
  * again afterwards).  With g = grad_scale * gradient, N = the 2-norm of all g together, c = min(1, max_norm / N):
  *     m <- beta1 m + (1 - beta1) c g ,   v <- beta2 v + (1 - beta2) (c g)^2
- *     p <- p (1 - lr * weight_decay) - lr * (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ *     p <- p - (lr * weight_decay) p - lr * (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
  * in fp32 (the sum of N in 64 bits), rounded to the parameter's type where there is a master copy, which holds p in fp32.
  * States of SPIRAL_DTYPE_FP32 hold m and v.  States of SPIRAL_DTYPE_E4M3 hold, for every block of SPIRAL_ADAMW_BLOCK elements of a tensor
  * (the last one may be shorter), codes and an fp32 scale: m = code * m_scale, sqrt(v) = code * v_scale, each scale the block's

@@ -151,7 +151,7 @@ __device__ __forceinline__ void step_runs(const AdamwArgs& a, const AdamwRec& r,
     const float c = clip();
     if (c < 0.f) return;
     const bool g_bf16 = r.grad_dtype == SPIRAL_DTYPE_BF16, p_bf16 = r.param_dtype == SPIRAL_DTYPE_BF16;
-    const float keep = r.decay ? a.keep : 1.f;
+    const float decay = r.decay ? a.decay : 0.f;
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
         const long long i = first + k * kRun + threadIdx.x * kPer;
@@ -178,7 +178,10 @@ __device__ __forceinline__ void step_runs(const AdamwArgs& a, const AdamwRec& r,
             }
             moments(a, g, m[e], v[e]);
             const float root = sqrtf(v[e]);
-            p[e] = p[e] * keep - a.step_size * m[e] * __builtin_amdgcn_rcpf(root * a.root_scale + a.eps);
+            // lr wd itself, not 1 - lr wd, which 32 bits know to 6e-8: at lr = 1e-6 a decay of 0.01 would be none and one of 0.1 a fifth too strong.  (An infinite
+            // parameter, as fp16 may have without a master, stays what it is.)
+            const float shrink = decay * __builtin_amdgcn_fmed3f(p[e], -3.402823466e38f, 3.402823466e38f);
+            p[e] -= shrink + a.step_size * m[e] * __builtin_amdgcn_rcpf(root * a.root_scale + a.eps);
             if (CODES) {
                 v[e] = root;
                 m_most = fmaxf(m_most, fabsf(m[e]));

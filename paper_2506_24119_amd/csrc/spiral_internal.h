@@ -267,8 +267,8 @@ struct AdamwArgs {
     long long chunks;
     double* part;                             // [kAdamwParts]
     float* norm;                              // or null
-    // rest1 = 1 - beta1, rest2 = 1 - beta2 (in 32 bits 1 - 0.9f is 2e-7 off), keep = 1 - lr wd, step_size = lr / (1 - beta1^t), root_scale = (1 - beta2^t)^-1/2
-    float beta1, rest1, beta2, rest2, eps, keep, step_size, root_scale, grad_scale, max_norm;
+    // rest1 = 1 - beta1, rest2 = 1 - beta2 (in 32 bits 1 - 0.9f is 2e-7 off), decay = lr wd, step_size = lr / (1 - beta1^t), root_scale = (1 - beta2^t)^-1/2
+    float beta1, rest1, beta2, rest2, eps, decay, step_size, root_scale, grad_scale, max_norm;
 };
 int adamw_steps(long long elements);          // runs of 1,024 elements in a chunk, for tensors of so many in all
 long long adamw_chunks(long long n, int steps);      // chunks that a tensor of n elements is cut into

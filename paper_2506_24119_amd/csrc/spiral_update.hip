@@ -275,7 +275,7 @@ extern "C" int spiral_adamw_step(spiral_adamw* o, double lr, double beta1, doubl
     a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1);
     a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2);
     a.eps = (float)eps;
-    a.keep = (float)(1.0 - lr * weight_decay);
+    a.decay = (float)(lr * weight_decay);
     a.step_size = (float)(lr / (1.0 - std::pow(beta1, step)));
     a.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, step)));
     a.grad_scale = grad_scale;
