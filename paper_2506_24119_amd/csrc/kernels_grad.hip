@@ -53,7 +53,7 @@ __device__ __forceinline__ float policy_slope(const GradArgs& a, long long row, 
         const float rc = fminf(fmaxf(r, 1.f - a.clip_eps), 1.f + a.clip_eps);
         d = r * A <= rc * A ? r * A : r * A > rc * A ? 0.f : NAN;
     }
-    return d * (a.scale * a.inv_t);
+    return (float)((double)d * a.unit);                // scale / T may pass 32 bits where the slope does not, and nothing times it is nothing
 }
 
 // U vectors' maximum, then their sum under it; those beyond the end (`in` says which) may count for the maximum: they repeat one that is there

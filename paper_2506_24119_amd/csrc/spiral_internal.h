@@ -244,7 +244,8 @@ struct GradArgs {
     const float* logp_old;                    // or null: no ratio
     const float* advantage;
     const int32_t* mask;                      // or null
-    float inv_t, clip_eps, scale;
+    float inv_t, clip_eps;
+    double unit;                              // scale / temperature
     float* logp;
 };
 int policy_grad_slices(long long n_rows, int V, int dtype);      // workgroups of a row; 1: one launch, more: two

@@ -114,7 +114,7 @@ extern "C" int spiral_policy_gradient(const void* dev_logits, int dtype, long lo
     a.logits = dev_logits; a.row_stride = row_stride; a.grad = dev_grad; a.grad_stride = grad_stride;
     a.n_rows = n_rows; a.V = V;
     a.targets = dev_targets; a.logp_old = dev_logp_old; a.advantage = dev_advantage; a.mask = dev_mask;
-    a.inv_t = 1.f / temperature; a.clip_eps = clip_eps; a.scale = scale; a.logp = dev_logp;
+    a.inv_t = 1.f / temperature; a.clip_eps = clip_eps; a.unit = (double)scale / temperature; a.logp = dev_logp;
     return done(launch_policy_grad(a, dtype, dev_workspace, (hipStream_t)stream), "policy_gradient");
 }
 
