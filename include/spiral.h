@@ -402,8 +402,8 @@ int  spiral_adamw_set_grads(spiral_adamw* o, const void* const* host_dev_grads, 
  * max_norm == 0: gradients are not clipped.  dev_norm (fp32 [1] or NULL) receives N.  Where N is computed (max_norm > 0 or
  * dev_norm given) and is not finite in fp32, the step changes no parameter and no state; where it is not computed, a gradient that is
  * not finite leaves its element undefined, and of 8-bit states its block.  Steps of one object must be ordered on one stream.
- * Errors: NOT_LOADED, INVALID_ARG (betas outside [0, 1), eps outside [1e-30, 1e30], a negative or not finite lr, weight_decay or max_norm, a grad_scale
- * that is not finite, step < 1, dev_norm misaligned or inside a buffer of the table or dev_mem), HIP. */
+ * Errors: NOT_LOADED, INVALID_ARG (betas outside [0, 1), eps outside [1e-30, 1e30], a negative or not finite lr, weight_decay or max_norm, lr * weight_decay
+ * or lr / (1 - beta1^step) past fp32's range, a grad_scale that is not finite, step < 1, dev_norm misaligned or inside a buffer of the table or dev_mem), HIP. */
 int  spiral_adamw_step(spiral_adamw* o, double lr, double beta1, double beta2, double eps, double weight_decay, int step,
                        float grad_scale, float max_norm, float* dev_norm, void* stream);
 void spiral_adamw_free(spiral_adamw* o);

@@ -257,6 +257,8 @@ extern "C" int spiral_adamw_step(spiral_adamw* o, double lr, double beta1, doubl
     if (!(eps >= 1e-30) || !(eps <= 1e30)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: eps must be in [1e-30, 1e30]");
     if (!(max_norm >= 0.f) || !std::isfinite(max_norm) || !std::isfinite(grad_scale)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: bad max_norm or grad_scale");
     if (step < 1) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: steps are counted from 1");
+    const float decay = (float)(lr * weight_decay), step_size = (float)(lr / (1.0 - std::pow(beta1, step)));
+    if (!std::isfinite(decay) || !std::isfinite(step_size)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: lr * weight_decay or lr / (1 - beta1^step) passes 32 bits");
     if (!aligned(dev_norm, 4)) return fail(SPIRAL_ERR_INVALID_ARG, "adamw_step: misaligned norm");
     if (dev_norm) {                                  // also none of the gradients, which other workgroups still read when it is written
         bool meets = overwritten(o, dev_norm, 4);
@@ -275,8 +277,8 @@ extern "C" int spiral_adamw_step(spiral_adamw* o, double lr, double beta1, doubl
     a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1);
     a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2);
     a.eps = (float)eps;
-    a.decay = (float)(lr * weight_decay);
-    a.step_size = (float)(lr / (1.0 - std::pow(beta1, step)));
+    a.decay = decay;
+    a.step_size = step_size;
     a.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, step)));
     a.grad_scale = grad_scale;
     a.max_norm = max_norm;
