@@ -309,15 +309,17 @@ int spiral_sample_truncated_ws(const float* dev_logits, int B, int V, float temp
                                void* dev_workspace, size_t workspace_bytes, void* stream);
 
 /* ---- sampling from given uniform numbers ---------------------------------------------------------
- * One token a row by the inverse of the cumulative distribution, with the log-probability under which it was drawn (the
- * old policy's in the ratio of the objective below).  Every row has its own settings, so that one call serves a batch of
- * requests.  With m = max_v logit_v and w_v = exp((logit_v - m) / T), evaluated in 64 bits:
+ * One token a row by the inverse of the cumulative distribution, with the log-probability under which it was drawn.  Every row
+ * has its own settings, so that one call serves a batch of requests.  With m = max_v logit_v and w_v = exp((logit_v - m) / T), evaluated in 64 bits:
  *     top_k in (0, V): keep the logits that are no less than the k-th largest                (<= 0 or >= V: off)
  *     top_p in (0, 1): over the top-k survivors, walk the logits in descending order and stop where the running sum of w
  *                      first reaches top_p times their sum; keep the logits that are no less than that one  (1: off)
  *     min_p in (0, 1]: keep w_v >= min_p                                                     (0: off)
  *     token = the least v whose running sum of the kept w_0 .. w_v exceeds u times their whole sum
  *     logp  = log( w_token / sum of the kept w )
+ * That is the old policy's in the ratio of the objective below only for rows without a cut at the objective's own temperature: top_k, top_p
+ * and min_p leave it larger by -log of the mass that is kept (and T == 0 leaves 0), so that every ratio would come out below 1.  For
+ * other rows take the old one from a call of spiral_policy_gradient on the weights that drew, or at temperature 1 from spiral_score.
  * Equal logits are kept or dropped together.  T == 0 is greedy: the lowest index of the maximum, logp 0, cuts and u ignored.
  * An undefined logit counts as -inf and is never drawn; logits of +inf share all of the mass; a row with nothing above
  * -inf gives token 0 with logp -inf.  u is meant to be uniform in [0, 1): less (or NaN) counts as 0, more as the number below 1.

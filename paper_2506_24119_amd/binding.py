@@ -453,7 +453,8 @@ def spiral_sample_uniform_workspace_bytes(B: int, V: int) -> int:
 
 
 def spiral_sample_uniform(dev_logits, temperature, top_k, top_p, min_p, dev_uniform, dev_workspace, dev_out_tokens, dev_out_logp=None, stream=None):
-    """dev_logits: [B, V] fp32, bf16 or fp16 with contiguous rows; the settings: None, one value, or one per row."""
+    """dev_logits: [B, V] fp32, bf16 or fp16 with contiguous rows; the settings: None, one value, or one per row.  dev_out_logp: of the kept
+    set, so a ratio's old log-probability only for rows without a cut at the objective's temperature."""
     B, V, stride = _rows_of(dev_logits, "logits")
     T, Tp = _setting(temperature, B, np.float32, "temperature")
     k, kp = _setting(top_k, B, np.int32, "top_k")
