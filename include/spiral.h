@@ -345,8 +345,11 @@ int spiral_sample_uniform(const void* dev_logits, int logits_dtype, long long ro
  * (dev_logp_old NULL: J = sum_t mask_t * A_t * logp_t, the REINFORCE sum), the call returns every logp_t and the gradient of
  * the loss -scale * J in the logits:
  *     grad[t, v] = -scale * mask_t * A_t * r_t * [r_t A_t <= clip(r_t) A_t] * (1{v = y_t} - softmax(z_t)_v) / temperature
- * (without the ratio and the bracket where dev_logp_old is NULL).  spiral_policy_objective gives the values of J from dev_logp.
- * Rows with mask 0 or a target < 0 count for nothing: logp 0, a gradient row of zeros, their logits are not read.  A target
+ * (without the ratio and the bracket where dev_logp_old is NULL; mask_t is 0 or 1, any value but 0 being 1).
+ * Rows with mask 0 or a target < 0 count for nothing: logp 0, a gradient row of zeros, their logits are not read.
+ * spiral_policy_objective gives the value of J from dev_logp: dev_out2[0], with a mask that is 0 wherever the target is < 0 too (it sees no
+ * targets and would take that 0 for a token's logp); without old ones dev_out2[1], with dev_logp in their place.  A logp of NaN shows in dev_out2[1] only.
+ * A target
  * >= V, a NaN or +inf logit or a row without any above -inf leaves that row's logp, and its gradient, NaN.  Sums are fp32
  * or more; the gradient is rounded once, to the logits' type.  Results repeat bit for bit.
  * dev_logits [n_rows, V], rows row_stride apart, dev_grad [n_rows, V], rows grad_stride apart, both of `dtype` (SPIRAL_DTYPE_FP32, _BF16,
