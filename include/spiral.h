@@ -376,7 +376,12 @@ int spiral_policy_gradient(const void* dev_logits, int dtype, long long row_stri
  * (the last one may be shorter), codes and an fp32 scale: m = code * m_scale, sqrt(v) = code * v_scale, each scale the block's
  * largest magnitude / 448, codes rounded to nearest even, but a positive sqrt(v) never to 0 (the denominator would be eps): to
  * the least code, 2^-9, instead.  A block whose largest magnitude is at most 1e-30 holds zeros.  The root is what is stored because its codes
- * reach the same 5 decades of gradient sizes that m's do.  All-zero states (codes and scales) are those of step 0. */
+ * reach the same 5 decades of gradient sizes that m's do.  All-zero states (codes and scales) are those of step 0.
+ * Nearest codes, 6 to 12% apart, cannot follow a decay of 1 - sqrt(beta2) a step by themselves: a root falls with its gradients and as its block's
+ * maximum moves.  Over many steps, against states of 32 bits: under gradients of one size sqrt(v) is 1.06 times as large in the median at beta2 = 0.95 (0.92 to
+ * 1.23 for nine elements in ten, updates 0.95 times the size), 1.1 times at 0.999 (0.74 to 1.48).  Where an element's gradients fall tenfold beside others of its
+ * block that do not, the root is 1.8 times too large after 100 steps at 0.95 and right after 300; at 0.99 it is 12 times too large after 1,000, and its
+ * updates as much too small.  8 bits are meant for beta2 up to 0.95; above, keep the states in 32. */
 #define SPIRAL_ADAMW_BLOCK 256
 typedef struct spiral_adamw spiral_adamw;
 typedef struct spiral_adamw_tensor {
