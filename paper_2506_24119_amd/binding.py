@@ -195,7 +195,8 @@ def _ip(a: Optional[np.ndarray]):
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())      # torch.cuda.current_stream() without its object: 0.5 us, not 3
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # not a public name: current_stream() without its object, 0.5 us and not 3
+        return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
 
