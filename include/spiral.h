@@ -349,9 +349,8 @@ int spiral_sample_uniform(const void* dev_logits, int logits_dtype, long long ro
  * Rows with mask 0 or a target < 0 count for nothing: logp 0, a gradient row of zeros, their logits are not read.
  * spiral_policy_objective gives the value of J from dev_logp: dev_out2[0], with a mask that is 0 wherever the target is < 0 too (it sees no
  * targets and would take that 0 for a token's logp); without old ones dev_out2[1], with dev_logp in their place.  A logp of NaN shows in dev_out2[1] only.
- * A target
- * >= V, a NaN or +inf logit or a row without any above -inf leaves that row's logp, and its gradient, NaN.  Sums are fp32
- * or more; the gradient is rounded once, to the logits' type.  Results repeat bit for bit.
+ * A target >= V, a NaN or +inf logit or a row without any above -inf leaves that row's logp, and its gradient, NaN.  Sums are fp32 or
+ * more; the gradient is rounded once, to the logits' type.  Results repeat bit for bit.
  * dev_logits [n_rows, V], rows row_stride apart, dev_grad [n_rows, V], rows grad_stride apart, both of `dtype` (SPIRAL_DTYPE_FP32, _BF16,
  * _FP16) and aligned to an element; the gradient may be written in place (same pointer, same stride) but not overlap the logits in another way.
  * Nothing else that is written (dev_grad, dev_logp, the workspace) may overlap another buffer; a matrix counts from its first row's start to its last one's end.

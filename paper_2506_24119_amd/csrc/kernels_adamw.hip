@@ -3,10 +3,11 @@
 // Bound by memory: 28 bytes an element for bf16 weights with fp32 masters and states, 12 + 4 with 8-bit states, of which the norm's sweep reads the
 // gradient's 2 once more.  A workgroup walks chunks of 4,096 elements of whatever tensor they fall in; all of a chunk's loads (4 runs of 4
 // neighbouring elements a thread) are in flight before the first is used, four workgroups a compute unit (128 registers, no spill; five
-// spill and gain 1% with 32-bit states, lose as much with 8-bit ones; chunks of 2,048 with eight: 9% and 5% slower).  Over 303 M elements, bf16 with masters: 1,673 us with 32-bit
-// states (102 in the norm and 5.4 TB/s in the step, where a copy of 4 GiB moves 4.8), 1,012 us with 8-bit states.  What brought them there from 10,279 and 5,624 us: wide loads of any alignment, all
+// spill and gain 1% with 32-bit states, lose as much with 8-bit ones; chunks of 2,048 with eight: 9% and 5% slower).  Over 303 M elements, bf16 with masters: 1,676 us with 32-bit
+// states (103 in the norm and 5.3 TB/s in the step, where a copy of 4 GiB moves 4.8), 1,027 us with 8-bit states.  What brought them there from 10,279 and 5,624 us: wide loads of any alignment, all
 // ahead (2,005, 2,026); as many workgroups as fit (1,779, 1,627); streaming loads and stores that nothing else evicts the gradients for (1,685, 1,502); records by scalar loads instead of
 // two dependent vector loads a chunk (8 bits: 1,108); chunks of four runs (1,670, 1,058).
+// The update's quotient is a product with the hardware's reciprocal, off by one step of 2^-23 where a division would be by half of one; all else is fp32, each operation rounded.
 #include "spiral_internal.h"
 
 namespace spiral {
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(kThreads, WGS) void adamw_step_kernel(AdamwArgs a) 
     }
 }
 
-// Chunks of one run as long as a long chunk would leave compute units without work: 2.5 M elements 20.7 us (73 MB: 14.9 in the step), with long ones 21.1.
+// Chunks of one run as long as a long chunk would leave compute units without work: 2.6 M elements 20.9 us (73 MB: 15.7 in the step), with long ones 21.1.
 int adamw_steps(long long elements) { return elements <= (long long)kAdamwParts * kRun * kLong ? 1 : kLong; }
 long long adamw_chunks(long long n, int steps) { return (n + steps * kRun - 1) / (steps * kRun); }
 

@@ -2,10 +2,16 @@
 //
 // Rows of less than 16,384 logits are a workgroup's (draw_row).  Longer ones are pieces of 2,048, a wave's each, so that 128 rows fill the card and one row still
 // has 75 waves; the sums of the pieces tell in which the number falls, and only that is looked at again.  An uncut batch is one sweep (draw_sum_kernel) and that
-// (draw_pick_kernel): 128 x 151,936 fp32 logits 18.5 + 5.3 us, 4.2 TB/s in the sweep, which the 64-bit weights bound as much as memory (bf16 18.7).  Cut batches: a sweep
-// that counts entries in bins (draw_count_kernel, 18.3 us), the bins between which the cuts fall (draw_plan_kernel, 8.9), a sweep that sums what is kept for sure and lists the
-// entries of those bins (draw_cut_kernel, 26.5), and the exact border among them (draw_pick_kernel, 15.6).  Counts are 32-bit LDS additions; 64-bit masses in the
-// histogram would take 46 us.  Lines, both sides measured: 16,000 and 17,000 logits with top-p, one row 29 and 24 us, 16 rows 35 and 29; uncut 14 to 17 and 13.
+// (draw_pick_kernel): 128 x 151,936 fp32 logits 18.9 + 5.2 us, 4.1 TB/s in the sweep (bf16 21.7 us in all: the sweep takes as long for half the bytes).  Its 6.7 M vector instructions, 22 an
+// entry and 14 of those in 64 bits, are 11 us of issue on every SIMD; the table's bank conflicts are 1 us, and the waves wait for half of their cycles.
+// Cut batches: a sweep that counts entries in bins (draw_count_kernel, 18.2 us), the bins between which the cuts fall (draw_plan_kernel, 9.1), a sweep that sums what is
+// kept for sure and lists the entries of those bins (draw_cut_kernel, 26.8), and the exact border among them (draw_pick_kernel, 13.9).  Counts are 32-bit LDS additions; 64-bit masses in
+// the histogram would take 46 us.  The line, both sides measured, 16,383 and 16,384 fp32 logits: uncut one row 12.5 and 8.2 us, 128 rows 16.7 and 9.5; top-p 0.9 25.2 and
+// 25.7, 29.5 and 28.7; top-k 50, which the workgroup finds in one sweep less, 18.5 and 21.6, 19.7 and 24.1.
+//
+// What is held in fewer bits than the weights: the masses between which a border is sought are whole numbers, of candidates multiples of 2^-50 of the largest weight (8,192 of them
+// fit 64 bits), of a row by a workgroup of 2^-44 at 151,936 logits, so that they add up alike in any order.  A candidate lighter than 2^-51 of the largest has none, and
+// a piece with nothing else is not drawn from: less than 2^-38 of the row, where the given numbers have 24 bits.  The weights of the token's own piece are summed as they are.
 #include <type_traits>
 
 #include "spiral_internal.h"

@@ -3,8 +3,11 @@
 // The slope of a row's gradient needs only the row itself (ratio, clip and advantage are its own), so one kernel does what a forward and a backward pass do:
 // max and sum in one sweep, slope * (softmax - 1{target}) in a second.  Bound by memory: each logit once from HBM, each gradient once to it.  The second
 // sweep reads what the first left in the last-level cache (512 rows of 304 KB at a time, of its 256 MB), but for what the threads have kept in
-// registers.  4,096 rows of 151,936 bf16 logits, a third of them masked: 410 us, 5.1 TB/s of the 2.08 GB that have to be moved (a copy of 4 GiB: 4.8); two
-// sweeps of single elements by 256 threads took 1,574.  1,500 rows of as many fp32: 360 us, 5.1 TB/s.
+// registers.  4,096 rows of 151,936 bf16 logits, a third of them masked: 411 us by the clock, 5.1 TB/s of the 2.08 GB that have to be moved (425 in a trace; a copy of 4 GiB: 4.8); two
+// sweeps of single elements by 256 threads took 1,574.  1,500 rows of as many fp32: 366 us, 5.0 TB/s.
+//
+// Exponentials are the hardware's exp2 of (l - m) (log2 e / T), the factor rounded once: off by up to 4 |z| + 4 of 2^-24, a little more than expf of (l - m) / T
+// would be.  1 / T is rounded before it multiplies; scale / T is held in 64 bits.
 #include "spiral_internal.h"
 
 namespace spiral {
@@ -256,8 +259,9 @@ __global__ __launch_bounds__(kSliceThreads) void policy_slice_kernel(GradArgs a,
 }
 
 // A workgroup takes 21 us for 304 KB, however few of them there are: up to 96 rows of 256 KB or more are cut, into slices of at least 16 KB, as many as give
-// every compute unit four (one row of 151,936 bf16 logits 21.4 -> 14.9 us with the host's share of 11 to 14, 64 of them 23.4 -> 16.3; 128: 24.1 -> 25.9, uncut they stay).  Shorter
-// rows are done before a second launch is made (50,000 fp32 logits: 12.3 us uncut, 14.8 cut).
+// every compute unit four.  Rows of 151,936 logits, uncut and cut: bf16 one 21.5 and 9.6 us, 64 of them 22.1 and 14.7, 96 22.7 and 18.8, 128 24.5 and 25.3; fp32 one 22.0 and 9.2, 64
+// 24.7 and 23.5, 80 26.0 and 29.3, 96 28.6 and 33.6 (a line of their own, at 64, would save those 80 to 96 rows an eighth).  Shorter rows are done before a second
+// launch is made (50,000 fp32 logits: 12.1 us uncut, 14.8 cut).
 int policy_grad_slices(long long n_rows, int V, int dtype) {
     const long long vecs = V / (dtype == SPIRAL_DTYPE_FP32 ? 4 : 8);
     if (n_rows > kSplitRows || vecs < kSplitFrom) return 1;
@@ -289,9 +293,9 @@ static hipError_t launch_some(const GradArgs& a, int slices, void* workspace, hi
         hipLaunchKernelGGL(policy_slice_kernel<T>, grid, dim3(kSliceThreads), 0, s, a, per, pairs, target_logit);
         return hipGetLastError();
     }
-    // As many threads as hold the whole row in 8 vectors each (3,000 rows of 8,000 bf16 logits 20 us; by 1,024 threads 64 to 100).  Longer rows of 16-bit logits
-    // keep 8 as well, two workgroups a compute unit (4,096 x 151,936: 410 us; with none 436, all 19 in one workgroup 704); 32-bit ones keep 20 and have the compute
-    // unit for themselves (1,500 x 151,936: 360 us; 8 and two workgroups 390, none 454).
+    // As many threads as hold the whole row in 8 vectors each (3,000 rows of 8,000 bf16 logits 22 us; by 1,024 threads 64 to 100).  Longer rows of 16-bit logits
+    // keep 8 as well, two workgroups a compute unit (4,096 x 151,936: 411 us; with none 436, all 19 in one workgroup 704); 32-bit ones keep 20 and have the compute
+    // unit for themselves (1,500 x 151,936: 366 us; 8 and two workgroups 390, none 454).
     const dim3 grid((unsigned)a.n_rows);
     constexpr bool WIDE = sizeof(T) == 4;
     if (n_vec <= 256 * 8) hipLaunchKernelGGL((policy_grad_kernel<T, 256, 8, 8>), grid, dim3(256), 0, s, a);
