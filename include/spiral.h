@@ -8,7 +8,8 @@
  * i.e. an untruncated categorical), plus the role-conditioned advantage
  * estimation baseline (Sec. 3, RAE equation; Alg. 1, policy-optimisation loop), and
  * what closes an update of the policy: a draw with its log-probability, the gradient
- * of the objective in the logits, AdamW.
+ * of the objective in the logits, what a decoder block has between its matrix products
+ * (attention, norms, rotation) forward and backward, AdamW.
  *
  * General rules
  *  - Every function returns SPIRAL_OK (0) or a negative SPIRAL_ERR_* code; it
@@ -20,8 +21,8 @@
  *    frees device memory and never synchronises the stream; all device work is
  *    enqueued on the stream that is passed in (`stream` is a hipStream_t, NULL =
  *    the default stream).  Host arrays are consumed before the call returns.
- *  - Opaque host objects (model, pool, optimiser, RAE state) are created and freed by the
- *    library.  Calls on the same object must not overlap.
+ *  - Opaque host objects (model, pool, attention plan, optimiser, RAE state) are created and freed by the
+ *    library.  Calls on the same object must not overlap (but for a plan's, which only read it).
  *  - A failed call leaves sequence lengths and page tables unchanged: the sequences' lengths, their page lists
  *    and the free list are host-side state that is advanced only after every launch of the call was accepted
  *    (pages taken earlier in the call are returned).  After SPIRAL_ERR_HIP some kernels of the call may already
@@ -51,11 +52,11 @@ extern "C" {
 #define SPIRAL_WEIGHT_FP32 0
 #define SPIRAL_WEIGHT_BF16 1
 
-/* element types of the buffers of the sampler with given numbers, the policy gradient and the optimiser */
+/* element types of the buffers of the sampler with given numbers, the learner's operators and the optimiser */
 #define SPIRAL_DTYPE_FP32 0
 #define SPIRAL_DTYPE_BF16 1
 #define SPIRAL_DTYPE_FP16 2
-#define SPIRAL_DTYPE_E4M3 3          /* optimiser states only: 8-bit floats (4 exponent, 3 mantissa bits) under a scale per block */
+#define SPIRAL_DTYPE_E4M3 3          /* optimiser states (a scale per block) and normed rows (a scale per row): 8-bit floats, 4 exponent and 3 mantissa bits */
 
 #define SPIRAL_MAX_BATCH 1024        /* sequences per prefill / decode / sample call */
 
@@ -364,6 +365,88 @@ int spiral_policy_gradient(const void* dev_logits, int dtype, long long row_stri
                            const int32_t* dev_targets, const float* dev_logp_old, const float* dev_advantage,
                            const int32_t* dev_mask, float temperature, float clip_eps, float scale, float* dev_logp,
                            void* dev_grad, long long grad_stride, void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* ---- causal attention over packed sequences (learner side) -----------------------------------------
+ * The attention of a decoder block and its gradient, for the learner's own forward and backward pass over whole games.  B sequences lie
+ * back to back in n_rows = sum(host_lens) rows (lengths of 0 are allowed); position i of a sequence sees its positions 0 .. i.  With
+ * query head h and its kv head h / (n_q_heads / n_kv_heads):
+ *     s_ij = scale q_i . k_j ,  lse_i = log sum_{j <= i} exp(s_ij) ,  p_ij = exp(s_ij - lse_i) ,  out_i = sum_{j <= i} p_ij v_j
+ * and for a gradient dout of the outputs, D_i = dout_i . out_i ,  t_ij = p_ij (dout_i . v_j - D_i):
+ *     dq_i = scale sum_{j <= i} t_ij k_j ,  dk_j = scale sum_{i >= j} t_ij q_i ,  dv_j = sum_{i >= j} p_ij dout_i
+ * the sums of dk and dv also over the query heads that share the kv head.  Nothing that a position does not see reaches its results, NaN and
+ * infinities included, and rows behind the last sequence are neither read nor written.  Sums and the softmax are fp32; p and t are
+ * rounded to the operands' type before they are multiplied (in fp16 a t below 2^-25 is 0: scale the loss as half precision wants it), outputs
+ * and gradients once at the end.  Results repeat bit for bit and do not depend on the other sequences of the call.
+ *
+ * A plan holds what follows from the lengths and heads alone: one for a micro-batch serves every layer's calls, forward and backward, on any
+ * streams at once (calls only read it).  host_lens is consumed before the call returns; dev_mem (spiral_attention_plan_bytes, 0 on bad
+ * arguments; 256-byte aligned) is written by kernels enqueued on `stream` and must stay valid as long as the plan; calls on other streams have to wait for them.
+ * q, out, dout, dq: [n_rows, n_q_heads, head_dim]; k, v, dk, dv: [n_rows, n_kv_heads, head_dim], of `dtype` (SPIRAL_DTYPE_BF16 or _FP16), a
+ * row's heads back to back, rows `stride` elements apart (so that q, k and v may be parts of one fused projection's rows, and their gradients
+ * of one buffer).  Matrices are 16-byte aligned and strides multiples of 8.  dev_lse: fp32 [n_q_heads, n_rows].  The backward call is given out and lse
+ * of the forward call on the same q, k, v.  dev_workspace: spiral_attention_backward_workspace_bytes(plan) bytes, 256-byte aligned,
+ * contents undefined before and after; calls that share it must be ordered on one stream.  What is written may not share an element with another buffer of the call (matrices that lie
+ * in each other's gaps have one stride, other interleavings are refused).
+ * Errors: NOT_LOADED (null plan), INVALID_ARG (null or misaligned pointer, a negative length, no rows, more than 2^31 - 1 of them, unknown type, a stride
+ * less than a row, no multiple of 8 or above 2^22, scale not in [1e-30, 1e30], memory or workspace too small, shared elements), SHAPE (head_dim not in {32, 64, 128},
+ * n_q_heads no multiple of n_kv_heads or above 1,024), HIP. */
+typedef struct spiral_attention_plan spiral_attention_plan;
+size_t spiral_attention_plan_bytes(const int32_t* host_lens, int B, int n_q_heads, int n_kv_heads, int head_dim);
+int    spiral_attention_plan_create(const int32_t* host_lens, int B, int n_q_heads, int n_kv_heads, int head_dim, void* dev_mem, size_t bytes,
+                                    void* stream, spiral_attention_plan** out);
+void   spiral_attention_plan_free(spiral_attention_plan* plan);
+int    spiral_attention_forward(const spiral_attention_plan* plan, const void* dev_q, long long q_stride, const void* dev_k, long long k_stride,
+                                const void* dev_v, long long v_stride, int dtype, float scale, void* dev_out, long long out_stride, float* dev_lse,
+                                void* stream);
+size_t spiral_attention_backward_workspace_bytes(const spiral_attention_plan* plan);
+int    spiral_attention_backward(const spiral_attention_plan* plan, const void* dev_q, long long q_stride, const void* dev_k, long long k_stride,
+                                 const void* dev_v, long long v_stride, const void* dev_out, long long out_stride, const float* dev_lse,
+                                 const void* dev_dout, long long dout_stride, int dtype, float scale, void* dev_dq, long long dq_stride,
+                                 void* dev_dk, long long dk_stride, void* dev_dv, long long dv_stride, void* dev_workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* ---- addition to the residual stream and RMSNorm (learner side) -------------------------------------
+ *     sum = x + residual ,  rstd = (mean_c sum_c^2 + eps)^(-1/2) ,  out_c = gain_c rstd sum_c                a row of d elements each
+ * in fp32; `sum` is rounded where it is written, not before it is normed.  dev_residual NULL: sum = x (dev_sum, where given, is a copy of it).
+ * out_dtype: that of x, or SPIRAL_DTYPE_E4M3: codes under an fp32 scale a row, out = code * dev_out_scale[row], scale = the row's largest |out| / 448
+ * (0, with codes of 0, where that is at most 1e-30), codes rounded to nearest even; a row with a NaN or an infinity has scale NaN and codes NaN.
+ * dev_x, dev_residual, dev_sum, dev_out: [n_rows, d], rows `stride` elements apart, aligned to an element; x, residual and sum of `dtype` (FP32, BF16, FP16).  dev_gain
+ * fp32 [d].  dev_sum, dev_rstd (fp32 [n_rows]) may be NULL; dev_sum may be dev_x or dev_residual itself (same pointer and stride).
+ * Backward, for gradients dout of out and dsum of sum (the residual branch's; NULL: none), with the sum and rstd that the forward call wrote:
+ *     u = rstd sum ,  a = gain dout ,  dx = dsum + rstd (a - u mean_c(a u)) ,  dgain_c = sum_rows dout_c u_c
+ * dx is the gradient of x and of the residual alike; dev_dx may be dev_dsum or dev_dout itself (same pointer and stride).  dev_dgain fp32 [d], or NULL.
+ * Sums are fp32 in a fixed order: results repeat bit for bit.  dev_workspace (spiral_add_rmsnorm_backward_workspace_bytes, 0 for invalid sizes): 256-byte
+ * aligned, contents undefined before and after; calls that share it must be ordered on one stream; may be NULL where dev_dgain is.
+ * Nothing else that is written may share an element with another buffer.
+ * Errors: INVALID_ARG (null or misaligned pointer, n_rows or d < 1, more than 2^31 - 1 rows, d above 2^24, unknown type, a stride < d, a scale without codes or codes
+ * without one, eps not in [0, 1], workspace too small, shared elements), HIP. */
+int    spiral_add_rmsnorm(const void* dev_x, long long x_stride, const void* dev_residual, long long residual_stride, const float* dev_gain, int dtype,
+                          long long n_rows, int d, float eps, void* dev_out, int out_dtype, long long out_stride, float* dev_out_scale,
+                          void* dev_sum, long long sum_stride, float* dev_rstd, void* stream);
+size_t spiral_add_rmsnorm_backward_workspace_bytes(long long n_rows, int d);
+int    spiral_add_rmsnorm_backward(const void* dev_dout, long long dout_stride, const void* dev_sum, long long sum_stride, const float* dev_gain,
+                                   const float* dev_rstd, const void* dev_dsum, long long dsum_stride, int dtype, long long n_rows, int d,
+                                   void* dev_dx, long long dx_stride, float* dev_dgain, void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* ---- norm and rotation of the q and k heads (learner side) --------------------------------------------
+ * What stands between the projections and the attention, on every q and k head of head_dim elements, as the decoder has it:
+ *     n = gain x / sqrt(mean x^2 + eps)   (dev_gain_* NULL: n = x) ,   pair (c, c + head_dim / 2) of n turned by position * theta^(-2c / head_dim)
+ * dev_positions: int32 [n_rows]; angles are evaluated in 64 bits.  dev_q [n_rows, n_q_heads, head_dim], dev_k [n_rows, n_kv_heads, head_dim] and the outputs, of `dtype`
+ * (FP32, BF16, FP16), a row's heads back to back, rows `stride` elements apart, aligned to an element; an output may be its input itself (same pointer and stride).
+ * Backward, for gradients of the outputs and the q and k that the forward call was given (not read, and may be NULL, where the gain is NULL):
+ * those of q and k, and of the gains (fp32 [head_dim], sums over rows and heads; dev_dgain_* NULL with the gain, or where they are not wanted); a gradient of an input may be
+ * that of the output itself (same pointer and stride).  Sums are fp32 in a fixed order.  dev_workspace: as above; may be NULL without gradients of gains.
+ * Errors: INVALID_ARG (null or misaligned pointer, n_rows < 1, more than 2^31 - 1 rows, a gradient of a gain without the gain, unknown type, a stride less than a
+ * row, eps not in [0, 1], theta not in [1, 1e30], workspace too small, shared elements), SHAPE (head_dim not in {32, 64, 128}, heads < 1 or above 1,024), HIP. */
+int    spiral_norm_rope(const void* dev_q, long long q_stride, const void* dev_k, long long k_stride, const float* dev_gain_q, const float* dev_gain_k,
+                        int dtype, long long n_rows, int n_q_heads, int n_kv_heads, int head_dim, float eps, double theta, const int32_t* dev_positions,
+                        void* dev_out_q, long long out_q_stride, void* dev_out_k, long long out_k_stride, void* stream);
+size_t spiral_norm_rope_backward_workspace_bytes(long long n_rows, int n_q_heads, int n_kv_heads, int head_dim);
+int    spiral_norm_rope_backward(const void* dev_q, long long q_stride, const void* dev_k, long long k_stride, const void* dev_dout_q, long long dout_q_stride,
+                                 const void* dev_dout_k, long long dout_k_stride, const float* dev_gain_q, const float* dev_gain_k, int dtype,
+                                 long long n_rows, int n_q_heads, int n_kv_heads, int head_dim, float eps, double theta, const int32_t* dev_positions,
+                                 void* dev_dq, long long dq_stride, void* dev_dk, long long dk_stride, float* dev_dgain_q, float* dev_dgain_k,
+                                 void* dev_workspace, size_t workspace_bytes, void* stream);
 
 /* ---- AdamW (learner side) --------------------------------------------------------------------------
  * One step over all tensors of a model at once, e.g. the weights that spiral_model_load was given (a repacked model is repacked

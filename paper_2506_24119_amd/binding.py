@@ -38,6 +38,9 @@ EXPORTS = [
     "spiral_decode_step_static", "spiral_static_workspace_bytes", "spiral_probe_stream_read",
     "spiral_sample_truncated_ws", "spiral_sample_truncated_workspace_bytes",
     "spiral_sample_uniform", "spiral_sample_uniform_workspace_bytes", "spiral_policy_gradient", "spiral_policy_gradient_workspace_bytes",
+    "spiral_attention_plan_bytes", "spiral_attention_plan_create", "spiral_attention_plan_free", "spiral_attention_forward", "spiral_attention_backward_workspace_bytes",
+    "spiral_attention_backward", "spiral_add_rmsnorm", "spiral_add_rmsnorm_backward_workspace_bytes", "spiral_add_rmsnorm_backward",
+    "spiral_norm_rope", "spiral_norm_rope_backward_workspace_bytes", "spiral_norm_rope_backward",
     "spiral_adamw_bytes", "spiral_adamw_create", "spiral_adamw_check_grads", "spiral_adamw_set_grads", "spiral_adamw_step", "spiral_adamw_free",
 ]
 
@@ -152,6 +155,31 @@ def load_library(path: Optional[str] = None):
     lib.spiral_policy_gradient.restype = C.c_int
     lib.spiral_policy_gradient.argtypes = [vp, C.c_int, C.c_longlong, C.c_longlong, C.c_int, vp, vp, vp, vp, C.c_float, C.c_float, C.c_float, vp,
                                            vp, C.c_longlong, vp, C.c_size_t, vp]
+    ll, ci, cf, sz = C.c_longlong, C.c_int, C.c_float, C.c_size_t
+    lib.spiral_attention_plan_bytes.restype = sz
+    lib.spiral_attention_plan_bytes.argtypes = [i32p, ci, ci, ci, ci]
+    lib.spiral_attention_plan_create.restype = ci
+    lib.spiral_attention_plan_create.argtypes = [i32p, ci, ci, ci, ci, vp, sz, vp, C.POINTER(vp)]
+    lib.spiral_attention_plan_free.restype = None
+    lib.spiral_attention_plan_free.argtypes = [vp]
+    lib.spiral_attention_forward.restype = ci
+    lib.spiral_attention_forward.argtypes = [vp, vp, ll, vp, ll, vp, ll, ci, cf, vp, ll, vp, vp]
+    lib.spiral_attention_backward_workspace_bytes.restype = sz
+    lib.spiral_attention_backward_workspace_bytes.argtypes = [vp]
+    lib.spiral_attention_backward.restype = ci
+    lib.spiral_attention_backward.argtypes = [vp, vp, ll, vp, ll, vp, ll, vp, ll, vp, vp, ll, ci, cf, vp, ll, vp, ll, vp, ll, vp, sz, vp]
+    lib.spiral_add_rmsnorm.restype = ci
+    lib.spiral_add_rmsnorm.argtypes = [vp, ll, vp, ll, vp, ci, ll, ci, cf, vp, ci, ll, vp, vp, ll, vp, vp]
+    lib.spiral_add_rmsnorm_backward_workspace_bytes.restype = sz
+    lib.spiral_add_rmsnorm_backward_workspace_bytes.argtypes = [ll, ci]
+    lib.spiral_add_rmsnorm_backward.restype = ci
+    lib.spiral_add_rmsnorm_backward.argtypes = [vp, ll, vp, ll, vp, vp, vp, ll, ci, ll, ci, vp, ll, vp, vp, sz, vp]
+    lib.spiral_norm_rope.restype = ci
+    lib.spiral_norm_rope.argtypes = [vp, ll, vp, ll, vp, vp, ci, ll, ci, ci, ci, cf, C.c_double, vp, vp, ll, vp, ll, vp]
+    lib.spiral_norm_rope_backward_workspace_bytes.restype = sz
+    lib.spiral_norm_rope_backward_workspace_bytes.argtypes = [ll, ci, ci, ci]
+    lib.spiral_norm_rope_backward.restype = ci
+    lib.spiral_norm_rope_backward.argtypes = [vp, ll, vp, ll, vp, ll, vp, ll, vp, vp, ci, ll, ci, ci, ci, cf, C.c_double, vp, vp, ll, vp, ll, vp, vp, vp, sz, vp]
     lib.spiral_adamw_bytes.restype = C.c_size_t
     lib.spiral_adamw_bytes.argtypes = [C.c_int]
     lib.spiral_adamw_create.restype = C.c_int
@@ -544,6 +572,142 @@ def spiral_adamw_step(opt: int, lr: float, beta1: float, beta2: float, eps: floa
 def spiral_adamw_free(opt: int):
     _adamw_grads.pop(opt, None)
     load_library().spiral_adamw_free(opt)
+
+
+# ------------------------------------------------------------------------- the learner's operators between matrix products
+_plans = {}                      # of every plan: rows, query heads, kv heads, head_dim, which the library's calls take on trust
+
+
+def _heads_of(t, shape, dtype, what: str):
+    """(address, row stride) of [rows, heads, head_dim] with a row's heads back to back, of the given shape and type."""
+    if t.dtype is not dtype or tuple(t.shape) != shape or (shape[2] > 1 and t.stride(2) != 1) or (shape[1] > 1 and t.stride(1) != shape[2]):
+        raise ValueError(f"{what}: {shape} of {dtype} with heads back to back is needed, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _matrix_of(t, n: int, d: int, dtype, what: str):
+    """(address, row stride) of [n, d] with contiguous rows, of the given type; None stays None."""
+    if t is None:
+        return None, 0
+    rows, cols, stride = _rows_of(t, what)
+    if (rows, cols) != (n, d) or t.dtype is not dtype:
+        raise ValueError(f"{what}: {n} x {d} of {dtype} is needed, got {rows} x {cols} of {t.dtype}")
+    return t.data_ptr(), stride
+
+
+def _room(t):
+    """(address, bytes) of a workspace; None: none."""
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+
+
+def spiral_attention_plan_bytes(lens, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    a = _i32(lens)
+    return int(load_library().spiral_attention_plan_bytes(_ip(a), a.size, n_q_heads, n_kv_heads, head_dim))
+
+
+def spiral_attention_plan_create(lens, n_q_heads: int, n_kv_heads: int, head_dim: int, dev_mem, stream=None) -> int:
+    """lens: the sequences' lengths.  dev_mem stays the caller's and has to outlive the plan."""
+    a = _i32(lens)
+    out = C.c_void_p()
+    _check(load_library().spiral_attention_plan_create(_ip(a), a.size, n_q_heads, n_kv_heads, head_dim, *_room(dev_mem), _stream_handle(stream), C.byref(out)))
+    _plans[out.value] = (int(a.sum(dtype=np.int64)), n_q_heads, n_kv_heads, head_dim)
+    return out.value
+
+
+def spiral_attention_plan_free(plan: int):
+    _plans.pop(plan, None)
+    load_library().spiral_attention_plan_free(plan)
+
+
+def _plan_of(plan):
+    p = _plans.get(plan)
+    if p is None:
+        raise ValueError("attention: no plan that spiral_attention_plan_create made, or one that is freed")
+    return p
+
+
+def spiral_attention_forward(plan: int, dev_q, dev_k, dev_v, scale: float, dev_out, dev_lse, stream=None):
+    """dev_q, dev_out: [n, q heads, head_dim], dev_k, dev_v: [n, kv heads, head_dim] of bf16 or fp16, heads back to back in a row; dev_lse: fp32 [q heads, n].
+    Rows behind the plan's are left out by the caller: n is the plan's."""
+    n, hq, hkv, hd = _plan_of(plan)
+    t = dev_q.dtype
+    _check(load_library().spiral_attention_forward(plan, *_heads_of(dev_q, (n, hq, hd), t, "q"), *_heads_of(dev_k, (n, hkv, hd), t, "k"),
+                                                   *_heads_of(dev_v, (n, hkv, hd), t, "v"), _dtype(dev_q), scale, *_heads_of(dev_out, (n, hq, hd), t, "out"),
+                                                   _vector(dev_lse, hq * n, "float32", "lse"), _stream_handle(stream)))
+
+
+def spiral_attention_backward_workspace_bytes(plan: int) -> int:
+    _plan_of(plan)
+    return int(load_library().spiral_attention_backward_workspace_bytes(plan))
+
+
+def spiral_attention_backward(plan: int, dev_q, dev_k, dev_v, dev_out, dev_lse, dev_dout, scale: float, dev_dq, dev_dk, dev_dv, dev_workspace, stream=None):
+    """The forward call's tensors, the output's gradient, and where those of q, k and v go (shaped like them)."""
+    n, hq, hkv, hd = _plan_of(plan)
+    t = dev_q.dtype
+    q, kv = (n, hq, hd), (n, hkv, hd)
+    _check(load_library().spiral_attention_backward(plan, *_heads_of(dev_q, q, t, "q"), *_heads_of(dev_k, kv, t, "k"), *_heads_of(dev_v, kv, t, "v"),
+                                                    *_heads_of(dev_out, q, t, "out"), _vector(dev_lse, hq * n, "float32", "lse"),
+                                                    *_heads_of(dev_dout, q, t, "dout"), _dtype(dev_q), scale, *_heads_of(dev_dq, q, t, "dq"),
+                                                    *_heads_of(dev_dk, kv, t, "dk"), *_heads_of(dev_dv, kv, t, "dv"), *_room(dev_workspace), _stream_handle(stream)))
+
+
+def spiral_add_rmsnorm(dev_x, dev_residual, dev_gain, eps: float, dev_out, dev_out_scale=None, dev_sum=None, dev_rstd=None, stream=None):
+    """dev_x: [n, d] fp32, bf16 or fp16; dev_residual and dev_sum of its type, or None; dev_out of its type, or float8_e4m3fn with dev_out_scale."""
+    n, d, stride = _rows_of(dev_x, "x")
+    t = dev_x.dtype
+    code = _dtype(dev_out)
+    out, out_stride = _matrix_of(dev_out, n, d, dev_out.dtype if code == SPIRAL_DTYPE_E4M3 else t, "out")
+    res, res_stride = _matrix_of(dev_residual, n, d, t, "residual")
+    total, sum_stride = _matrix_of(dev_sum, n, d, t, "sum")
+    _check(load_library().spiral_add_rmsnorm(dev_x.data_ptr(), stride, res, res_stride, _vector(dev_gain, d, "float32", "gain"), _dtype(dev_x), n, d, eps,
+                                             out, code, out_stride, _vector(dev_out_scale, n, "float32", "scale"), total, sum_stride,
+                                             _vector(dev_rstd, n, "float32", "rstd"), _stream_handle(stream)))
+
+
+def spiral_add_rmsnorm_backward_workspace_bytes(n_rows: int, d: int) -> int:
+    return int(load_library().spiral_add_rmsnorm_backward_workspace_bytes(n_rows, d))
+
+
+def spiral_add_rmsnorm_backward(dev_dout, dev_sum, dev_gain, dev_rstd, dev_dsum, dev_dx, dev_dgain, dev_workspace, stream=None):
+    """dev_dout, dev_sum, dev_dsum (or None) and dev_dx: [n, d] of one type; dev_dgain: fp32 [d] or None."""
+    n, d, stride = _rows_of(dev_sum, "sum")
+    t = dev_sum.dtype
+    dout, dout_stride = _matrix_of(dev_dout, n, d, t, "dout")
+    dsum, dsum_stride = _matrix_of(dev_dsum, n, d, t, "dsum")
+    dx, dx_stride = _matrix_of(dev_dx, n, d, t, "dx")
+    _check(load_library().spiral_add_rmsnorm_backward(dout, dout_stride, dev_sum.data_ptr(), stride, _vector(dev_gain, d, "float32", "gain"),
+                                                      _vector(dev_rstd, n, "float32", "rstd"), dsum, dsum_stride, _dtype(dev_sum), n, d, dx, dx_stride,
+                                                      _vector(dev_dgain, d, "float32", "gain's gradient"), *_room(dev_workspace), _stream_handle(stream)))
+
+
+def spiral_norm_rope(dev_q, dev_k, dev_gain_q, dev_gain_k, eps: float, theta: float, dev_positions, dev_out_q, dev_out_k, stream=None):
+    """dev_q: [n, q heads, head_dim], dev_k: [n, kv heads, head_dim] of one type; the gains fp32 [head_dim] or None; the outputs shaped like the inputs, or these themselves."""
+    n, hq, hd = dev_q.shape
+    q, kv, t = (n, hq, hd), (n, dev_k.shape[1], hd), dev_q.dtype
+    _check(load_library().spiral_norm_rope(*_heads_of(dev_q, q, t, "q"), *_heads_of(dev_k, kv, t, "k"), _vector(dev_gain_q, hd, "float32", "q's gain"),
+                                           _vector(dev_gain_k, hd, "float32", "k's gain"), _dtype(dev_q), n, hq, kv[1], hd, eps, theta,
+                                           _vector(dev_positions, n, "int32", "positions"), *_heads_of(dev_out_q, q, t, "q's output"),
+                                           *_heads_of(dev_out_k, kv, t, "k's output"), _stream_handle(stream)))
+
+
+def spiral_norm_rope_backward_workspace_bytes(n_rows: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(load_library().spiral_norm_rope_backward_workspace_bytes(n_rows, n_q_heads, n_kv_heads, head_dim))
+
+
+def spiral_norm_rope_backward(dev_q, dev_k, dev_dout_q, dev_dout_k, dev_gain_q, dev_gain_k, eps: float, theta: float, dev_positions, dev_dq, dev_dk,
+                              dev_dgain_q, dev_dgain_k, dev_workspace, stream=None):
+    """dev_q and dev_k as the forward call was given them (None where there is no gain); the gradients of its outputs, of its inputs and of the gains (None: not wanted)."""
+    n, hq, hd = dev_dout_q.shape
+    q, kv, t = (n, hq, hd), (n, dev_dout_k.shape[1], hd), dev_dout_q.dtype
+    none = (None, 0)
+    _check(load_library().spiral_norm_rope_backward(*(none if dev_q is None else _heads_of(dev_q, q, t, "q")), *(none if dev_k is None else _heads_of(dev_k, kv, t, "k")),
+                                                    *_heads_of(dev_dout_q, q, t, "gradient of q's output"), *_heads_of(dev_dout_k, kv, t, "gradient of k's output"),
+                                                    _vector(dev_gain_q, hd, "float32", "q's gain"), _vector(dev_gain_k, hd, "float32", "k's gain"),
+                                                    _dtype(dev_dout_q), n, hq, kv[1], hd, eps, theta, _vector(dev_positions, n, "int32", "positions"),
+                                                    *_heads_of(dev_dq, q, t, "q's gradient"), *_heads_of(dev_dk, kv, t, "k's gradient"),
+                                                    _vector(dev_dgain_q, hd, "float32", "gradient of q's gain"), _vector(dev_dgain_k, hd, "float32", "gradient of k's gain"),
+                                                    *_room(dev_workspace), _stream_handle(stream)))
 
 
 # ------------------------------------------------------------------------- RAE (host only)

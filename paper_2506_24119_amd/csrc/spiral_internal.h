@@ -252,6 +252,63 @@ int policy_grad_slices(long long n_rows, int V, int dtype);      // workgroups o
 size_t policy_grad_workspace_bytes(long long n_rows, int V);
 hipError_t launch_policy_grad(const GradArgs& a, int dtype, void* workspace, hipStream_t s);
 
+// the learner's attention over packed sequences
+struct PackArgs {
+    const void *q, *k, *v, *out_in, *dout;    // out_in, dout: backward only
+    void *out, *dq, *dk, *dv;
+    long long q_stride, k_stride, v_stride, out_stride, dout_stride, dq_stride, dk_stride, dv_stride;      // elements
+    float* lse;                               // [Hq][n_rows]
+    float* delta;                             // [Hq][n_rows]: dout . out
+    const int32_t* starts;                    // [n_seqs + 1] first rows
+    long long n_rows;
+    int32_t n_seqs, n_q_heads, n_kv_heads;
+    float scale, scale_log2e;
+};
+hipError_t launch_pack_forward(const PackArgs& a, int dtype, int hd, hipStream_t s);
+hipError_t launch_pack_backward(const PackArgs& a, int dtype, int hd, hipStream_t s);
+
+// addition and RMSNorm
+struct NormRowsArgs {
+    const void *x, *residual; long long x_stride, residual_stride;
+    const float* gain;
+    long long n_rows;
+    int32_t d, out_dtype;
+    float eps;
+    void *out, *sum; long long out_stride, sum_stride;      // sum: or null
+    float *out_scale, *rstd;                  // or null
+};
+struct NormGradArgs {
+    const void *dout, *sum, *dsum; long long dout_stride, sum_stride, dsum_stride;       // dsum: or null
+    const float *gain, *rstd;
+    long long n_rows;
+    int32_t d;
+    void* dx; long long dx_stride;
+    float* dgain;                             // or null
+    float* part;                              // workspace
+};
+hipError_t launch_add_norm_rows(const NormRowsArgs& a, int dtype, hipStream_t s);
+size_t norm_grad_workspace_bytes(long long n_rows, int d);
+hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, hipStream_t s);
+
+// norm and rotation of heads: q and k as two sides of one call
+struct RopeSide {
+    const void *x, *dout; void* out;          // forward: x -> out; backward: dout (and x) -> out
+    long long x_stride, dout_stride, out_stride;
+    const float* gain;                        // or null
+    float* dgain;                             // or null
+    int32_t heads;
+};
+struct RopeArgs {
+    RopeSide side[2];
+    long long n_rows;
+    const int32_t* positions;
+    float eps;
+    float* part;                              // backward: partial sums of the gains' gradients
+};
+hipError_t launch_norm_rope(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, hipStream_t s);
+size_t norm_rope_grad_workspace_bytes(long long n_rows, int n_heads, int hd);
+hipError_t launch_norm_rope_grad(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, hipStream_t s);
+
 // AdamW over many tensors
 constexpr int kAdamwBlock = SPIRAL_ADAMW_BLOCK;
 constexpr int kAdamwParts = 2048;             // workgroups, and partial sums of the norm, at most

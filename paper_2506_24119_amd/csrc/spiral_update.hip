@@ -1,41 +1,12 @@
 // Host side of what closes a policy update: the draw from given numbers, the gradient of the objective, the optimiser's step.
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
-#include <cstring>
 #include <memory>
 #include <new>
 
-#include "spiral_internal.h"
+#include "host_checks.h"
 
 using namespace spiral;
-
-static int fail(int code, const char* fmt, ...) {
-    char text[384];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(text, sizeof(text), fmt, ap);
-    va_end(ap);
-    return spiral_set_error(code, text);
-}
-static int done(hipError_t e, const char* who) { return e == hipSuccess ? SPIRAL_OK : fail(SPIRAL_ERR_HIP, "%s: %s", who, hipGetErrorString(e)); }
-
-static int dtype_size(int dtype) {          // of logits, parameters and gradients; 0: none of them
-    return dtype == SPIRAL_DTYPE_FP32 ? 4 : dtype == SPIRAL_DTYPE_BF16 || dtype == SPIRAL_DTYPE_FP16 ? 2 : 0;
-}
-static bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-
-// Of a call's buffers none that is written may be another one too: workgroups would read what others have already written.
-struct Span { uintptr_t lo, hi; bool written; };
-static Span span_of(const void* p, size_t bytes, bool written) { return {(uintptr_t)p, (uintptr_t)p + (p ? bytes : 0), written}; }
-static uintptr_t matrix_bytes(long long rows, long long stride, int V, int size) { return ((uintptr_t)(rows - 1) * stride + V) * size; }
-static bool any_overlap(const Span* s, int n) {
-    for (int i = 0; i < n; ++i)
-        for (int j = 0; j < i; ++j)
-            if ((s[i].written || s[j].written) && s[i].lo < s[j].hi && s[j].lo < s[i].hi) return true;
-    return false;
-}
 
 // ---------------------------------------------------------------------------------------------
 // draw
