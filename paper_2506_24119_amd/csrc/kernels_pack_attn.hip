@@ -2,6 +2,8 @@
 //
 // A row alone: one wave computes one (row, head) of the outputs, of dq, or of dk and dv, token by token, and reads nothing that
 // the row does not see.  All sums are fp32.
+#include <type_traits>
+
 #include "spiral_internal.h"
 
 namespace spiral {
@@ -29,16 +31,6 @@ __device__ __forceinline__ float wave_most(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return v;
-}
-
-// the sequence of a row: the last that starts at or before it and is not empty
-__device__ __forceinline__ int sequence_of(const PackArgs& a, int row) {
-    int lo = 0, hi = a.n_seqs;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.starts[mid] <= row) lo = mid; else hi = mid;
-    }
-    return lo;
 }
 
 // A lane holds dimensions lane and lane + 64 (HD = 32: the upper half of the wave repeats the lower)
@@ -96,15 +88,14 @@ __device__ void dq_row(const PackArgs& a, const T* k, const T* v, const T* q, co
         if (lane + 64 * j < HD) dq[lane + 64 * j] = (T)(g[j] * a.scale);
 }
 
-// dk and dv of one token and kv head; row0: the sequence's first row, len: its length, t: the token's position
-template <class T, int HD>
-__device__ void dkv_row(const PackArgs& a, int row0, int len, int t, int kvh, int lane) {
+// dk and dv of one token and kv head from the query heads h0 .. h1 - 1, or their part of them; row0: the sequence's first row, len: its length, t: the token's position
+template <class T, int HD, bool PARTS>
+__device__ void dkv_row(const PackArgs& a, int row0, int len, int t, int kvh, int h0, int h1, int part, int lane) {
     constexpr int DL = kDims<HD>;
-    const int G = a.n_q_heads / a.n_kv_heads;
     const T* k = (const T*)a.k + (size_t)(row0 + t) * a.k_stride + kvh * HD;
     const T* v = (const T*)a.v + (size_t)(row0 + t) * a.v_stride + kvh * HD;
     float gk[DL] = {}, gv[DL] = {};
-    for (int h = kvh * G; h < (kvh + 1) * G; ++h) {
+    for (int h = h0; h < h1; ++h) {
         const T* q = (const T*)a.q + (size_t)row0 * a.q_stride + h * HD;
         const T* dout = (const T*)a.dout + (size_t)row0 * a.dout_stride + h * HD;
         const float* lse = a.lse + (size_t)h * a.n_rows + row0;
@@ -128,58 +119,496 @@ __device__ void dkv_row(const PackArgs& a, int row0, int len, int t, int kvh, in
             }
         }
     }
+    const size_t width = (size_t)a.n_kv_heads * HD, plane = (size_t)a.n_rows * width;
+    float* to = PARTS ? a.part + (size_t)part * 2 * plane + (size_t)(row0 + t) * width + kvh * HD : nullptr;
     T* dk = (T*)a.dk + (size_t)(row0 + t) * a.dk_stride + kvh * HD;
     T* dv = (T*)a.dv + (size_t)(row0 + t) * a.dv_stride + kvh * HD;
 #pragma unroll
-    for (int j = 0; j < DL; ++j)
-        if (lane + 64 * j < HD) {
-            dk[lane + 64 * j] = (T)(gk[j] * a.scale);
-            dv[lane + 64 * j] = (T)gv[j];
+    for (int j = 0; j < DL; ++j) {
+        const int d = lane + 64 * j;
+        if (d >= HD) continue;
+        if (PARTS) to[d] = gk[j], to[plane + d] = gv[j];
+        else dk[d] = (T)(gk[j] * a.scale), dv[d] = (T)gv[j];
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Tiles of 64 rows of one head in LDS, row-major, brought there by loads that write LDS themselves.  A row's 16-byte pieces are permuted so that
+// neither kind of read meets a bank twice: 8 lanes that read one piece of 8 consecutive rows, and the transposing read, in which 16 lanes
+// read 32 bytes of four consecutive rows each.
+template <int HD> struct Tile {
+    static constexpr int ROW = HD * 2, PIECES = HD / 8, BYTES = 64 * ROW, LOADS = BYTES / 4096;        // LOADS: of 1 KB, a wave of four
+    static __device__ __forceinline__ int swizzle(int row) {
+        return HD == 32 ? (row & 2) | ((row >> 2) & 1) : ((row & 3) << 1) | ((row >> 2) & 1);
+    }
+};
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <class T> __device__ __forceinline__ f32x16 mma(const u32x4& x, const u32x4& y, const f32x16& c) {
+    if constexpr (std::is_same_v<T, __bf16>) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Vec8<__bf16>, x), __builtin_bit_cast(Vec8<__bf16>, y), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Vec8<_Float16>, x), __builtin_bit_cast(Vec8<_Float16>, y), c, 0, 0, 0);
+}
+template <class T> __device__ __forceinline__ uint32_t pack2(float x, float y) {            // rounded to nearest
+    typedef T Pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, Pair{(T)x, (T)y});
+}
+__device__ __forceinline__ f32x16 zeros() {
+    f32x16 z;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = 0.f;
+    return z;
+}
+
+// 64 lanes x 16 bytes straight to 1 KB of LDS at `to` (wave-uniform); what lies beyond the buffer's end comes as zeros
+__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char* to, uint32_t off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, off, 0, 0, 0);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_upto(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
+}
+
+// What a wave brings of a tile: the lane's offsets from the tile's first row.  Rows past the sequence's end come as zeros: the buffer descriptor ends there.
+template <int HD> struct Bring {
+    uint32_t off[Tile<HD>::LOADS];
+    uint32_t row_bytes;
+    __device__ __forceinline__ Bring(long long stride, int wave, int lane) : row_bytes((uint32_t)stride * 2u) {
+#pragma unroll
+        for (int u = 0; u < Tile<HD>::LOADS; ++u) {
+            const int at = (wave * Tile<HD>::LOADS + u) * 64 + lane, row = at / Tile<HD>::PIECES, piece = at % Tile<HD>::PIECES;
+            off[u] = row * row_bytes + ((piece ^ Tile<HD>::swizzle(row)) * 16);
         }
+    }
+    // first: the tile's first row, of `rows` that are there
+    __device__ __forceinline__ void operator()(const void* first, int rows, char* lds, int wave) const {
+        const __amdgpu_buffer_rsrc_t r = buffer_upto(first, (uint32_t)max(0, min(rows, 64)) * row_bytes);
+#pragma unroll
+        for (int u = 0; u < Tile<HD>::LOADS; ++u) to_lds(r, lds + (wave * Tile<HD>::LOADS + u) * 1024, off[u]);
+    }
+};
+
+// A matrix operand's lane holds a row (l32 of 32) and eight of 16 contracted elements (the half that lh says).
+// By rows: the contraction runs along the row.  Transposed: operand rows are dimensions, the contraction runs over the tile's rows, of 16 in the order
+// 4 lh .. + 3, 8 + 4 lh .. + 3: that in which a product's result leaves them.
+template <int HD> struct Reads {
+    int row, col;                             // of a lane: offset of its row's piece 0 or 1, of its transposed corner
+    __device__ __forceinline__ Reads(int lane) {
+        const int l32 = lane & 31, lh = lane >> 5, i = lane & 15, r = 4 * lh + (i >> 2);
+        row = l32 * Tile<HD>::ROW + ((lh ^ Tile<HD>::swizzle(l32)) * 16);
+        col = r * Tile<HD>::ROW + (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ Tile<HD>::swizzle(r)) * 16) + (i & 1) * 8;
+    }
+    // rows 32 half .. + 31, elements 16 ks .. + 15
+    __device__ __forceinline__ u32x4 by_row(const char* tile, int half, int ks) const {
+        return *(const u32x4*)(tile + ((row ^ ((ks & 3) * 32)) + (ks >> 2) * 128 + half * 32 * Tile<HD>::ROW));
+    }
+    // dimensions 32 dt .. + 31, rows 16 group .. + 15
+    __device__ __forceinline__ u32x4 transposed(const char* tile, int group, int dt) const {
+        typedef __attribute__((address_space(3))) s16x4 Corner;
+        const char* p = tile + ((col ^ ((dt & 1) * 64)) + (dt >> 1) * 128 + group * 16 * Tile<HD>::ROW);
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Corner*)p));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Corner*)(p + 8 * Tile<HD>::ROW)));
+        return u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+};
+
+// 32 rows of a head in registers, as a matrix operand: row l32 (zeros where `there` is false), elements 16 ks + 8 lh .. + 7
+template <int HD> __device__ __forceinline__ void hold(u32x4 (&f)[HD / 16], const void* row, bool there, int lh) {
+#pragma unroll
+    for (int ks = 0; ks < HD / 16; ++ks) {
+        const u32x4 v = *(const u32x4*)((const char*)row + ks * 32 + lh * 16);
+        f[ks] = there ? v : u32x4{0u, 0u, 0u, 0u};
+    }
+}
+
+// Writes 32 rows of results whose transpose the wave holds (lane: row l32; registers 4b .. 4b + 3 of tile dt: dimensions 32 dt + 8 b + 4 lh .. + 3), each times its
+// row's factor, through a private part of LDS, so that whole rows leave.
+template <class T, int HD>
+__device__ __forceinline__ void put_rows(const f32x16 (&acc)[HD / 32], float factor, char* lds, T* first, long long stride, int n_valid, int lane) {
+    constexpr int ROW = HD * 2 + 16;          // bytes between rows: 16 lanes that write 8 bytes of 16 rows each
+    const int l32 = lane & 31, lh = lane >> 5;
+#pragma unroll
+    for (int dt = 0; dt < HD / 32; ++dt)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            *(u32x2*)(lds + l32 * ROW + (dt * 32 + b * 8 + lh * 4) * 2) = u32x2{pack2<T>(acc[dt][4 * b] * factor, acc[dt][4 * b + 1] * factor),
+                                                                            pack2<T>(acc[dt][4 * b + 2] * factor, acc[dt][4 * b + 3] * factor)};
+    __builtin_amdgcn_wave_barrier();
+    constexpr int LANES = HD / 8;             // of a row
+#pragma unroll
+    for (int u = 0; u < 32 * LANES / 64; ++u) {
+        const int row = u * (64 / LANES) + lane / LANES, piece = lane % LANES;
+        const u32x4 v = *(const u32x4*)(lds + row * ROW + piece * 16);
+        if (row < n_valid) *(u32x4*)(first + (size_t)row * stride + piece * 8) = v;
+    }
+}
+template <int HD> constexpr int kPutBytes = 32 * (HD * 2 + 16);
+
+template <int N> __device__ __forceinline__ bool any_undefined(const f32x16 (&acc)[N]) {
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) bad = bad || acc[t][r] != acc[t][r];
+    return bad;
+}
+
+// A workgroup's place: four units of a (sequence, kv head), a unit being 32 positions of one query head; units are counted heads first.
+struct Unit {
+    int row0, len, kvh, h, pos0, n_valid, stages, my_stages;
+    bool active;
+    __device__ __forceinline__ Unit(const PackArgs& a, int wave) {
+        const int4 it = a.q_items[a.first_item + blockIdx.y];
+        const int G = a.n_q_heads / a.n_kv_heads;
+        row0 = it.x; len = it.y; kvh = blockIdx.x;
+        const int tiles = (len + 31) >> 5, u = it.z * 4 + wave, tile = u / G, last = min(it.z * 4 + 3, tiles * G - 1) / G;
+        active = tile < tiles;
+        h = kvh * G + (active ? u - tile * G : 0);
+        pos0 = active ? tile * 32 : 0;
+        n_valid = active ? min(32, len - pos0) : 0;
+        stages = (min(len, last * 32 + 32) + 63) >> 6;
+        my_stages = active ? (pos0 + n_valid + 63) >> 6 : 0;
+    }
+};
+
+template <class T, int HD>
+__global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD>::BYTES;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * TB > 4 * kPutBytes<HD> ? 4 * TB : 4 * kPutBytes<HD>];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
+    const Unit w(a, wave);
+    const T* k = (const T*)a.k + (size_t)w.row0 * a.k_stride + w.kvh * HD;
+    const T* v = (const T*)a.v + (size_t)w.row0 * a.v_stride + w.kvh * HD;
+    const Bring<HD> bring_k(a.k_stride, wave, lane), bring_v(a.v_stride, wave, lane);
+    const Reads<HD> at(lane);
+    auto bring = [&](int st) {
+        char* to = lds + (st & 1) * 2 * TB;
+        bring_k(k + (size_t)st * 64 * a.k_stride, w.len - st * 64, to, wave);
+        bring_v(v + (size_t)st * 64 * a.v_stride, w.len - st * 64, to + TB, wave);
+    };
+    bring(0);
+    const bool there = l32 < w.n_valid;
+    const size_t my_row = (size_t)w.row0 + (there ? w.pos0 + l32 : 0);
+    u32x4 qf[KS];
+    hold<HD>(qf, (const T*)a.q + my_row * a.q_stride + w.h * HD, there, lh);
+    f32x16 acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = zeros();
+    float m = kLeast, l = 0.f;
+    const int limit = w.pos0 + l32;
+
+    for (int st = 0; st < w.stages; ++st) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (st + 1 < w.stages) bring(st + 1);
+        if (st >= w.my_stages) continue;
+        const char* kt = lds + (st & 1) * 2 * TB;
+        const char* vt = kt + TB;
+        f32x16 s[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            s[half] = zeros();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s[half] = mma<T>(at.by_row(kt, half, ks), qf[ks], s[half]);
+        }
+        if (st * 64 + 63 > w.pos0) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (st * 64 + half * 32 + 8 * (r >> 2) + 4 * lh + (r & 3) > limit) s[half][r] = -INFINITY;
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[half][r]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.scale_log2e;
+        if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {          // the reference moves only where weights would pass 2^8
+            const float m_new = fmaxf(m, mx), shrink = __builtin_amdgcn_exp2f(m - m_new);
+            l *= shrink;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[d][r] *= shrink;
+            m = m_new;
+        }
+        u32x4 p[4];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[half][r], a.scale_log2e, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[half][r + 1], a.scale_log2e, -m));
+                l += x + y;
+                p[half * 2 + (r >> 3)][(r >> 1) & 3] = pack2<T>(x, y);
+            }
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] = mma<T>(at.transposed(vt, g, d), p[g], acc[d]);
+    }
+    __syncthreads();                              // the last tiles have been read
+    if (!w.active) return;
+    l += __shfl_xor(l, 32, 64);
+    T* out = (T*)a.out + ((size_t)w.row0 + w.pos0) * a.out_stride + w.h * HD;
+    float* lse = a.lse + (size_t)w.h * a.n_rows + w.row0 + w.pos0;
+    put_rows<T, HD>(acc, 1.f / l, lds + wave * kPutBytes<HD>, out, a.out_stride, w.n_valid, lane);
+    if (lh == 0 && there) lse[l32] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+    const bool bad = there && (any_undefined(acc) || l != l);
+    uint64_t rows = __builtin_amdgcn_ballot_w64(bad);
+    rows = (rows | (rows >> 32)) & 0xFFFFFFFFull;
+    while (rows) {                                // 0 times an undefined value of a row that is not seen
+        const int r = __builtin_ctzll(rows);
+        rows &= rows - 1;
+        forward_row<T, HD>(a, k, v, (const T*)a.q + ((size_t)w.row0 + w.pos0 + r) * a.q_stride + w.h * HD, w.pos0 + r, out + (size_t)r * a.out_stride, lse + r, lane);
+    }
 }
 
 template <class T, int HD>
-__global__ __launch_bounds__(256) void pack_forward_kernel(PackArgs a) {
-    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
-    if (row >= a.n_rows) return;
-    const int first = a.starts[sequence_of(a, row)], kvh = h / (a.n_q_heads / a.n_kv_heads);
-    forward_row<T, HD>(a, (const T*)a.k + (size_t)first * a.k_stride + kvh * HD, (const T*)a.v + (size_t)first * a.v_stride + kvh * HD,
-                       (const T*)a.q + (size_t)row * a.q_stride + h * HD, row - first, (T*)a.out + (size_t)row * a.out_stride + h * HD,
-                       a.lse + (size_t)h * a.n_rows + row, lane);
+__global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD>::BYTES;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * TB > 4 * kPutBytes<HD> ? 4 * TB : 4 * kPutBytes<HD>];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
+    const Unit w(a, wave);
+    const T* k = (const T*)a.k + (size_t)w.row0 * a.k_stride + w.kvh * HD;
+    const T* v = (const T*)a.v + (size_t)w.row0 * a.v_stride + w.kvh * HD;
+    const Bring<HD> bring_k(a.k_stride, wave, lane), bring_v(a.v_stride, wave, lane);
+    const Reads<HD> at(lane);
+    auto bring = [&](int st) {
+        char* to = lds + (st & 1) * 2 * TB;
+        bring_k(k + (size_t)st * 64 * a.k_stride, w.len - st * 64, to, wave);
+        bring_v(v + (size_t)st * 64 * a.v_stride, w.len - st * 64, to + TB, wave);
+    };
+    bring(0);
+    const bool there = l32 < w.n_valid;
+    const size_t my_row = (size_t)w.row0 + (there ? w.pos0 + l32 : 0);
+    u32x4 qf[KS], df[KS];
+    hold<HD>(qf, (const T*)a.q + my_row * a.q_stride + w.h * HD, there, lh);
+    hold<HD>(df, (const T*)a.dout + my_row * a.dout_stride + w.h * HD, there, lh);
+    float delta = 0.f;
+    {
+        const T* o = (const T*)a.out_in + my_row * a.out_stride + w.h * HD + lh * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const Vec8<T> x = *(const Vec8<T>*)(o + ks * 16), y = __builtin_bit_cast(Vec8<T>, df[ks]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)x[e], (float)y[e], delta);
+        }
+        delta += __shfl_xor(delta, 32, 64);
+    }
+    const float lse = there ? a.lse[(size_t)w.h * a.n_rows + my_row] : INFINITY, lse2 = lse * kLog2e;
+    if (there && lh == 0) a.delta[(size_t)w.h * a.n_rows + my_row] = delta;
+    if (!there) delta = 0.f;
+    f32x16 acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = zeros();
+    const int limit = w.pos0 + l32;
+
+    for (int st = 0; st < w.stages; ++st) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (st + 1 < w.stages) bring(st + 1);
+        if (st >= w.my_stages) continue;
+        const char* kt = lds + (st & 1) * 2 * TB;
+        const char* vt = kt + TB;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f32x16 s = zeros(), dp = zeros();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(kt, half, ks), qf[ks], s);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) dp = mma<T>(at.by_row(vt, half, ks), df[ks], dp);
+            const bool cut = st * 64 + half * 32 + 31 > w.pos0;
+            u32x4 t[2];
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                float x[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    x[e] = __builtin_amdgcn_exp2f(fmaf(s[r + e], a.scale_log2e, -lse2)) * (dp[r + e] - delta);
+                    if (cut && st * 64 + half * 32 + 8 * (r >> 2) + 4 * lh + (r & 3) + e > limit) x[e] = 0.f;
+                }
+                t[r >> 3][(r >> 1) & 3] = pack2<T>(x[0], x[1]);
+            }
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[d] = mma<T>(at.transposed(kt, half * 2 + g, d), t[g], acc[d]);
+        }
+    }
+    __syncthreads();
+    if (!w.active) return;
+    T* dq = (T*)a.dq + ((size_t)w.row0 + w.pos0) * a.dq_stride + w.h * HD;
+    put_rows<T, HD>(acc, a.scale, lds + wave * kPutBytes<HD>, dq, a.dq_stride, w.n_valid, lane);
+    uint64_t rows = __builtin_amdgcn_ballot_w64(there && any_undefined(acc));
+    rows = (rows | (rows >> 32)) & 0xFFFFFFFFull;
+    while (rows) {
+        const int r = __builtin_ctzll(rows);
+        rows &= rows - 1;
+        const size_t row = (size_t)w.row0 + w.pos0 + r;
+        dq_row<T, HD>(a, k, v, (const T*)a.q + row * a.q_stride + w.h * HD, (const T*)a.dout + row * a.dout_stride + w.h * HD, __shfl(lse, r, 64), __shfl(delta, r, 64),
+                      w.pos0 + r, dq + (size_t)r * a.dq_stride, lane);
+    }
 }
 
-template <class T, int HD>
-__global__ __launch_bounds__(256) void pack_dq_kernel(PackArgs a) {
-    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
-    if (row >= a.n_rows) return;
-    const int first = a.starts[sequence_of(a, row)], kvh = h / (a.n_q_heads / a.n_kv_heads);
-    const T* dout = (const T*)a.dout + (size_t)row * a.dout_stride + h * HD;
-    const T* out = (const T*)a.out_in + (size_t)row * a.out_stride + h * HD;
-    const float delta = wave_sum(lane < HD / 8 ? dot8(dout + lane * 8, out + lane * 8, 0.f) : 0.f);
-    if (lane == 0) a.delta[(size_t)h * a.n_rows + row] = delta;
-    dq_row<T, HD>(a, (const T*)a.k + (size_t)first * a.k_stride + kvh * HD, (const T*)a.v + (size_t)first * a.v_stride + kvh * HD,
-                  (const T*)a.q + (size_t)row * a.q_stride + h * HD, dout, a.lse[(size_t)h * a.n_rows + row], delta, row - first,
-                  (T*)a.dq + (size_t)row * a.dq_stride + h * HD, lane);
+// 128 tokens of a kv head a workgroup, 32 a wave; the heads of the group (or a part of them) and their rows from the tokens on pass by.
+template <class T, int HD, bool PARTS>
+__global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD>::BYTES;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * TB > 4 * kPutBytes<HD> ? 4 * TB : 4 * kPutBytes<HD>];
+    __shared__ __attribute__((aligned(16))) float s_row[2][2][64];              // [stage][lse2 or delta][row]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
+    const int4 it = a.k_items[a.first_item + blockIdx.y];
+    const int row0 = it.x, len = it.y, block0 = it.z * 128, G = a.n_q_heads / a.n_kv_heads;
+    const int kvh = blockIdx.x % a.n_kv_heads, part = blockIdx.x / a.n_kv_heads;
+    const int h0 = kvh * G + part * G / a.parts, h1 = kvh * G + (part + 1) * G / a.parts;
+    const int tok0 = block0 + wave * 32, n_valid = max(0, min(32, len - tok0));
+    const int q_stages = (len - block0 + 63) >> 6, stages = q_stages * (h1 - h0);
+    const Bring<HD> bring_q(a.q_stride, wave, lane), bring_d(a.dout_stride, wave, lane);
+    const Reads<HD> at(lane);
+    int next_h = h0, next_q = 0;                  // of the stage to be brought next
+    float row_value = 0.f;
+    auto bring = [&](int st) {
+        char* to = lds + (st & 1) * 2 * TB;
+        const int q0 = block0 + next_q * 64;
+        bring_q((const T*)a.q + (size_t)(row0 + q0) * a.q_stride + next_h * HD, len - q0, to, wave);
+        bring_d((const T*)a.dout + (size_t)(row0 + q0) * a.dout_stride + next_h * HD, len - q0, to + TB, wave);
+        if (wave < 2) {
+            const float* from = (wave ? a.delta : a.lse) + (size_t)next_h * a.n_rows + row0 + q0;
+            row_value = q0 + lane < len ? (wave ? from[lane] : from[lane] * kLog2e) : wave ? 0.f : INFINITY;       // rows that are not there weigh nothing
+        }
+        if (++next_q == q_stages) { next_q = 0; ++next_h; }
+    };
+    auto park = [&](int st) { if (wave < 2) s_row[st & 1][wave][lane] = row_value; };
+    bring(0);
+    const bool there = l32 < n_valid;
+    const size_t my_row = (size_t)row0 + (there ? tok0 + l32 : 0);
+    u32x4 kf[KS], vf[KS];
+    hold<HD>(kf, (const T*)a.k + my_row * a.k_stride + kvh * HD, there, lh);
+    hold<HD>(vf, (const T*)a.v + my_row * a.v_stride + kvh * HD, there, lh);
+    f32x16 dk[DT], dv[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) dk[d] = zeros(), dv[d] = zeros();
+    park(0);
+    int q_stage = 0;
+    for (int st = 0; st < stages; ++st) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const bool more = st + 1 < stages;
+        if (more) bring(st + 1);
+        const int q0 = block0 + q_stage * 64;
+        if (++q_stage == q_stages) q_stage = 0;
+        const char* qt = lds + (st & 1) * 2 * TB;
+        const char* ot = qt + TB;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int qh = q0 + half * 32;
+            if (n_valid > 0 && qh + 31 >= tok0 && qh < len) {
+                f32x16 s = zeros(), dp = zeros();
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(qt, half, ks), kf[ks], s);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) dp = mma<T>(at.by_row(ot, half, ks), vf[ks], dp);
+                const bool cut = qh < tok0 + 31;
+                u32x4 p[2], t[2];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const f32x4 lse2 = *(const f32x4*)&s_row[st & 1][0][half * 32 + b * 8 + lh * 4], delta = *(const f32x4*)&s_row[st & 1][1][half * 32 + b * 8 + lh * 4];
+                    float x[4], y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = __builtin_amdgcn_exp2f(fmaf(s[4 * b + e], a.scale_log2e, -lse2[e]));
+                        y[e] = x[e] * (dp[4 * b + e] - delta[e]);
+                        if (cut && qh + b * 8 + lh * 4 + e < tok0 + l32) x[e] = y[e] = 0.f;
+                    }
+                    p[b >> 1][(b & 1) * 2] = pack2<T>(x[0], x[1]); p[b >> 1][(b & 1) * 2 + 1] = pack2<T>(x[2], x[3]);
+                    t[b >> 1][(b & 1) * 2] = pack2<T>(y[0], y[1]); t[b >> 1][(b & 1) * 2 + 1] = pack2<T>(y[2], y[3]);
+                }
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        dv[d] = mma<T>(at.transposed(ot, half * 2 + g, d), p[g], dv[d]);
+                        dk[d] = mma<T>(at.transposed(qt, half * 2 + g, d), t[g], dk[d]);
+                    }
+            }
+        }
+        if (more) park(st + 1);
+    }
+    __syncthreads();
+    if (n_valid <= 0) return;
+    const size_t first = (size_t)row0 + tok0;
+    if constexpr (PARTS) {                        // fp32 [part][dk or dv][row][kv head][HD]: the lane's row, four dimensions at a time
+        if (there) {
+            const size_t width = (size_t)a.n_kv_heads * HD, plane = (size_t)a.n_rows * width;
+            float* to = a.part + (size_t)part * 2 * plane + (first + l32) * width + kvh * HD + lh * 4;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    *(f32x4*)(to + d * 32 + b * 8) = f32x4{dk[d][4 * b], dk[d][4 * b + 1], dk[d][4 * b + 2], dk[d][4 * b + 3]};
+                    *(f32x4*)(to + plane + d * 32 + b * 8) = f32x4{dv[d][4 * b], dv[d][4 * b + 1], dv[d][4 * b + 2], dv[d][4 * b + 3]};
+                }
+        }
+    } else {
+        char* mine = lds + wave * kPutBytes<HD>;
+        put_rows<T, HD>(dk, a.scale, mine, (T*)a.dk + first * a.dk_stride + kvh * HD, a.dk_stride, n_valid, lane);
+        __builtin_amdgcn_wave_barrier();
+        put_rows<T, HD>(dv, 1.f, mine, (T*)a.dv + first * a.dv_stride + kvh * HD, a.dv_stride, n_valid, lane);
+    }
+    uint64_t rows = __builtin_amdgcn_ballot_w64(there && (any_undefined(dk) || any_undefined(dv)));
+    rows = (rows | (rows >> 32)) & 0xFFFFFFFFull;
+    while (rows) {
+        const int r = __builtin_ctzll(rows);
+        rows &= rows - 1;
+        dkv_row<T, HD, PARTS>(a, row0, len, tok0 + r, kvh, h0, h1, part, lane);
+    }
 }
 
-template <class T, int HD>
-__global__ __launch_bounds__(256) void pack_dkv_kernel(PackArgs a) {
-    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= a.n_rows) return;
-    const int b = sequence_of(a, row), first = a.starts[b];
-    dkv_row<T, HD>(a, first, a.starts[b + 1] - first, row - first, blockIdx.y, lane);
+// dk and dv as the sums of their parts: eight dimensions a thread
+template <class T>
+__global__ __launch_bounds__(256) void pack_join_kernel(PackArgs a, int width) {
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8, plane = (size_t)a.n_rows * width;
+    if (i >= 2 * plane) return;
+    const bool is_v = i >= plane;
+    float g[8] = {};
+    for (int p = 0; p < a.parts; ++p) {
+        const f32x4 x = *(const f32x4*)(a.part + (size_t)p * 2 * plane + i), y = *(const f32x4*)(a.part + (size_t)p * 2 * plane + i + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[e] += x[e], g[4 + e] += y[e];
+    }
+    const size_t j = is_v ? i - plane : i, row = j / width;
+    T* to = (is_v ? (T*)a.dv + row * a.dv_stride : (T*)a.dk + row * a.dk_stride) + (j - row * width);
+    const float c = is_v ? 1.f : a.scale;
+    *(u32x4*)to = u32x4{pack2<T>(g[0] * c, g[1] * c), pack2<T>(g[2] * c, g[3] * c), pack2<T>(g[4] * c, g[5] * c), pack2<T>(g[6] * c, g[7] * c)};
+}
+
+constexpr int kMostItems = 65535;                 // of a launch: its second dimension
+
+hipError_t in_launches(void (*kernel)(PackArgs), PackArgs a, int items, int wide, hipStream_t s) {
+    for (a.first_item = 0; a.first_item < items; a.first_item += kMostItems) {
+        hipLaunchKernelGGL(kernel, dim3(wide, items - a.first_item < kMostItems ? items - a.first_item : kMostItems), dim3(256), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <class T, int HD> hipError_t forward_impl(const PackArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((pack_forward_kernel<T, HD>), dim3((unsigned)((a.n_rows + 3) / 4), a.n_q_heads), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return in_launches(pack_forward_kernel<T, HD>, a, a.n_q_items, a.n_kv_heads, s);
 }
 template <class T, int HD> hipError_t backward_impl(const PackArgs& a, hipStream_t s) {
-    const unsigned blocks = (unsigned)((a.n_rows + 3) / 4);
-    hipLaunchKernelGGL((pack_dq_kernel<T, HD>), dim3(blocks, a.n_q_heads), dim3(256), 0, s, a);
-    const hipError_t e = hipGetLastError();
+    hipError_t e = in_launches(pack_dq_kernel<T, HD>, a, a.n_q_items, a.n_kv_heads, s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((pack_dkv_kernel<T, HD>), dim3(blocks, a.n_kv_heads), dim3(256), 0, s, a);
+    e = in_launches(a.parts > 1 ? pack_dkv_kernel<T, HD, true> : pack_dkv_kernel<T, HD, false>, a, a.n_k_items, a.n_kv_heads * a.parts, s);
+    if (e != hipSuccess || a.parts == 1) return e;
+    const size_t vecs = (size_t)a.n_rows * a.n_kv_heads * HD / 4;
+    hipLaunchKernelGGL((pack_join_kernel<T>), dim3((unsigned)((vecs + 255) / 256)), dim3(256), 0, s, a, a.n_kv_heads * HD);
     return hipGetLastError();
 }
 

@@ -1,5 +1,6 @@
 // Host side of the learner's operators between a decoder block's matrix products: attention over packed sequences, addition with RMSNorm, norm and
 // rotation of heads.
+#include <algorithm>
 #include <cmath>
 #include <memory>
 #include <new>
@@ -14,53 +15,78 @@ constexpr long long kMostRows = 0x7FFFFFFFll;
 // attention
 // ---------------------------------------------------------------------------------------------
 struct spiral_attention_plan {
-    int n_seqs = 0, n_q_heads = 0, n_kv_heads = 0, head_dim = 0;
+    int n_q_heads = 0, n_kv_heads = 0, head_dim = 0, n_q_items = 0, n_k_items = 0, parts = 1;
     long long n_rows = 0;
-    const int32_t* starts = nullptr;          // device
+    const int4 *q_items = nullptr, *k_items = nullptr;      // device
 };
+
+// Workgroups of a sequence: four units of 32 rows and a query head of the group, 128 tokens.
+static long long q_blocks(int len, int group) { return (((long long)len + 31) / 32 * group + 3) / 4; }
+static long long k_blocks(int len) { return ((long long)len + 127) / 128; }
+// The gradients of k and v take a workgroup 128 tokens and one kv head.  Where those are few, and the first tokens' much longer than the last's, the
+// group's heads are shared out.
+static int k_parts(long long items, int group, int n_kv_heads) {
+    const long long wanted = 2048, wgs = items * n_kv_heads;
+    return (int)std::min<long long>(group, std::max<long long>(1, (wanted + wgs - 1) / wgs));
+}
 
 static size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-static int check_plan(const int32_t* host_lens, int B, int hq, int hkv, int hd, long long* rows, const char* who) {
+struct PlanSizes { long long rows = 0, q_items = 0, k_items = 0; };
+static int check_plan(const int32_t* host_lens, int B, int hq, int hkv, int hd, PlanSizes* z, const char* who) {
     if (!host_lens || B < 1) return fail(SPIRAL_ERR_INVALID_ARG, "%s: no sequences", who);
     if (hd != 32 && hd != 64 && hd != 128) return fail(SPIRAL_ERR_SHAPE, "%s: head_dim %d is not 32, 64 or 128", who, hd);
     if (hkv < 1 || hq < 1 || hq % hkv || hq > 1024) return fail(SPIRAL_ERR_SHAPE, "%s: %d query heads on %d kv heads", who, hq, hkv);
-    long long n = 0;
     for (int i = 0; i < B; ++i) {
         if (host_lens[i] < 0) return fail(SPIRAL_ERR_INVALID_ARG, "%s: length %d of sequence %d", who, host_lens[i], i);
-        n += host_lens[i];
+        z->rows += host_lens[i];
+        z->q_items += q_blocks(host_lens[i], hq / hkv);
+        z->k_items += k_blocks(host_lens[i]);
     }
-    if (n < 1 || n > kMostRows) return fail(SPIRAL_ERR_INVALID_ARG, "%s: %lld rows", who, n);
-    *rows = n;
+    if (z->rows < 1 || z->rows > kMostRows) return fail(SPIRAL_ERR_INVALID_ARG, "%s: %lld rows", who, z->rows);
+    if (z->q_items > (1 << 28)) return fail(SPIRAL_ERR_INVALID_ARG, "%s: %lld rows of groups of %d heads", who, z->rows, hq / hkv);
     return SPIRAL_OK;
 }
 
 extern "C" size_t spiral_attention_plan_bytes(const int32_t* host_lens, int B, int n_q_heads, int n_kv_heads, int head_dim) {
-    long long rows;
-    if (check_plan(host_lens, B, n_q_heads, n_kv_heads, head_dim, &rows, "attention_plan_bytes")) return 0;
-    return up256(((size_t)B + 1) * 4);
+    PlanSizes z;
+    if (check_plan(host_lens, B, n_q_heads, n_kv_heads, head_dim, &z, "attention_plan_bytes")) return 0;
+    return up256((size_t)(z.q_items + z.k_items) * sizeof(int4));
 }
 
 extern "C" int spiral_attention_plan_create(const int32_t* host_lens, int B, int n_q_heads, int n_kv_heads, int head_dim, void* dev_mem, size_t bytes,
                                             void* stream, spiral_attention_plan** out) {
     if (!out) return fail(SPIRAL_ERR_INVALID_ARG, "attention_plan_create: null out");
     *out = nullptr;
-    long long rows;
-    const int rc = check_plan(host_lens, B, n_q_heads, n_kv_heads, head_dim, &rows, "attention_plan_create");
+    PlanSizes z;
+    const int rc = check_plan(host_lens, B, n_q_heads, n_kv_heads, head_dim, &z, "attention_plan_create");
     if (rc) return rc;
-    const size_t need = spiral_attention_plan_bytes(host_lens, B, n_q_heads, n_kv_heads, head_dim);
+    const size_t n_items = (size_t)(z.q_items + z.k_items), need = up256(n_items * sizeof(int4));
     if (!dev_mem || !aligned(dev_mem, 256) || bytes < need)
         return fail(SPIRAL_ERR_INVALID_ARG, "attention_plan_create: memory is null, not 256-byte aligned or less than %zu bytes", need);
+    struct Seq { int row0, len; };
     std::unique_ptr<spiral_attention_plan> p(new (std::nothrow) spiral_attention_plan());
-    std::unique_ptr<int32_t[]> starts(new (std::nothrow) int32_t[(size_t)B + 1]);
-    if (!p || !starts) return fail(SPIRAL_ERR_INVALID_ARG, "attention_plan_create: out of host memory");
-    starts[0] = 0;
-    for (int i = 0; i < B; ++i) starts[i + 1] = starts[i] + host_lens[i];
-    p->n_seqs = B; p->n_q_heads = n_q_heads; p->n_kv_heads = n_kv_heads; p->head_dim = head_dim;
-    p->n_rows = rows;
-    p->starts = (const int32_t*)dev_mem;
-    const hipError_t e = launch_upload((int32_t*)dev_mem, starts.get(), B + 1, (hipStream_t)stream);
-    if (e != hipSuccess) return done(e, "attention_plan_create");
+    std::unique_ptr<Seq[]> seqs(new (std::nothrow) Seq[B]);
+    std::unique_ptr<int4[]> items(new (std::nothrow) int4[n_items]);
+    if (!p || !seqs || !items) return fail(SPIRAL_ERR_INVALID_ARG, "attention_plan_create: out of host memory");
+    int row = 0;
+    for (int i = 0; i < B; ++i) { seqs[i] = {row, host_lens[i]}; row += host_lens[i]; }
+    // the longest sequences first, and of each the blocks with the most before (or behind) them: workgroups start in this order, the short ones fill the end
+    std::sort(seqs.get(), seqs.get() + B, [](const Seq& x, const Seq& y) { return x.len != y.len ? x.len > y.len : x.row0 < y.row0; });
+    const int group = n_q_heads / n_kv_heads;
+    int4* at = items.get();
+    for (int i = 0; i < B; ++i)
+        for (long long b = q_blocks(seqs[i].len, group) - 1; b >= 0; --b) *at++ = int4{seqs[i].row0, seqs[i].len, (int)b, 0};
+    for (int i = 0; i < B; ++i)
+        for (long long b = 0; b < k_blocks(seqs[i].len); ++b) *at++ = int4{seqs[i].row0, seqs[i].len, (int)b, 0};
+    p->n_q_heads = n_q_heads; p->n_kv_heads = n_kv_heads; p->head_dim = head_dim;
+    p->n_rows = z.rows; p->n_q_items = (int)z.q_items; p->n_k_items = (int)z.k_items;
+    p->parts = k_parts(z.k_items, group, n_kv_heads);
+    p->q_items = (const int4*)dev_mem; p->k_items = p->q_items + z.q_items;
+    for (size_t t = 0; t < n_items; t += 1 << 20) {              // sizes of launch_upload are ints
+        const hipError_t e = launch_upload((int32_t*)dev_mem + t * 4, (const int32_t*)(items.get() + t), (int)std::min<size_t>(1 << 20, n_items - t) * 4, (hipStream_t)stream);
+        if (e != hipSuccess) return done(e, "attention_plan_create");
+    }
     *out = p.release();
     return SPIRAL_OK;
 }
@@ -73,8 +99,8 @@ static bool matrix_ok(const void* p, long long stride, long long width) {
 }
 static PackArgs pack_args(const spiral_attention_plan* p, float scale) {
     PackArgs a = {};
-    a.starts = p->starts; a.n_seqs = p->n_seqs; a.n_rows = p->n_rows;
-    a.n_q_heads = p->n_q_heads; a.n_kv_heads = p->n_kv_heads;
+    a.q_items = p->q_items; a.n_q_items = p->n_q_items; a.k_items = p->k_items; a.n_k_items = p->n_k_items; a.n_rows = p->n_rows;
+    a.n_q_heads = p->n_q_heads; a.n_kv_heads = p->n_kv_heads; a.parts = p->parts;
     a.scale = scale; a.scale_log2e = (float)(scale * 1.4426950408889634);
     return a;
 }
@@ -100,7 +126,9 @@ extern "C" int spiral_attention_forward(const spiral_attention_plan* plan, const
 }
 
 extern "C" size_t spiral_attention_backward_workspace_bytes(const spiral_attention_plan* plan) {
-    return plan ? up256((size_t)plan->n_rows * plan->n_q_heads * 4) : 0;
+    if (!plan) return 0;
+    const size_t delta = up256((size_t)plan->n_rows * plan->n_q_heads * 4);
+    return delta + (plan->parts > 1 ? up256((size_t)plan->parts * 2 * plan->n_rows * plan->n_kv_heads * plan->head_dim * 4) : 0);
 }
 
 extern "C" int spiral_attention_backward(const spiral_attention_plan* plan, const void* dev_q, long long q_stride, const void* dev_k, long long k_stride,
@@ -127,6 +155,7 @@ extern "C" int spiral_attention_backward(const spiral_attention_plan* plan, cons
     PackArgs a = pack_args(plan, scale);
     a.q = dev_q; a.k = dev_k; a.v = dev_v; a.out_in = dev_out; a.lse = (float*)dev_lse; a.dout = dev_dout;
     a.dq = dev_dq; a.dk = dev_dk; a.dv = dev_dv; a.delta = (float*)dev_workspace;
+    a.part = (float*)((char*)dev_workspace + up256((size_t)n * plan->n_q_heads * 4));
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.out_stride = out_stride; a.dout_stride = dout_stride;
     a.dq_stride = dq_stride; a.dk_stride = dk_stride; a.dv_stride = dv_stride;
     return done(launch_pack_backward(a, dtype, plan->head_dim, (hipStream_t)stream), "attention_backward");

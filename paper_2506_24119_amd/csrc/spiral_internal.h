@@ -259,9 +259,11 @@ struct PackArgs {
     long long q_stride, k_stride, v_stride, out_stride, dout_stride, dq_stride, dk_stride, dv_stride;      // elements
     float* lse;                               // [Hq][n_rows]
     float* delta;                             // [Hq][n_rows]: dout . out
-    const int32_t* starts;                    // [n_seqs + 1] first rows
+    float* part;                              // [parts][dk, dv][n_rows][n_kv_heads * hd], where there is more than one
+    // what workgroups take: {first row and length of a sequence, block of its rows (four units of 32 rows and a head) or of its tokens (128)}
+    const int4 *q_items, *k_items;
     long long n_rows;
-    int32_t n_seqs, n_q_heads, n_kv_heads;
+    int32_t n_q_items, n_k_items, first_item, n_q_heads, n_kv_heads, parts;      // parts: of a group's heads in the gradients of k and v
     float scale, scale_log2e;
 };
 hipError_t launch_pack_forward(const PackArgs& a, int dtype, int hd, hipStream_t s);
