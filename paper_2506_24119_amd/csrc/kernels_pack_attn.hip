@@ -184,7 +184,8 @@ template <int HD> struct Bring {
     }
     // first: the tile's first row, of `rows` that are there
     __device__ __forceinline__ void operator()(const void* first, int rows, char* lds, int wave) const {
-        const __amdgpu_buffer_rsrc_t r = buffer_upto(first, (uint32_t)max(0, min(rows, 64)) * row_bytes);
+        // (a descriptor has to be in scalar registers: one that the compiler keeps in vector registers costs a loop a load)
+        const __amdgpu_buffer_rsrc_t r = buffer_upto(first, __builtin_amdgcn_readfirstlane((uint32_t)max(0, min(rows, 64)) * row_bytes));
 #pragma unroll
         for (int u = 0; u < Tile<HD>::LOADS; ++u) to_lds(r, lds + (wave * Tile<HD>::LOADS + u) * 1024, off[u]);
     }
