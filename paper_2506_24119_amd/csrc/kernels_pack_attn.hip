@@ -133,14 +133,13 @@ __device__ void dkv_row(const PackArgs& a, int row0, int len, int t, int kvh, in
 }
 
 // ------------------------------------------------------------------------------------------------
-// Tiles of 64 rows of one head in LDS, row-major, brought there by loads that write LDS themselves.  A row's 16-byte pieces are permuted so that
-// neither kind of read meets a bank twice: 8 lanes that read one piece of 8 consecutive rows, and the transposing read, in which 16 lanes
-// read 32 bytes of four consecutive rows each.
+// Tiles of 64 rows of one head in LDS, brought there by loads that write LDS themselves: for each 32 dimensions a part of 64 rows x 64 bytes.  LDS serves 256
+// bytes a cycle from as many banks.  Within four rows the transposing read (32 lanes: 64 bytes of four consecutive rows each) meets no bank twice as it
+// is; for 16 lanes that read one 16-byte piece of 16 consecutive rows each, a row's four pieces are permuted by its number's bits 2 and 3.  Operand
+// addresses are then two of a lane and constants, for either read.
 template <int HD> struct Tile {
-    static constexpr int ROW = HD * 2, PIECES = HD / 8, BYTES = 64 * ROW, LOADS = BYTES / 4096;        // LOADS: of 1 KB, a wave of four
-    static __device__ __forceinline__ int swizzle(int row) {
-        return HD == 32 ? (row & 2) | ((row >> 2) & 1) : ((row & 3) << 1) | ((row >> 2) & 1);
-    }
+    static constexpr int PARTS = HD / 32, PART = 4096, BYTES = PARTS * PART;
+    static __device__ __forceinline__ int swizzle(int row) { return (row >> 2) & 3; }
 };
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -163,31 +162,32 @@ __device__ __forceinline__ f32x16 zeros() {
     return z;
 }
 
-// 64 lanes x 16 bytes straight to 1 KB of LDS at `to` (wave-uniform); what lies beyond the buffer's end comes as zeros
-__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char* to, uint32_t off) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, off, 0, 0, 0);
+// 64 lanes x 16 bytes straight to 1 KB of LDS at `to` (wave-uniform), IMM counted on both sides; what lies beyond the buffer's end comes as zeros
+template <int IMM> __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char* to, uint32_t off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, off, 0, IMM, 0);
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_upto(const void* p, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
 }
 
-// What a wave brings of a tile: the lane's offsets from the tile's first row.  Rows past the sequence's end come as zeros: the buffer descriptor ends there.
+// What a wave of four brings of a tile: 16 of its rows.  Rows past the sequence's end come as zeros: the buffer descriptor ends there.
 template <int HD> struct Bring {
-    uint32_t off[Tile<HD>::LOADS];
-    uint32_t row_bytes;
+    uint32_t off, row_bytes;
     __device__ __forceinline__ Bring(long long stride, int wave, int lane) : row_bytes((uint32_t)stride * 2u) {
-#pragma unroll
-        for (int u = 0; u < Tile<HD>::LOADS; ++u) {
-            const int at = (wave * Tile<HD>::LOADS + u) * 64 + lane, row = at / Tile<HD>::PIECES, piece = at % Tile<HD>::PIECES;
-            off[u] = row * row_bytes + ((piece ^ Tile<HD>::swizzle(row)) * 16);
-        }
+        const int row = wave * 16 + (lane >> 2);
+        off = row * row_bytes + (((lane & 3) ^ Tile<HD>::swizzle(row)) * 16);
     }
     // first: the tile's first row, of `rows` that are there
     __device__ __forceinline__ void operator()(const void* first, int rows, char* lds, int wave) const {
         // (a descriptor has to be in scalar registers: one that the compiler keeps in vector registers costs a loop a load)
         const __amdgpu_buffer_rsrc_t r = buffer_upto(first, __builtin_amdgcn_readfirstlane((uint32_t)max(0, min(rows, 64)) * row_bytes));
-#pragma unroll
-        for (int u = 0; u < Tile<HD>::LOADS; ++u) to_lds(r, lds + (wave * Tile<HD>::LOADS + u) * 1024, off[u]);
+        char* to = lds + wave * 1024;
+        to_lds<0>(r, to, off);
+        if constexpr (HD >= 64) to_lds<64>(r, to + Tile<HD>::PART - 64, off);
+        if constexpr (HD >= 128) {
+            to_lds<128>(r, to + 2 * Tile<HD>::PART - 128, off);
+            to_lds<192>(r, to + 3 * Tile<HD>::PART - 192, off);
+        }
     }
 };
 
@@ -195,22 +195,24 @@ template <int HD> struct Bring {
 // By rows: the contraction runs along the row.  Transposed: operand rows are dimensions, the contraction runs over the tile's rows, of 16 in the order
 // 4 lh .. + 3, 8 + 4 lh .. + 3: that in which a product's result leaves them.
 template <int HD> struct Reads {
-    int row, col;                             // of a lane: offset of its row's piece 0 or 1, of its transposed corner
+    int row[2], col[2];                       // of a lane: its row's piece of the first 16 elements and of the second; its transposed corner, and that 8 rows on
     __device__ __forceinline__ Reads(int lane) {
         const int l32 = lane & 31, lh = lane >> 5, i = lane & 15, r = 4 * lh + (i >> 2);
-        row = l32 * Tile<HD>::ROW + ((lh ^ Tile<HD>::swizzle(l32)) * 16);
-        col = r * Tile<HD>::ROW + (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ Tile<HD>::swizzle(r)) * 16) + (i & 1) * 8;
+        row[0] = l32 * 64 + ((lh ^ Tile<HD>::swizzle(l32)) * 16);
+        row[1] = row[0] ^ 32;
+        col[0] = r * 64 + (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ Tile<HD>::swizzle(r)) * 16) + (i & 1) * 8;
+        col[1] = (col[0] ^ 32) + 8 * 64;
     }
     // rows 32 half .. + 31, elements 16 ks .. + 15
     __device__ __forceinline__ u32x4 by_row(const char* tile, int half, int ks) const {
-        return *(const u32x4*)(tile + ((row ^ ((ks & 3) * 32)) + (ks >> 2) * 128 + half * 32 * Tile<HD>::ROW));
+        return *(const u32x4*)(tile + row[ks & 1] + (ks >> 1) * Tile<HD>::PART + half * 32 * 64);
     }
     // dimensions 32 dt .. + 31, rows 16 group .. + 15
     __device__ __forceinline__ u32x4 transposed(const char* tile, int group, int dt) const {
         typedef __attribute__((address_space(3))) s16x4 Corner;
-        const char* p = tile + ((col ^ ((dt & 1) * 64)) + (dt >> 1) * 128 + group * 16 * Tile<HD>::ROW);
-        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Corner*)p));
-        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Corner*)(p + 8 * Tile<HD>::ROW)));
+        const char* p = tile + dt * Tile<HD>::PART + group * 16 * 64;
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Corner*)(p + col[0])));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Corner*)(p + col[1])));
         return u32x4{lo.x, lo.y, hi.x, hi.y};
     }
 };
@@ -472,19 +474,21 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
     const Bring<HD> bring_q(a.q_stride, wave, lane), bring_d(a.dout_stride, wave, lane);
     const Reads<HD> at(lane);
     int next_h = h0, next_q = 0;                  // of the stage to be brought next
-    float row_value = 0.f;
+    float row_value = 0.f;                        // of the stage being brought: its row `lane`'s lse or delta
+    bool row_there = false;
     auto bring = [&](int st) {
         char* to = lds + (st & 1) * 2 * TB;
         const int q0 = block0 + next_q * 64;
         bring_q((const T*)a.q + (size_t)(row0 + q0) * a.q_stride + next_h * HD, len - q0, to, wave);
         bring_d((const T*)a.dout + (size_t)(row0 + q0) * a.dout_stride + next_h * HD, len - q0, to + TB, wave);
-        if (wave < 2) {
-            const float* from = (wave ? a.delta : a.lse) + (size_t)next_h * a.n_rows + row0 + q0;
-            row_value = q0 + lane < len ? (wave ? from[lane] : from[lane] * kLog2e) : wave ? 0.f : INFINITY;       // rows that are not there weigh nothing
-        }
+        if (wave < 2) row_value = ((wave ? a.delta : a.lse) + (size_t)next_h * a.n_rows + row0 + q0)[min(lane, len - 1 - q0)];
+        row_there = q0 + lane < len;
         if (++next_q == q_stages) { next_q = 0; ++next_h; }
     };
-    auto park = [&](int st) { if (wave < 2) s_row[st & 1][wave][lane] = row_value; };
+    auto park = [&](int st) {                     // rows that are not there weigh nothing
+        if (wave == 0) s_row[st & 1][0][lane] = row_there ? row_value * kLog2e : INFINITY;
+        else if (wave == 1) s_row[st & 1][1][lane] = row_there ? row_value : 0.f;
+    };
     bring(0);
     const bool there = l32 < n_valid;
     const size_t my_row = (size_t)row0 + (there ? tok0 + l32 : 0);
