@@ -133,14 +133,14 @@ __device__ void dkv_row(const PackArgs& a, int row0, int len, int t, int kvh, in
 }
 
 // ------------------------------------------------------------------------------------------------
-// Tiles of 64 rows of one head in LDS, brought there by loads that write LDS themselves: for each 32 dimensions a part of 64 rows x 64 bytes.  LDS serves 256
+// Tiles of 64 (or 32) rows of one head in LDS, brought there by loads that write LDS themselves: for each 32 dimensions a part of 64 bytes a row.  LDS serves 256
 // bytes a cycle from as many banks.  Within four rows the transposing read (32 lanes: 64 bytes of four consecutive rows each) meets no bank twice as it
 // is; for 16 lanes that read one 16-byte piece of 16 consecutive rows each, a row's four pieces are permuted by its number's bits 2 and 3.  Operand
 // addresses are then two of a lane and constants, for either read.
-template <int HD> struct Tile {
-    static constexpr int PARTS = HD / 32, PART = 4096, BYTES = PARTS * PART;
-    static __device__ __forceinline__ int swizzle(int row) { return (row >> 2) & 3; }
+template <int HD, int ROWS = 64> struct Tile {
+    static constexpr int PARTS = HD / 32, PART = ROWS * 64, BYTES = PARTS * PART;
 };
+__device__ __forceinline__ int swizzle(int row) { return (row >> 2) & 3; }
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -175,7 +175,7 @@ template <int HD> struct Bring {
     uint32_t off, row_bytes;
     __device__ __forceinline__ Bring(long long stride, int wave, int lane) : row_bytes((uint32_t)stride * 2u) {
         const int row = wave * 16 + (lane >> 2);
-        off = row * row_bytes + (((lane & 3) ^ Tile<HD>::swizzle(row)) * 16);
+        off = row * row_bytes + (((lane & 3) ^ swizzle(row)) * 16);
     }
     // first: the tile's first row, of `rows` that are there
     __device__ __forceinline__ void operator()(const void* first, int rows, char* lds, int wave) const {
@@ -191,26 +191,42 @@ template <int HD> struct Bring {
     }
 };
 
+// The same of a tile of 32 rows, 16 rows of a part a load: HD / 16 loads, of which a wave of four makes every fourth.
+template <int HD> struct Bring32 {
+    static constexpr int LOADS = HD / 16;
+    uint32_t off, row_bytes;
+    __device__ __forceinline__ Bring32(long long stride, int wave, int lane) : row_bytes((uint32_t)stride * 2u) {
+        const int row = (wave & 1) * 16 + (lane >> 2);
+        off = row * row_bytes + (((lane & 3) ^ swizzle(row)) * 16) + (wave >> 1) * 64;
+    }
+    __device__ __forceinline__ void operator()(const void* first, int rows, char* lds, int wave) const {
+        const __amdgpu_buffer_rsrc_t r = buffer_upto(first, __builtin_amdgcn_readfirstlane((uint32_t)max(0, min(rows, 32)) * row_bytes));
+        char* to = lds + wave * 1024;
+        if (LOADS >= 4 || wave < LOADS) to_lds<0>(r, to, off);
+        if constexpr (LOADS > 4) to_lds<128>(r, to + 4096 - 128, off);
+    }
+};
+
 // A matrix operand's lane holds a row (l32 of 32) and eight of 16 contracted elements (the half that lh says).
 // By rows: the contraction runs along the row.  Transposed: operand rows are dimensions, the contraction runs over the tile's rows, of 16 in the order
 // 4 lh .. + 3, 8 + 4 lh .. + 3: that in which a product's result leaves them.
-template <int HD> struct Reads {
+template <int HD, int ROWS = 64> struct Reads {
     int row[2], col[2];                       // of a lane: its row's piece of the first 16 elements and of the second; its transposed corner, and that 8 rows on
     __device__ __forceinline__ Reads(int lane) {
         const int l32 = lane & 31, lh = lane >> 5, i = lane & 15, r = 4 * lh + (i >> 2);
-        row[0] = l32 * 64 + ((lh ^ Tile<HD>::swizzle(l32)) * 16);
+        row[0] = l32 * 64 + ((lh ^ swizzle(l32)) * 16);
         row[1] = row[0] ^ 32;
-        col[0] = r * 64 + (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ Tile<HD>::swizzle(r)) * 16) + (i & 1) * 8;
+        col[0] = r * 64 + (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ swizzle(r)) * 16) + (i & 1) * 8;
         col[1] = (col[0] ^ 32) + 8 * 64;
     }
     // rows 32 half .. + 31, elements 16 ks .. + 15
     __device__ __forceinline__ u32x4 by_row(const char* tile, int half, int ks) const {
-        return *(const u32x4*)(tile + row[ks & 1] + (ks >> 1) * Tile<HD>::PART + half * 32 * 64);
+        return *(const u32x4*)(tile + row[ks & 1] + (ks >> 1) * Tile<HD, ROWS>::PART + half * 32 * 64);
     }
     // dimensions 32 dt .. + 31, rows 16 group .. + 15
     __device__ __forceinline__ u32x4 transposed(const char* tile, int group, int dt) const {
         typedef __attribute__((address_space(3))) s16x4 Corner;
-        const char* p = tile + dt * Tile<HD>::PART + group * 16 * 64;
+        const char* p = tile + dt * Tile<HD, ROWS>::PART + group * 16 * 64;
         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Corner*)(p + col[0])));
         const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Corner*)(p + col[1])));
         return u32x4{lo.x, lo.y, hi.x, hi.y};
@@ -257,6 +273,17 @@ template <int N> __device__ __forceinline__ bool any_undefined(const f32x16 (&ac
         for (int r = 0; r < 16; ++r) bad = bad || acc[t][r] != acc[t][r];
     return bad;
 }
+// whether a row of HD elements has one that is infinite or undefined
+template <class T, int HD> __device__ __forceinline__ bool not_finite(const T* row) {
+    float s = 0.f;
+#pragma unroll 1
+    for (int d = 0; d < HD; d += 8) {
+        const Vec8<T> x = *(const Vec8<T>*)(row + d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf((float)x[e], 0.f, s);
+    }
+    return s != s;
+}
 
 // A workgroup's place: four units of a (sequence, kv head), a unit being 32 positions of one query head; units are counted heads first.
 struct Unit {
@@ -286,12 +313,10 @@ __global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
     const T* v = (const T*)a.v + (size_t)w.row0 * a.v_stride + w.kvh * HD;
     const Bring<HD> bring_k(a.k_stride, wave, lane), bring_v(a.v_stride, wave, lane);
     const Reads<HD> at(lane);
-    auto bring = [&](int st) {
-        char* to = lds + (st & 1) * 2 * TB;
-        bring_k(k + (size_t)st * 64 * a.k_stride, w.len - st * 64, to, wave);
-        bring_v(v + (size_t)st * 64 * a.v_stride, w.len - st * 64, to + TB, wave);
-    };
-    bring(0);
+    char* const vlds = lds + 2 * TB;
+    auto more_k = [&](int st) { bring_k(k + (size_t)st * 64 * a.k_stride, w.len - st * 64, lds + (st & 1) * TB, wave); };
+    auto more_v = [&](int st) { bring_v(v + (size_t)st * 64 * a.v_stride, w.len - st * 64, vlds + (st & 1) * TB, wave); };
+    more_k(0);
     const bool there = l32 < w.n_valid;
     const size_t my_row = (size_t)w.row0 + (there ? w.pos0 + l32 : 0);
     u32x4 qf[KS];
@@ -302,21 +327,17 @@ __global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
     float m = kLeast, l = 0.f;
     const int limit = w.pos0 + l32;
 
-    for (int st = 0; st < w.stages; ++st) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (st + 1 < w.stages) bring(st + 1);
-        if (st >= w.my_stages) continue;
-        const char* kt = lds + (st & 1) * 2 * TB;
-        const char* vt = kt + TB;
-        f32x16 s[2];
+    auto scores = [&](f32x16 (&s)[2], int st) {
+        const char* kt = lds + (st & 1) * TB;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             s[half] = zeros();
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) s[half] = mma<T>(at.by_row(kt, half, ks), qf[ks], s[half]);
         }
+    };
+    // what the rows do not see of stage st, and the reference of their exponents
+    auto refer = [&](f32x16 (&s)[2], int st) {
         if (st * 64 + 63 > w.pos0) {
 #pragma unroll
             for (int half = 0; half < 2; ++half)
@@ -329,8 +350,9 @@ __global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[half][r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.scale_log2e;
-        if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {          // the reference moves only where weights would pass 2^8
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);
+        mx = fmaxf(__int_as_float(both[0]), __int_as_float(both[1])) * a.scale_log2e;
+        if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {          // it moves only where weights would pass 2^8
             const float m_new = fmaxf(m, mx), shrink = __builtin_amdgcn_exp2f(m - m_new);
             l *= shrink;
 #pragma unroll
@@ -339,19 +361,49 @@ __global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
                 for (int r = 0; r < 16; ++r) acc[d][r] *= shrink;
             m = m_new;
         }
-        u32x4 p[4];
+    };
+    auto weigh = [&](const f32x16& s, u32x4 (&p)[2]) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int r = 0; r < 16; r += 2) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2e, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[r + 1], a.scale_log2e, -m));
+            l += x + y;
+            p[r >> 3][(r >> 1) & 3] = pack2<T>(x, y);
+        }
+    };
+    // Stage st's weights and products, and meanwhile the scores of the next (past the last: of what stands in LDS, for nothing).
+    auto step = [&](f32x16 (&s)[2], f32x16 (&next)[2], int st) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (st + 2 < w.stages) more_k(st + 2);
+        if (st + 1 < w.stages) more_v(st + 1);
+        if (st >= w.my_stages) return;
+        const char* vt = vlds + (st & 1) * TB;
+        scores(next, st + 1);
 #pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[half][r], a.scale_log2e, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[half][r + 1], a.scale_log2e, -m));
-                l += x + y;
-                p[half * 2 + (r >> 3)][(r >> 1) & 3] = pack2<T>(x, y);
-            }
+        for (int half = 0; half < 2; ++half) {
+            u32x4 p[2];
+            weigh(s[half], p);
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+            for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) acc[d] = mma<T>(at.transposed(vt, g, d), p[g], acc[d]);
+                for (int d = 0; d < DT; ++d) acc[d] = mma<T>(at.transposed(vt, half * 2 + g, d), p[g], acc[d]);
+        }
+        if (st + 1 < w.my_stages) refer(next, st + 1);
+    };
+    if (w.stages > 1) more_k(1);
+    more_v(0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    f32x16 s[2], next[2];
+    if (w.my_stages > 0) {
+        scores(s, 0);
+        refer(s, 0);
+    }
+    for (int st = 0; st < w.stages; st += 2) {
+        step(s, next, st);
+        if (st + 1 < w.stages) step(next, s, st + 1);
     }
     __syncthreads();                              // the last tiles have been read
     if (!w.active) return;
@@ -360,13 +412,18 @@ __global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
     float* lse = a.lse + (size_t)w.h * a.n_rows + w.row0 + w.pos0;
     put_rows<T, HD>(acc, 1.f / l, lds + wave * kPutBytes<HD>, out, a.out_stride, w.n_valid, lane);
     if (lh == 0 && there) lse[l32] = (m + __builtin_amdgcn_logf(l)) * kLn2;
-    const bool bad = there && (any_undefined(acc) || l != l);
-    uint64_t rows = __builtin_amdgcn_ballot_w64(bad);
+    // A weight of 0 times an infinite or undefined value of a token that the row does not see: such rows are computed alone.  (Where l is undefined, so is the row.)
+    uint64_t rows = __builtin_amdgcn_ballot_w64(there && l == l && any_undefined(acc));
     rows = (rows | (rows >> 32)) & 0xFFFFFFFFull;
-    while (rows) {                                // 0 times an undefined value of a row that is not seen
-        const int r = __builtin_ctzll(rows);
-        rows &= rows - 1;
-        forward_row<T, HD>(a, k, v, (const T*)a.q + ((size_t)w.row0 + w.pos0 + r) * a.q_stride + w.h * HD, w.pos0 + r, out + (size_t)r * a.out_stride, lse + r, lane);
+    if (rows) {
+        const int t0 = (w.my_stages - 1) * 64, t = t0 + lane;
+        const uint64_t odd = __builtin_amdgcn_ballot_w64(t < w.len && not_finite<T, HD>(v + (size_t)t * a.v_stride));
+        while (rows) {
+            const int r = __builtin_ctzll(rows);
+            rows &= rows - 1;
+            if (odd >> (w.pos0 + r - t0) >> 1)
+                forward_row<T, HD>(a, k, v, (const T*)a.q + ((size_t)w.row0 + w.pos0 + r) * a.q_stride + w.h * HD, w.pos0 + r, out + (size_t)r * a.out_stride, lse + r, lane);
+        }
     }
 }
 
@@ -447,102 +504,112 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
     if (!w.active) return;
     T* dq = (T*)a.dq + ((size_t)w.row0 + w.pos0) * a.dq_stride + w.h * HD;
     put_rows<T, HD>(acc, a.scale, lds + wave * kPutBytes<HD>, dq, a.dq_stride, w.n_valid, lane);
-    uint64_t rows = __builtin_amdgcn_ballot_w64(there && any_undefined(acc));
+    uint64_t rows = __builtin_amdgcn_ballot_w64(there && lse == lse && delta == delta && any_undefined(acc));      // as in the forward kernel, of keys
     rows = (rows | (rows >> 32)) & 0xFFFFFFFFull;
-    while (rows) {
-        const int r = __builtin_ctzll(rows);
-        rows &= rows - 1;
-        const size_t row = (size_t)w.row0 + w.pos0 + r;
-        dq_row<T, HD>(a, k, v, (const T*)a.q + row * a.q_stride + w.h * HD, (const T*)a.dout + row * a.dout_stride + w.h * HD, __shfl(lse, r, 64), __shfl(delta, r, 64),
-                      w.pos0 + r, dq + (size_t)r * a.dq_stride, lane);
+    if (rows) {
+        const int t0 = (w.my_stages - 1) * 64, t = t0 + lane;
+        const uint64_t odd = __builtin_amdgcn_ballot_w64(t < w.len && not_finite<T, HD>(k + (size_t)t * a.k_stride));
+        while (rows) {
+            const int r = __builtin_ctzll(rows);
+            rows &= rows - 1;
+            const size_t row = (size_t)w.row0 + w.pos0 + r;
+            if (odd >> (w.pos0 + r - t0) >> 1)
+                dq_row<T, HD>(a, k, v, (const T*)a.q + row * a.q_stride + w.h * HD, (const T*)a.dout + row * a.dout_stride + w.h * HD, __shfl(lse, r, 64), __shfl(delta, r, 64),
+                              w.pos0 + r, dq + (size_t)r * a.dq_stride, lane);
+        }
     }
 }
 
-// 128 tokens of a kv head a workgroup, 32 a wave; the heads of the group (or a part of them) and their rows from the tokens on pass by.
+// 128 tokens of a kv head a workgroup, 32 a wave; the heads of the group (or a part of them) and their rows from the tokens on pass by, 32 at a time.  Keys stay in
+// registers, values in LDS: with both in registers, beside two accumulators, there are too few left to read operands ahead.
+template <int HD> constexpr int kDkvBytes = 2 * Tile<HD>::BYTES + 4 * Tile<HD, 32>::BYTES + 512;
 template <class T, int HD, bool PARTS>
 __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
-    constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD>::BYTES;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * TB > 4 * kPutBytes<HD> ? 4 * TB : 4 * kPutBytes<HD>];
-    __shared__ __attribute__((aligned(16))) float s_row[2][2][64];              // [stage][lse2 or delta][row]
+    constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD, 32>::BYTES;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    static_assert(4 * kPutBytes<HD> <= kDkvBytes<HD>, "results leave through the same LDS");
+    char* const stages_lds = lds + 2 * Tile<HD>::BYTES;                          // [stage parity][queries, gradients]
+    float* const s_row = (float*)(stages_lds + 4 * TB);                         // [stage parity][lse2, delta][row]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
     const int4 it = a.k_items[a.first_item + blockIdx.y];
     const int row0 = it.x, len = it.y, block0 = it.z * 128, G = a.n_q_heads / a.n_kv_heads;
     const int kvh = blockIdx.x % a.n_kv_heads, part = blockIdx.x / a.n_kv_heads;
     const int h0 = kvh * G + part * G / a.parts, h1 = kvh * G + (part + 1) * G / a.parts;
     const int tok0 = block0 + wave * 32, n_valid = max(0, min(32, len - tok0));
-    const int q_stages = (len - block0 + 63) >> 6, stages = q_stages * (h1 - h0);
-    const Bring<HD> bring_q(a.q_stride, wave, lane), bring_d(a.dout_stride, wave, lane);
-    const Reads<HD> at(lane);
-    int next_h = h0, next_q = 0;                  // of the stage to be brought next
-    float row_value = 0.f;                        // of the stage being brought: its row `lane`'s lse or delta
+    const int q_stages = (len - block0 + 31) >> 5, stages = q_stages * (h1 - h0);
+    const Bring32<HD> bring_q(a.q_stride, wave, lane), bring_d(a.dout_stride, wave, lane);
+    int next_h = h0, next_q = block0;             // of the stage to be brought next
+    float row_value = 0.f;                        // its row l32's lse or delta
     bool row_there = false;
     auto bring = [&](int st) {
-        char* to = lds + (st & 1) * 2 * TB;
-        const int q0 = block0 + next_q * 64;
-        bring_q((const T*)a.q + (size_t)(row0 + q0) * a.q_stride + next_h * HD, len - q0, to, wave);
-        bring_d((const T*)a.dout + (size_t)(row0 + q0) * a.dout_stride + next_h * HD, len - q0, to + TB, wave);
-        if (wave < 2) row_value = ((wave ? a.delta : a.lse) + (size_t)next_h * a.n_rows + row0 + q0)[min(lane, len - 1 - q0)];
-        row_there = q0 + lane < len;
-        if (++next_q == q_stages) { next_q = 0; ++next_h; }
+        char* to = stages_lds + (st & 1) * 2 * TB;
+        bring_q((const T*)a.q + (size_t)(row0 + next_q) * a.q_stride + next_h * HD, len - next_q, to, wave);
+        bring_d((const T*)a.dout + (size_t)(row0 + next_q) * a.dout_stride + next_h * HD, len - next_q, to + TB, wave);
+        if (wave == 0) row_value = ((lh ? a.delta : a.lse) + (size_t)next_h * a.n_rows + row0 + next_q)[min(l32, len - 1 - next_q)];
+        row_there = next_q + l32 < len;
+        if ((next_q += 32) >= len) { next_q = block0; ++next_h; }
     };
     auto park = [&](int st) {                     // rows that are not there weigh nothing
-        if (wave == 0) s_row[st & 1][0][lane] = row_there ? row_value * kLog2e : INFINITY;
-        else if (wave == 1) s_row[st & 1][1][lane] = row_there ? row_value : 0.f;
+        if (wave == 0) s_row[(st & 1) * 64 + lane] = lh ? (row_there ? row_value : 0.f) : row_there ? row_value * kLog2e : INFINITY;
     };
+    {
+        const Bring<HD> bring_v(a.v_stride, wave, lane);
+        const T* v = (const T*)a.v + (size_t)(row0 + block0) * a.v_stride + kvh * HD;
+        bring_v(v, len - block0, lds, wave);
+        bring_v(v + (size_t)64 * a.v_stride, len - block0 - 64, lds + Tile<HD>::BYTES, wave);
+    }
     bring(0);
     const bool there = l32 < n_valid;
-    const size_t my_row = (size_t)row0 + (there ? tok0 + l32 : 0);
-    u32x4 kf[KS], vf[KS];
-    hold<HD>(kf, (const T*)a.k + my_row * a.k_stride + kvh * HD, there, lh);
-    hold<HD>(vf, (const T*)a.v + my_row * a.v_stride + kvh * HD, there, lh);
+    u32x4 kf[KS];
+    hold<HD>(kf, (const T*)a.k + ((size_t)row0 + (there ? tok0 + l32 : 0)) * a.k_stride + kvh * HD, there, lh);
     f32x16 dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = zeros(), dv[d] = zeros();
     park(0);
-    int q_stage = 0;
+    const Reads<HD> at_v(lane);
+    const Reads<HD, 32> at(lane);
+    const char* vt = lds + (wave >> 1) * Tile<HD>::BYTES;
+    int q0 = block0;
     for (int st = 0; st < stages; ++st) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const bool more = st + 1 < stages;
         if (more) bring(st + 1);
-        const int q0 = block0 + q_stage * 64;
-        if (++q_stage == q_stages) q_stage = 0;
-        const char* qt = lds + (st & 1) * 2 * TB;
+        const char* qt = stages_lds + (st & 1) * 2 * TB;
         const char* ot = qt + TB;
+        const float* rows = s_row + (st & 1) * 64 + lh * 4;
+        if (n_valid > 0 && q0 + 31 >= tok0) {
+            f32x16 s = zeros(), dp = zeros();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int qh = q0 + half * 32;
-            if (n_valid > 0 && qh + 31 >= tok0 && qh < len) {
-                f32x16 s = zeros(), dp = zeros();
+            for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(qt, 0, ks), kf[ks], s);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(qt, half, ks), kf[ks], s);
+            for (int ks = 0; ks < KS; ++ks) dp = mma<T>(at.by_row(ot, 0, ks), at_v.by_row(vt, wave & 1, ks), dp);
+            const bool cut = q0 < tok0 + 31;
+            u32x4 p[2], t[2];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) dp = mma<T>(at.by_row(ot, half, ks), vf[ks], dp);
-                const bool cut = qh < tok0 + 31;
-                u32x4 p[2], t[2];
+            for (int b = 0; b < 4; ++b) {
+                const f32x4 lse2 = *(const f32x4*)(rows + b * 8), delta = *(const f32x4*)(rows + 32 + b * 8);
+                float x[4], y[4];
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const f32x4 lse2 = *(const f32x4*)&s_row[st & 1][0][half * 32 + b * 8 + lh * 4], delta = *(const f32x4*)&s_row[st & 1][1][half * 32 + b * 8 + lh * 4];
-                    float x[4], y[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[e] = __builtin_amdgcn_exp2f(fmaf(s[4 * b + e], a.scale_log2e, -lse2[e]));
-                        y[e] = x[e] * (dp[4 * b + e] - delta[e]);
-                        if (cut && qh + b * 8 + lh * 4 + e < tok0 + l32) x[e] = y[e] = 0.f;
-                    }
-                    p[b >> 1][(b & 1) * 2] = pack2<T>(x[0], x[1]); p[b >> 1][(b & 1) * 2 + 1] = pack2<T>(x[2], x[3]);
-                    t[b >> 1][(b & 1) * 2] = pack2<T>(y[0], y[1]); t[b >> 1][(b & 1) * 2 + 1] = pack2<T>(y[2], y[3]);
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = __builtin_amdgcn_exp2f(fmaf(s[4 * b + e], a.scale_log2e, -lse2[e]));
+                    y[e] = x[e] * (dp[4 * b + e] - delta[e]);
+                    if (cut && q0 + b * 8 + lh * 4 + e < tok0 + l32) x[e] = y[e] = 0.f;
                 }
-#pragma unroll
-                for (int g = 0; g < 2; ++g)
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        dv[d] = mma<T>(at.transposed(ot, half * 2 + g, d), p[g], dv[d]);
-                        dk[d] = mma<T>(at.transposed(qt, half * 2 + g, d), t[g], dk[d]);
-                    }
+                p[b >> 1][(b & 1) * 2] = pack2<T>(x[0], x[1]); p[b >> 1][(b & 1) * 2 + 1] = pack2<T>(x[2], x[3]);
+                t[b >> 1][(b & 1) * 2] = pack2<T>(y[0], y[1]); t[b >> 1][(b & 1) * 2 + 1] = pack2<T>(y[2], y[3]);
             }
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) dv[d] = mma<T>(at.transposed(ot, g, d), p[g], dv[d]);
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) dk[d] = mma<T>(at.transposed(qt, g, d), t[g], dk[d]);
         }
+        if ((q0 += 32) >= len) q0 = block0;
         if (more) park(st + 1);
     }
     __syncthreads();
@@ -566,12 +633,28 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
         __builtin_amdgcn_wave_barrier();
         put_rows<T, HD>(dv, 1.f, mine, (T*)a.dv + first * a.dv_stride + kvh * HD, a.dv_stride, n_valid, lane);
     }
-    uint64_t rows = __builtin_amdgcn_ballot_w64(there && (any_undefined(dk) || any_undefined(dv)));
-    rows = (rows | (rows >> 32)) & 0xFFFFFFFFull;
-    while (rows) {
-        const int r = __builtin_ctzll(rows);
-        rows &= rows - 1;
-        dkv_row<T, HD, PARTS>(a, row0, len, tok0 + r, kvh, h0, h1, part, lane);
+    // A weight of 0 times an infinite or undefined value of a row before the token: of the wave's first 32 rows only.  Tokens behind such a row are computed alone, but
+    // for those that are undefined anyway, before (or at) the last row whose weights are.
+    uint64_t toks = __builtin_amdgcn_ballot_w64(there && (any_undefined(dk) || any_undefined(dv)));
+    toks = (toks | (toks >> 32)) & 0xFFFFFFFFull;
+    if (!toks) return;
+    uint64_t odd = 0;
+    int last = -1;
+    for (int h = h0; h < h1; ++h) {
+        const size_t row = first + l32;
+        odd |= __builtin_amdgcn_ballot_w64(there && (not_finite<T, HD>((const T*)a.q + row * a.q_stride + h * HD) || not_finite<T, HD>((const T*)a.dout + row * a.dout_stride + h * HD)));
+        for (int i0 = tok0; i0 < len; i0 += 64) {
+            const int i = i0 + lane;
+            const float x = i < len ? a.lse[(size_t)h * a.n_rows + row0 + i] : 0.f;
+            const uint64_t none = __builtin_amdgcn_ballot_w64(x != x);
+            if (none) last = max(last, i0 + 63 - __builtin_clzll(none));
+        }
+    }
+    odd &= 0xFFFFFFFFull;
+    while (toks) {
+        const int r = __builtin_ctzll(toks);
+        toks &= toks - 1;
+        if (tok0 + r > last && (odd & ((1ull << r) - 1))) dkv_row<T, HD, PARTS>(a, row0, len, tok0 + r, kvh, h0, h1, part, lane);
     }
 }
 
@@ -595,9 +678,13 @@ __global__ __launch_bounds__(256) void pack_join_kernel(PackArgs a, int width) {
 
 constexpr int kMostItems = 65535;                 // of a launch: its second dimension
 
-hipError_t in_launches(void (*kernel)(PackArgs), PackArgs a, int items, int wide, hipStream_t s) {
+hipError_t in_launches(void (*kernel)(PackArgs), PackArgs a, int items, int wide, int lds, hipStream_t s) {
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
     for (a.first_item = 0; a.first_item < items; a.first_item += kMostItems) {
-        hipLaunchKernelGGL(kernel, dim3(wide, items - a.first_item < kMostItems ? items - a.first_item : kMostItems), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(kernel, dim3(wide, items - a.first_item < kMostItems ? items - a.first_item : kMostItems), dim3(256), lds, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -605,12 +692,12 @@ hipError_t in_launches(void (*kernel)(PackArgs), PackArgs a, int items, int wide
 }
 
 template <class T, int HD> hipError_t forward_impl(const PackArgs& a, hipStream_t s) {
-    return in_launches(pack_forward_kernel<T, HD>, a, a.n_q_items, a.n_kv_heads, s);
+    return in_launches(pack_forward_kernel<T, HD>, a, a.n_q_items, a.n_kv_heads, 0, s);
 }
 template <class T, int HD> hipError_t backward_impl(const PackArgs& a, hipStream_t s) {
-    hipError_t e = in_launches(pack_dq_kernel<T, HD>, a, a.n_q_items, a.n_kv_heads, s);
+    hipError_t e = in_launches(pack_dq_kernel<T, HD>, a, a.n_q_items, a.n_kv_heads, 0, s);
     if (e != hipSuccess) return e;
-    e = in_launches(a.parts > 1 ? pack_dkv_kernel<T, HD, true> : pack_dkv_kernel<T, HD, false>, a, a.n_k_items, a.n_kv_heads * a.parts, s);
+    e = in_launches(a.parts > 1 ? pack_dkv_kernel<T, HD, true> : pack_dkv_kernel<T, HD, false>, a, a.n_k_items, a.n_kv_heads * a.parts, kDkvBytes<HD>, s);
     if (e != hipSuccess || a.parts == 1) return e;
     const size_t vecs = (size_t)a.n_rows * a.n_kv_heads * HD / 4;
     hipLaunchKernelGGL((pack_join_kernel<T>), dim3((unsigned)((vecs + 255) / 256)), dim3(256), 0, s, a, a.n_kv_heads * HD);
