@@ -1,5 +1,7 @@
 // What a decoder block has beside its matrix products and its attention, for the learner: addition to the residual stream with RMSNorm, and the
 // norm and rotation of the q and k heads, each forward and backward.
+#include <algorithm>
+
 #include "spiral_internal.h"
 
 namespace spiral {
@@ -9,211 +11,476 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kE4m3Least = 1e-30f;          // a row whose largest |out| is no more holds zeros
 
-template <int N> __device__ __forceinline__ float group_sum(float v, float* s) {       // of N waves, in every thread
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int w = 0; w < N; ++w) v += s[w];
-    return v;
+// Sums and maxima over a wave without a trip through LDS: rotations within rows of 16 lanes, then exchanges of rows.  Every lane adds the same pairs, so all have
+// the same bits.
+template <int N> __device__ __forceinline__ float row_ror(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xF, 0xF, false)); }
+template <class Op> __device__ __forceinline__ float over_wave(float v, Op op) {
+    v = op(v, row_ror<8>(v));
+    v = op(v, row_ror<4>(v));
+    v = op(v, row_ror<2>(v));
+    v = op(v, row_ror<1>(v));
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+    v = op(__int_as_float(r[0]), __int_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return op(__int_as_float(r[0]), __int_as_float(r[1]));
 }
-template <int N> __device__ __forceinline__ float group_max(float v, float* s) {       // NaN where any is
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { const float x = __shfl_xor(v, o, 64); v = v != v || x != x ? NAN : fmaxf(v, x); }
+struct Add { __device__ __forceinline__ float operator()(float x, float y) const { return x + y; } };
+struct Most { __device__ __forceinline__ float operator()(float x, float y) const { return x != x || y != y ? NAN : fmaxf(x, y); } };      // undefined where any is
+// over the WAVES waves that share a row
+template <int WAVES, class Op> __device__ __forceinline__ float over_row(float v, float* s, Op op) {
+    v = over_wave(v, op);
+    if (WAVES == 1) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
     __syncthreads();
     v = s[0];
 #pragma unroll
-    for (int w = 1; w < N; ++w) v = v != v || s[w] != s[w] ? NAN : fmaxf(v, s[w]);
+    for (int w = 1; w < WAVES; ++w) v = op(v, s[w]);
     return v;
 }
 
 __device__ __forceinline__ uint8_t to_e4m3(float v) { return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xFF); }
+__device__ __forceinline__ uint32_t to_e4m3x4(const float* v) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
+}
+// what a row's outputs are multiplied by to be encoded, and its codes to be decoded; undefined where the row's largest is infinite or undefined
+__device__ __forceinline__ float code_factor(float most) { return most <= kE4m3Least ? 0.f : most < INFINITY ? 448.f / most : NAN; }
+__device__ __forceinline__ float code_scale(float most) { return most <= kE4m3Least ? 0.f : most < INFINITY ? most / 448.f : NAN; }
 
-// a row a workgroup, swept three times
-template <class T>
-__global__ __launch_bounds__(kThreads) void add_norm_rows_kernel(NormRowsArgs a) {
-    __shared__ float s[kThreads / 64];
-    const long long r = blockIdx.x;
-    const T* x = (const T*)a.x + r * a.x_stride;
-    const T* res = a.residual ? (const T*)a.residual + r * a.residual_stride : nullptr;
-    auto sum_at = [&](int c) { return (float)x[c] + (res ? (float)res[c] : 0.f); };
-    float sq = 0.f;
-    for (int c = threadIdx.x; c < a.d; c += kThreads) { const float h = sum_at(c); sq = fmaf(h, h, sq); }
-    const float rstd = 1.f / sqrtf(group_sum<kThreads / 64>(sq, s) / a.d + a.eps);
-    if (a.rstd && threadIdx.x == 0) a.rstd[r] = rstd;
-    float inv = 0.f;
-    if (a.out_scale) {
-        float most = 0.f;
-        for (int c = threadIdx.x; c < a.d; c += kThreads) {
-            const float y = fabsf(sum_at(c) * rstd * a.gain[c]);
-            most = most != most || y != y ? NAN : fmaxf(most, y);
+// Eight neighbouring elements, aligned to one: the wide accesses take any address
+template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
+template <class T> using Eights = typename Eight<T>::type;
+
+// A lane's v-th eight elements of a row of d >= 8.  Those of the last v that would pass the row's end are read from d - 8 on, without a branch, and the first `skip` of
+// them (all: 8) are another lane's: they are left out of sums and not written, as their place may hold the output already.
+template <int LANES, int NV> struct Share {
+    int t, d;
+    __device__ __forceinline__ int begin(int v) const { return (v * LANES + t) * 8; }
+    __device__ __forceinline__ int at(int v) const { return v < NV - 1 ? begin(v) : min(begin(v), d - 8); }
+    __device__ __forceinline__ int skip(int v) const { return v < NV - 1 ? 0 : min(begin(v) - at(v), 8); }
+    template <class V, class E> __device__ __forceinline__ void put(E* row, int v, V x) const {
+        typedef V Any __attribute__((aligned(sizeof(E))));
+        const int n = skip(v);
+        if (n == 0) *(Any*)(row + at(v)) = x;
+        else
+#pragma unroll
+            for (int e = 1; e < 8; ++e)
+                if (e >= n) row[at(v) + e] = __builtin_bit_cast(E __attribute__((ext_vector_type(8))), x)[e];
+    }
+};
+template <class T> __device__ __forceinline__ Eights<T> eight(const T* p) { return *(const Eights<T>*)p; }
+// What a second sweep over the same values widens again: kept from the first, they would take three times the registers (16,384 rows of 3,584 bf16: 160 us and spills, now 97).
+template <class T> __device__ __forceinline__ void forget(Eights<T>& x) { asm volatile("" : "+v"(x)); }
+template <> __device__ __forceinline__ void forget<float>(Eights<float>&) {}
+
+// A row by one wave or by four, in registers: NV times eight elements a lane.  One read of what there is to read, one write; every load of a row is on its way before
+// its first element is needed.
+template <class T, bool OUT8, int WAVES, int NV>
+__global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
+    __shared__ float s[WAVES];
+    constexpr int LANES = 64 * WAVES;
+    const Share<LANES, NV> mine{(int)(threadIdx.x % LANES), a.d};
+    for (long long r = (long long)blockIdx.x * (4 / WAVES) + threadIdx.x / LANES; r < a.n_rows; r += (long long)gridDim.x * (4 / WAVES)) {
+        const T* x = (const T*)a.x + r * a.x_stride;
+        const T* res = a.residual ? (const T*)a.residual + r * a.residual_stride : nullptr;
+        Eights<T> xv[NV], rv[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            xv[v] = eight(x + mine.at(v));
+            if (res) rv[v] = eight(res + mine.at(v));
         }
-        most = group_max<kThreads / 64>(most, s);
-        const bool some = !(most <= kE4m3Least);
-        if (!(most < INFINITY)) most = NAN;
-        inv = some ? 448.f / most : 0.f;
-        if (threadIdx.x == 0) a.out_scale[r] = some ? most / 448.f : 0.f;
-    }
-    for (int c = threadIdx.x; c < a.d; c += kThreads) {
-        const float h = sum_at(c), y = h * rstd * a.gain[c];
-        if (a.sum) ((T*)a.sum)[r * a.sum_stride + c] = (T)h;
-        if (a.out_scale) ((uint8_t*)a.out)[r * a.out_stride + c] = to_e4m3(y * inv);
-        else ((T*)a.out)[r * a.out_stride + c] = (T)y;
+        float h[NV][8], sq = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[v][e] = (float)xv[v][e] + (res ? (float)rv[v][e] : 0.f);
+                const float in = e >= mine.skip(v) ? h[v][e] : 0.f;
+                sq = fmaf(in, in, sq);
+            }
+        const float rstd = 1.f / sqrtf(over_row<WAVES>(sq, s, Add()) / a.d + a.eps);
+        if (a.rstd && mine.t == 0) a.rstd[r] = rstd;
+        float most = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if (a.sum) {
+                Eights<T> y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = (T)h[v][e];
+                mine.put((T*)a.sum + r * a.sum_stride, v, y);
+            }
+            const Eights<float> g = eight(a.gain + mine.at(v));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[v][e] *= rstd * g[e];
+                if (OUT8) most = e >= mine.skip(v) ? Most()(most, fabsf(h[v][e])) : most;
+            }
+            if (!OUT8) {
+                Eights<T> y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = (T)h[v][e];
+                mine.put((T*)a.out + r * a.out_stride, v, y);
+            }
+        }
+        if (OUT8) {
+            most = over_row<WAVES>(most, s, Most());
+            const float inv = code_factor(most);
+            if (mine.t == 0) a.out_scale[r] = code_scale(most);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[v][e] *= inv;
+                typedef uint32_t Codes __attribute__((ext_vector_type(2)));
+                mine.put((uint8_t*)a.out + r * a.out_stride, v, Codes{to_e4m3x4(h[v]), to_e4m3x4(h[v] + 4)});
+            }
+        }
     }
 }
 
+// rows that registers do not hold, and those of fewer than eight elements: a row a workgroup, swept three times
 template <class T>
-__global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormGradArgs a) {
+__global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a) {
     __shared__ float s[kThreads / 64];
-    const long long r = blockIdx.x;
-    const T* dy = (const T*)a.dout + r * a.dout_stride;
-    const T* h = (const T*)a.sum + r * a.sum_stride;
-    const float rstd = a.rstd[r];
-    float along = 0.f;
-    for (int c = threadIdx.x; c < a.d; c += kThreads) along = fmaf((float)dy[c] * a.gain[c], (float)h[c] * rstd, along);
-    along = group_sum<kThreads / 64>(along, s) / a.d;
-    for (int c = threadIdx.x; c < a.d; c += kThreads) {
-        float g = rstd * ((float)dy[c] * a.gain[c] - (float)h[c] * rstd * along);
-        if (a.dsum) g += (float)((const T*)a.dsum)[r * a.dsum_stride + c];
-        ((T*)a.dx)[r * a.dx_stride + c] = (T)g;
+    for (long long r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
+        const T* x = (const T*)a.x + r * a.x_stride;
+        const T* res = a.residual ? (const T*)a.residual + r * a.residual_stride : nullptr;
+        auto sum_at = [&](int c) { return (float)x[c] + (res ? (float)res[c] : 0.f); };
+        float sq = 0.f;
+        for (int c = threadIdx.x; c < a.d; c += kThreads) { const float h = sum_at(c); sq = fmaf(h, h, sq); }
+        const float rstd = 1.f / sqrtf(over_row<4>(sq, s, Add()) / a.d + a.eps);
+        if (a.rstd && threadIdx.x == 0) a.rstd[r] = rstd;
+        float inv = 0.f;
+        if (a.out_scale) {
+            float most = 0.f;
+            for (int c = threadIdx.x; c < a.d; c += kThreads) most = Most()(most, fabsf(sum_at(c) * rstd * a.gain[c]));
+            most = over_row<4>(most, s, Most());
+            inv = code_factor(most);
+            if (threadIdx.x == 0) a.out_scale[r] = code_scale(most);
+        }
+        for (int c = threadIdx.x; c < a.d; c += kThreads) {
+            const float h = sum_at(c), y = h * rstd * a.gain[c];
+            if (a.sum) ((T*)a.sum)[r * a.sum_stride + c] = (T)h;
+            if (a.out_scale) ((uint8_t*)a.out)[r * a.out_stride + c] = to_e4m3(y * inv);
+            else ((T*)a.out)[r * a.out_stride + c] = (T)y;
+        }
     }
 }
-constexpr int kGainRows = 128;                // rows of a partial sum
+
+// Gradient: rows as above, workgroups take every gridDim.x-th (group of four) and keep the gain's sums over their rows in registers.
+template <class T, int WAVES, int NV>
+__global__ __launch_bounds__(kThreads, 2) void norm_grad_kernel(NormGradArgs a) {
+    constexpr int LANES = 64 * WAVES;
+    __shared__ float s[WAVES];
+    const int d = a.d;
+    const Share<LANES, NV> mine{(int)(threadIdx.x % LANES), d};
+    float dg[NV][8] = {};
+    for (long long r = (long long)blockIdx.x * (4 / WAVES) + threadIdx.x / LANES; r < a.n_rows; r += (long long)gridDim.x * (4 / WAVES)) {
+        const T* dy = (const T*)a.dout + r * a.dout_stride;
+        const T* h = (const T*)a.sum + r * a.sum_stride;
+        const T* ds = a.dsum ? (const T*)a.dsum + r * a.dsum_stride : nullptr;
+        Eights<T> yv[NV], hv[NV], sv[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            yv[v] = eight(dy + mine.at(v));
+            hv[v] = eight(h + mine.at(v));
+            if (ds) sv[v] = eight(ds + mine.at(v));
+        }
+        const float rstd = a.rstd[r];
+        const float* gain = a.gain;
+        float along = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const Eights<float> g = eight(gain + mine.at(v));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = (float)yv[v][e] * ((float)hv[v][e] * rstd), in = e >= mine.skip(v) ? p : 0.f;
+                along = fmaf(in, g[e], along);
+                dg[v][e] += in;
+            }
+        }
+        along = over_row<WAVES>(along, s, Add()) / d;
+        asm volatile("" : "+s"(gain));            // read again, not kept, like the rest
+        T* dx = (T*)a.dx + r * a.dx_stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            forget<T>(yv[v]);
+            forget<T>(hv[v]);
+            const Eights<float> g = eight(gain + mine.at(v));
+            Eights<T> x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (T)(rstd * ((float)yv[v][e] * g[e] - (float)hv[v][e] * rstd * along) + (ds ? (float)sv[v][e] : 0.f));
+            mine.put(dx, v, x);
+        }
+    }
+    if (!a.dgain) return;
+    // the workgroup's sums: of four waves that had rows of their own, through LDS
+    __shared__ float s_gain[WAVES == 1 ? 3 * 64 * 8 : 1];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        if (WAVES == 1) {
+            const int wave = threadIdx.x >> 6, t = mine.t;
+            __syncthreads();
+            if (wave)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s_gain[((wave - 1) * 8 + e) * 64 + t] = dg[v][e];
+            __syncthreads();
+            if (wave) continue;
+#pragma unroll
+            for (int w = 0; w < 3; ++w)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dg[v][e] += s_gain[(w * 8 + e) * 64 + t];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= mine.skip(v)) a.part[(size_t)blockIdx.x * d + mine.at(v) + e] = dg[v][e];
+    }
+}
+// Sums over the parts: 32 columns a workgroup, its 32 groups of 32 lanes take every 32nd part.
+__global__ __launch_bounds__(1024) void add_parts_kernel(const float* part, long long parts, int d, float* out, float* out2, int split) {
+    __shared__ float s[32][33];
+    const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float x = 0.f;
+    if (c < d)
+#pragma unroll 8
+        for (long long p = g; p < parts; p += 32) x += part[(size_t)p * d + c];
+    s[g][lane] = x;
+    __syncthreads();
+    if (g || c >= d) return;
+    x = 0.f;
+#pragma unroll
+    for (int w = 0; w < 32; ++w) x += s[w][lane];
+    float* to = c < split ? out : out2;
+    if (to) to[c < split ? c : c - split] = x;
+}
+
+// rows that registers do not hold
+template <class T>
+__global__ __launch_bounds__(kThreads) void norm_grad_long_kernel(NormGradArgs a) {
+    __shared__ float s[kThreads / 64];
+    for (long long r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
+        const T* dy = (const T*)a.dout + r * a.dout_stride;
+        const T* h = (const T*)a.sum + r * a.sum_stride;
+        const float rstd = a.rstd[r];
+        float along = 0.f;
+        for (int c = threadIdx.x; c < a.d; c += kThreads) along = fmaf((float)dy[c] * a.gain[c], (float)h[c] * rstd, along);
+        along = over_row<4>(along, s, Add()) / a.d;
+        for (int c = threadIdx.x; c < a.d; c += kThreads) {
+            float g = rstd * ((float)dy[c] * a.gain[c] - (float)h[c] * rstd * along);
+            if (a.dsum) g += (float)((const T*)a.dsum)[r * a.dsum_stride + c];
+            ((T*)a.dx)[r * a.dx_stride + c] = (T)g;
+        }
+    }
+}
+// their gain's sums, before dx may overwrite what they are made of: every gridDim.y-th row a part
 template <class T>
 __global__ __launch_bounds__(kThreads) void gain_part_kernel(NormGradArgs a) {
     const int c = blockIdx.x * kThreads + threadIdx.x;
     if (c >= a.d) return;
-    const long long r0 = (long long)blockIdx.y * kGainRows, r1 = r0 + kGainRows < a.n_rows ? r0 + kGainRows : a.n_rows;
     float g = 0.f;
-    for (long long r = r0; r < r1; ++r) g = fmaf((float)((const T*)a.dout)[r * a.dout_stride + c], (float)((const T*)a.sum)[r * a.sum_stride + c] * a.rstd[r], g);
+    for (long long r = blockIdx.y; r < a.n_rows; r += gridDim.y)
+        g = fmaf((float)((const T*)a.dout)[r * a.dout_stride + c], (float)((const T*)a.sum)[r * a.sum_stride + c] * a.rstd[r], g);
     a.part[(size_t)blockIdx.y * a.d + c] = g;
 }
-__global__ __launch_bounds__(kThreads) void add_parts_kernel(const float* part, long long parts, int d, float* out) {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= d) return;
-    float g = 0.f;
-    for (long long p = 0; p < parts; ++p) g += part[(size_t)p * d + c];
-    out[c] = g;
-}
 
-// a head a wave: lane c holds the pair (c, c + HD / 2)
-template <class T, int HD>
-__global__ __launch_bounds__(kThreads) void norm_rope_kernel(RopeArgs a, RopeFreq f) {
-    const int lane = threadIdx.x & 63, heads = a.side[0].heads + a.side[1].heads;
-    const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit >= a.n_rows * heads) return;
-    const long long r = unit / heads;
-    int h = (int)(unit % heads);
-    const bool second = h >= a.side[0].heads;
-    const RopeSide& s = a.side[second];
-    if (second) h -= a.side[0].heads;
-    const bool in = lane < HD / 2;
-    const int c = in ? lane : 0;
-    const T* x = (const T*)s.x + r * s.x_stride + h * HD;
-    float lo = in ? (float)x[c] : 0.f, hi = in ? (float)x[c + HD / 2] : 0.f;
-    if (s.gain) {
-        const float rstd = 1.f / sqrtf(wave_sum(fmaf(lo, lo, hi * hi)) / HD + a.eps);
-        lo *= rstd * s.gain[c];
-        hi *= rstd * s.gain[c + HD / 2];
-    }
-    double sn, cs;
-    sincos((double)a.positions[r] * f.inv_freq[c], &sn, &cs);
-    const float2 y = rotate_pair(lo, hi, (float)cs, (float)sn);
-    T* out = (T*)s.out + r * s.out_stride + h * HD;
-    if (in) { out[c] = (T)y.x; out[c + HD / 2] = (T)y.y; }
-}
-
-constexpr int kRopeParts = 1024;              // workgroups of the backward kernel at most: partial sums of the gains' gradients
-template <class T, int HD>
-__global__ __launch_bounds__(kThreads) void norm_rope_grad_kernel(RopeArgs a, RopeFreq f) {
-    __shared__ float s_part[4][2 * HD];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = a.side[0].heads + a.side[1].heads;
-    const bool in = lane < HD / 2;
-    const int c = in ? lane : 0;
-    float dg[2][2] = {};
-    for (long long unit = (long long)blockIdx.x * 4 + wave; unit < a.n_rows * heads; unit += (long long)gridDim.x * 4) {
-        const long long r = unit / heads;
-        int h = (int)(unit % heads);
-        const bool second = h >= a.side[0].heads;
-        const RopeSide& s = a.side[second];
-        if (second) h -= a.side[0].heads;
-        const T* dy = (const T*)s.dout + r * s.dout_stride + h * HD;
-        double sn, cs;
-        sincos((double)a.positions[r] * f.inv_freq[c], &sn, &cs);
-        float2 g = rotate_pair((float)dy[c], (float)dy[c + HD / 2], (float)cs, -(float)sn);
-        if (s.gain) {
-            const T* x = (const T*)s.x + r * s.x_stride + h * HD;
-            float lo = in ? (float)x[c] : 0.f, hi = in ? (float)x[c + HD / 2] : 0.f;
-            const float rstd = 1.f / sqrtf(wave_sum(fmaf(lo, lo, hi * hi)) / HD + a.eps);
-            lo *= rstd; hi *= rstd;
-            if (second) { dg[1][0] = fmaf(g.x, lo, dg[1][0]); dg[1][1] = fmaf(g.y, hi, dg[1][1]); }
-            else        { dg[0][0] = fmaf(g.x, lo, dg[0][0]); dg[0][1] = fmaf(g.y, hi, dg[0][1]); }
-            g.x *= s.gain[c]; g.y *= s.gain[c + HD / 2];
-            const float along = wave_sum(in ? fmaf(g.x, lo, g.y * hi) : 0.f) / HD;
-            g.x = rstd * (g.x - lo * along);
-            g.y = rstd * (g.y - hi * along);
-        }
-        T* out = (T*)s.out + r * s.out_stride + h * HD;
-        if (in) { out[c] = (T)g.x; out[c + HD / 2] = (T)g.y; }
-    }
-    if (!a.part) return;
-    if (in) {
+// Cosine and sine of the eight angles position * freq of a lane, freq in turns: the turns' fraction and its quarter in 64 bits, then the Taylor polynomials of the at most
+// pi / 4 that is left, off by 2^-29.
+__device__ __forceinline__ void turn8(int position, const double* freq, float (&cs)[8], float (&sn)[8]) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) { s_part[wave][i * HD + c] = dg[i][0]; s_part[wave][i * HD + c + HD / 2] = dg[i][1]; }
+    for (int e = 0; e < 8; ++e) {
+        const double turns = (double)position * freq[e], quarters = turns * 4.0, q = rint(quarters);
+        const float x = (float)(quarters - q) * 1.57079632679489662f, x2 = x * x;
+        const float si = fmaf(x * x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
+        const float co = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+        const int k = (int)(long long)q & 3;
+        const float c0 = k & 1 ? si : co, s0 = k & 1 ? co : si;
+        cs[e] = k == 1 || k == 2 ? -c0 : c0;
+        sn[e] = k & 2 ? -s0 : s0;
     }
+}
+// over the HD / 16 lanes that share a head, bit for bit the same in each: exchanges within four lanes, then of four with four
+template <int HD> __device__ __forceinline__ float over_head(float v) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, false));
+    if (HD >= 64) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, false));
+    if (HD >= 128) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, false));
+    return v;
+}
+
+// A row a wave.  HD / 16 lanes share a head: each has eight pairs (c, c + HD / 2) of neighbouring c, whose angles it evaluates once for all heads of the row.
+template <class T, int HD, bool GRAD>
+__global__ __launch_bounds__(kThreads) void norm_rope_kernel(RopeArgs a, RopeFreq f) {
+    constexpr int LANES = HD / 16, SLOTS = 64 / LANES;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (lane % LANES) * 8, slot = lane / LANES;
+    float gain[2][2][8], dg[2][2][8];
+    double freq[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) freq[e] = f.inv_freq[c + e];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            gain[i][0][e] = a.side[i].gain ? a.side[i].gain[c + e] : 1.f;
+            gain[i][1][e] = a.side[i].gain ? a.side[i].gain[c + HD / 2 + e] : 1.f;
+            dg[i][0][e] = dg[i][1][e] = 0.f;
+        }
+    for (long long r = (long long)blockIdx.x * 4 + wave; r < a.n_rows; r += (long long)gridDim.x * 4) {
+        float cs[8], sn[8];
+        turn8(a.positions[r], freq, cs, sn);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const RopeSide& s = a.side[i];
+            const T* x = (const T*)s.x + r * s.x_stride + c;
+            const T* dy = (const T*)s.dout + r * s.dout_stride + c;
+            T* out = (T*)s.out + r * s.out_stride + c;
+            const bool norm = s.gain != nullptr;
+            for (int h = slot; h < s.heads; h += SLOTS) {
+                Eights<T> lo, hi, ylo, yhi;
+                if (!GRAD || norm) lo = *(const Eights<T>*)(x + h * HD), hi = *(const Eights<T>*)(x + h * HD + HD / 2);
+                if (GRAD) ylo = *(const Eights<T>*)(dy + h * HD), yhi = *(const Eights<T>*)(dy + h * HD + HD / 2);
+                float rstd = 1.f;
+                if (norm) {
+                    float sq = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sq = fmaf((float)lo[e], (float)lo[e], fmaf((float)hi[e], (float)hi[e], sq));
+                    rstd = 1.f / sqrtf(over_head<HD>(sq) / HD + a.eps);
+                }
+                Eights<T> olo, ohi;
+                if (!GRAD) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float p = (float)lo[e], q = (float)hi[e];
+                        if (norm) p *= rstd * gain[i][0][e], q *= rstd * gain[i][1][e];
+                        const float2 y = rotate_pair(p, q, cs[e], sn[e]);
+                        olo[e] = (T)y.x; ohi[e] = (T)y.y;
+                    }
+                } else {
+                    float p[8], q[8], along = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 g = rotate_pair((float)ylo[e], (float)yhi[e], cs[e], -sn[e]);
+                        p[e] = g.x; q[e] = g.y;
+                        if (norm) {
+                            const float u = (float)lo[e] * rstd, w = (float)hi[e] * rstd;
+                            dg[i][0][e] = fmaf(g.x, u, dg[i][0][e]);
+                            dg[i][1][e] = fmaf(g.y, w, dg[i][1][e]);
+                            p[e] *= gain[i][0][e]; q[e] *= gain[i][1][e];
+                            along = fmaf(p[e], u, fmaf(q[e], w, along));
+                        }
+                    }
+                    if (norm) along = over_head<HD>(along) / HD;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        olo[e] = (T)(norm ? rstd * (p[e] - (float)lo[e] * rstd * along) : p[e]);
+                        ohi[e] = (T)(norm ? rstd * (q[e] - (float)hi[e] * rstd * along) : q[e]);
+                    }
+                }
+                *(Eights<T>*)(out + h * HD) = olo;
+                *(Eights<T>*)(out + h * HD + HD / 2) = ohi;
+            }
+        }
+    }
+    if (!GRAD || !a.part) return;
+    // the gains' sums: over the slots of a wave, then the waves
+    __shared__ float s_part[4][2 * HD];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float x = dg[i][b][e];
+#pragma unroll
+                for (int o = LANES; o < 64; o <<= 1) x += __shfl_xor(x, o, 64);
+                if (slot == 0) s_part[wave][i * HD + b * (HD / 2) + c + e] = x;
+            }
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * HD; e += kThreads)
-        a.part[(size_t)blockIdx.x * 2 * HD + e] = s_part[0][e] + s_part[1][e] + s_part[2][e] + s_part[3][e];
-}
-__global__ __launch_bounds__(kThreads) void rope_gain_kernel(const float* part, int parts, int hd, float* dq, float* dk) {
-    const int e = threadIdx.x;
-    if (e >= 2 * hd) return;
-    float g = 0.f;
-    for (int p = 0; p < parts; ++p) g += part[(size_t)p * 2 * hd + e];
-    float* to = e < hd ? dq : dk;
-    if (to) to[e % hd] = g;
+    if (threadIdx.x < 2 * HD)
+        a.part[(size_t)blockIdx.x * 2 * HD + threadIdx.x] = s_part[0][threadIdx.x] + s_part[1][threadIdx.x] + s_part[2][threadIdx.x] + s_part[3][threadIdx.x];
 }
 
-int rope_grad_blocks(long long n_rows, int heads) {
-    const long long units = (n_rows * heads + 3) / 4;
-    return (int)(units < kRopeParts ? units : kRopeParts);
+// ------------------------------------------------------------------------------------------------ launches
+// A wave holds rows of up to kMostVecs times 512 elements (the gradient, which has three rows and a sum to hold, fewer: 3,584 bf16 by one wave 97 us and
+// by four 98, but 4,096 by one spill), four waves, which also take shorter ones where there are few rows, four times as many.
+constexpr int kFewRows = 2048;
+constexpr long long kMostBlocks = 1 << 22;    // of a launch: workgroups of more rows take several
+template <class T> constexpr int kMostVecs = sizeof(T) == 4 ? 4 : 8;
+template <class T> constexpr int kMostGradVecs = sizeof(T) == 4 ? 4 : 6;
+int norm_waves(long long n_rows, int d, int most_vecs) {      // 0: not in registers (fewer than eight elements neither)
+    return d < 8 || d > 4 * 512 * most_vecs ? 0 : d > 512 * most_vecs || n_rows < kFewRows ? 4 : 1;
+}
+constexpr int kGradBlocks = 512, kLongParts = 128;
+template <class T> long long norm_grad_parts(long long n_rows, int d) {
+    const int waves = norm_waves(n_rows, d, kMostGradVecs<T>);
+    return std::min<long long>(waves == 1 ? (n_rows + 3) / 4 : n_rows, waves ? kGradBlocks : kLongParts);
+}
+unsigned at_most(long long blocks, long long most) { return (unsigned)(blocks < most ? blocks : most); }
+
+template <class T, bool OUT8, int WAVES> void add_norm_rows(const NormRowsArgs& a, hipStream_t s) {
+    const dim3 grid(at_most((a.n_rows + 4 / WAVES - 1) / (4 / WAVES), kMostBlocks)), block(kThreads);
+    switch ((a.d + 512 * WAVES - 1) / (512 * WAVES)) {
+        case 1: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 1>), grid, block, 0, s, a); return;
+        case 2: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 2>), grid, block, 0, s, a); return;
+        case 3: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 3>), grid, block, 0, s, a); return;
+        case 4: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 4>), grid, block, 0, s, a); return;
+        case 5: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 5>), grid, block, 0, s, a); return;
+        case 6: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 6>), grid, block, 0, s, a); return;
+        case 7: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 7>), grid, block, 0, s, a); return;
+        case 8: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 8>), grid, block, 0, s, a); return;
+    }
+}
+template <class T> hipError_t add_norm_of(const NormRowsArgs& a, hipStream_t s) {
+    const int waves = norm_waves(a.n_rows, a.d, kMostVecs<T>);
+    const bool out8 = a.out_scale != nullptr;
+    if (!waves) hipLaunchKernelGGL((add_norm_long_kernel<T>), dim3(at_most(a.n_rows, kMostBlocks)), dim3(kThreads), 0, s, a);
+    else if (waves == 1) { if (out8) add_norm_rows<T, true, 1>(a, s); else add_norm_rows<T, false, 1>(a, s); }
+    else if (out8) add_norm_rows<T, true, 4>(a, s);
+    else add_norm_rows<T, false, 4>(a, s);
+    return hipGetLastError();
 }
 
-template <class T> hipError_t norm_grad_impl(const NormGradArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((norm_grad_kernel<T>), dim3((unsigned)a.n_rows), dim3(kThreads), 0, s, a);
-    hipError_t e = hipGetLastError();
+template <class T, int WAVES> void norm_grad_rows(const NormGradArgs& a, unsigned blocks, hipStream_t s) {
+    const dim3 grid(blocks), block(kThreads);
+    switch ((a.d + 512 * WAVES - 1) / (512 * WAVES)) {
+        case 1: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 1>), grid, block, 0, s, a); return;
+        case 2: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 2>), grid, block, 0, s, a); return;
+        case 3: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 3>), grid, block, 0, s, a); return;
+        case 4: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 4>), grid, block, 0, s, a); return;
+        case 5: if constexpr (kMostGradVecs<T> > 4) hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 5>), grid, block, 0, s, a); return;
+        case 6: if constexpr (kMostGradVecs<T> > 4) hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 6>), grid, block, 0, s, a); return;
+    }
+}
+template <class T> hipError_t norm_grad_of(const NormGradArgs& a, hipStream_t s) {
+    const int waves = norm_waves(a.n_rows, a.d, kMostGradVecs<T>);
+    const long long parts = norm_grad_parts<T>(a.n_rows, a.d);
+    if (!waves) {
+        if (a.dgain) hipLaunchKernelGGL((gain_part_kernel<T>), dim3((a.d + kThreads - 1) / kThreads, (unsigned)parts), dim3(kThreads), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((norm_grad_long_kernel<T>), dim3(at_most(a.n_rows, kMostBlocks)), dim3(kThreads), 0, s, a);
+    } else if (waves == 1) norm_grad_rows<T, 1>(a, (unsigned)parts, s);
+    else norm_grad_rows<T, 4>(a, (unsigned)parts, s);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.dgain) return e;
-    const int cols = (a.d + kThreads - 1) / kThreads;
-    const long long parts = (a.n_rows + kGainRows - 1) / kGainRows;
-    if (parts > 65535) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gain_part_kernel<T>), dim3(cols, (unsigned)parts), dim3(kThreads), 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(add_parts_kernel, dim3(cols), dim3(kThreads), 0, s, a.part, parts, a.d, a.dgain);
+    hipLaunchKernelGGL(add_parts_kernel, dim3((a.d + 31) / 32), dim3(1024), 0, s, a.part, parts, a.d, a.dgain, nullptr, a.d);
     return hipGetLastError();
 }
 
-template <class T, int HD> hipError_t rope_impl(const RopeArgs& a, const RopeFreq& f, hipStream_t s) {
-    const long long blocks = (a.n_rows * (a.side[0].heads + a.side[1].heads) + 3) / 4;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((norm_rope_kernel<T, HD>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, f);
-    return hipGetLastError();
-}
-template <class T, int HD> hipError_t rope_grad_impl(const RopeArgs& a, const RopeFreq& f, hipStream_t s) {
-    const int blocks = rope_grad_blocks(a.n_rows, a.side[0].heads + a.side[1].heads);
-    hipLaunchKernelGGL((norm_rope_grad_kernel<T, HD>), dim3(blocks), dim3(kThreads), 0, s, a, f);
+constexpr int kRopeBlocks = 512;              // of the gradient: as many parts
+int rope_grad_blocks(long long n_rows) { return (int)at_most((n_rows + 3) / 4, kRopeBlocks); }
+
+template <class T, int HD> hipError_t rope_impl(const RopeArgs& a, const RopeFreq& f, bool grad, hipStream_t s) {
+    if (!grad) {
+        hipLaunchKernelGGL((norm_rope_kernel<T, HD, false>), dim3(at_most((a.n_rows + 3) / 4, kMostBlocks)), dim3(kThreads), 0, s, a, f);
+        return hipGetLastError();
+    }
+    const int blocks = rope_grad_blocks(a.n_rows);
+    hipLaunchKernelGGL((norm_rope_kernel<T, HD, true>), dim3(blocks), dim3(kThreads), 0, s, a, f);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
-    hipLaunchKernelGGL(rope_gain_kernel, dim3(1), dim3(kThreads), 0, s, a.part, blocks, HD, a.side[0].dgain, a.side[1].dgain);
+    hipLaunchKernelGGL(add_parts_kernel, dim3(2 * HD / 32), dim3(1024), 0, s, a.part, (long long)blocks, 2 * HD, a.side[0].dgain, a.side[1].dgain, HD);
     return hipGetLastError();
 }
 template <class T> hipError_t rope_of(const RopeArgs& a, const RopeFreq& f, int hd, bool grad, hipStream_t s) {
-    if (hd == 32) return grad ? rope_grad_impl<T, 32>(a, f, s) : rope_impl<T, 32>(a, f, s);
-    if (hd == 64) return grad ? rope_grad_impl<T, 64>(a, f, s) : rope_impl<T, 64>(a, f, s);
-    return grad ? rope_grad_impl<T, 128>(a, f, s) : rope_impl<T, 128>(a, f, s);
+    return hd == 32 ? rope_impl<T, 32>(a, f, grad, s) : hd == 64 ? rope_impl<T, 64>(a, f, grad, s) : rope_impl<T, 128>(a, f, grad, s);
 }
 hipError_t rope_any(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, bool grad, hipStream_t s) {
     return dtype == SPIRAL_DTYPE_FP32 ? rope_of<float>(a, f, hd, grad, s) : dtype == SPIRAL_DTYPE_BF16 ? rope_of<__bf16>(a, f, hd, grad, s) : rope_of<_Float16>(a, f, hd, grad, s);
@@ -222,18 +489,14 @@ hipError_t rope_any(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, boo
 }  // namespace
 
 hipError_t launch_add_norm_rows(const NormRowsArgs& a, int dtype, hipStream_t s) {
-    const dim3 grid((unsigned)a.n_rows), block(kThreads);
-    if (dtype == SPIRAL_DTYPE_FP32) hipLaunchKernelGGL((add_norm_rows_kernel<float>), grid, block, 0, s, a);
-    else if (dtype == SPIRAL_DTYPE_BF16) hipLaunchKernelGGL((add_norm_rows_kernel<__bf16>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((add_norm_rows_kernel<_Float16>), grid, block, 0, s, a);
-    return hipGetLastError();
+    return dtype == SPIRAL_DTYPE_FP32 ? add_norm_of<float>(a, s) : dtype == SPIRAL_DTYPE_BF16 ? add_norm_of<__bf16>(a, s) : add_norm_of<_Float16>(a, s);
 }
-size_t norm_grad_workspace_bytes(long long n_rows, int d) { return (size_t)((n_rows + kGainRows - 1) / kGainRows) * d * 4; }
+size_t norm_grad_workspace_bytes(long long n_rows, int d) { return (size_t)std::min<long long>(n_rows, kGradBlocks) * d * 4; }      // of any type
 hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, hipStream_t s) {
-    return dtype == SPIRAL_DTYPE_FP32 ? norm_grad_impl<float>(a, s) : dtype == SPIRAL_DTYPE_BF16 ? norm_grad_impl<__bf16>(a, s) : norm_grad_impl<_Float16>(a, s);
+    return dtype == SPIRAL_DTYPE_FP32 ? norm_grad_of<float>(a, s) : dtype == SPIRAL_DTYPE_BF16 ? norm_grad_of<__bf16>(a, s) : norm_grad_of<_Float16>(a, s);
 }
 hipError_t launch_norm_rope(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, hipStream_t s) { return rope_any(a, f, dtype, hd, false, s); }
-size_t norm_rope_grad_workspace_bytes(long long n_rows, int n_heads, int hd) { return (size_t)rope_grad_blocks(n_rows, n_heads) * 2 * hd * 4; }
+size_t norm_rope_grad_workspace_bytes(long long n_rows, int hd) { return (size_t)rope_grad_blocks(n_rows) * 2 * hd * 4; }
 hipError_t launch_norm_rope_grad(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, hipStream_t s) { return rope_any(a, f, dtype, hd, true, s); }
 
 }  // namespace spiral

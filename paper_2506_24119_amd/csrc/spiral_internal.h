@@ -307,8 +307,9 @@ struct RopeArgs {
     float eps;
     float* part;                              // backward: partial sums of the gains' gradients
 };
+// (frequencies in turns a position here, not in radians)
 hipError_t launch_norm_rope(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, hipStream_t s);
-size_t norm_rope_grad_workspace_bytes(long long n_rows, int n_heads, int hd);
+size_t norm_rope_grad_workspace_bytes(long long n_rows, int hd);
 hipError_t launch_norm_rope_grad(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, hipStream_t s);
 
 // AdamW over many tensors
