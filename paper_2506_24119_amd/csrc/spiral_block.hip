@@ -23,10 +23,12 @@ struct spiral_attention_plan {
 // Workgroups of a sequence: four units of 32 rows and a query head of the group, 128 tokens.
 static long long q_blocks(int len, int group) { return (((long long)len + 31) / 32 * group + 3) / 4; }
 static long long k_blocks(int len) { return ((long long)len + 127) / 128; }
-// The gradients of k and v take a workgroup 128 tokens and one kv head.  Where those are few, and the first tokens' much longer than the last's, the
-// group's heads are shared out.
-static int k_parts(long long items, int group, int n_kv_heads) {
-    const long long wanted = 2048, wgs = items * n_kv_heads;
+// The gradients of k and v take a workgroup 128 tokens and one kv head.  Where those are few, and the first tokens' much longer than the last's, the group's heads
+// are shared out (28 heads on 4, one sequence of 300 tokens: 112 -> 53 us forward and backward, of 4,000: 1,328 -> 577, of 16,001: 9.6 -> 7.8 ms), but for so few
+// stages of 32 rows that the launch that joins the parts would take longer.
+static int k_parts(long long items, int longest, int group, int n_kv_heads) {
+    const long long wanted = 1024, least_stages = 12, wgs = items * n_kv_heads;
+    if ((longest + 31) / 32 * (long long)group < least_stages) return 1;
     return (int)std::min<long long>(group, std::max<long long>(1, (wanted + wgs - 1) / wgs));
 }
 
@@ -84,7 +86,7 @@ extern "C" int spiral_attention_plan_create(const int32_t* host_lens, int B, int
     std::stable_sort(items.get() + z.q_items, at, [](const int4& x, const int4& y) { return x.y - 128ll * x.z > y.y - 128ll * y.z; });
     p->n_q_heads = n_q_heads; p->n_kv_heads = n_kv_heads; p->head_dim = head_dim;
     p->n_rows = z.rows; p->n_q_items = (int)z.q_items; p->n_k_items = (int)z.k_items;
-    p->parts = k_parts(z.k_items, group, n_kv_heads);
+    p->parts = k_parts(z.k_items, seqs[0].len, group, n_kv_heads);
     p->q_items = (const int4*)dev_mem; p->k_items = p->q_items + z.q_items;
     for (size_t t = 0; t < n_items; t += 1 << 20) {              // sizes of launch_upload are ints
         const hipError_t e = launch_upload((int32_t*)dev_mem + t * 4, (const int32_t*)(items.get() + t), (int)std::min<size_t>(1 << 20, n_items - t) * 4, (hipStream_t)stream);
