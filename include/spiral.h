@@ -376,7 +376,8 @@ int spiral_policy_gradient(const void* dev_logits, int dtype, long long row_stri
  * the sums of dk and dv also over the query heads that share the kv head.  Nothing that a position does not see reaches its results, NaN and
  * infinities included, and rows behind the last sequence are neither read nor written.  Sums and the softmax are fp32; p and t are
  * rounded to the operands' type before they are multiplied (in fp16 a t below 2^-25 is 0: scale the loss as half precision wants it), outputs
- * and gradients once at the end.  Results repeat bit for bit and do not depend on the other sequences of the call.
+ * and gradients once at the end (in fp16 what passes its range is infinite, so that a loss scale that is too large shows).  Results repeat bit for bit.  A sequence's out, lse and dq do not depend on the other sequences of the call; of dk and dv the order in which a group's
+ * heads are added follows from the call's lengths (few and long ones: some heads by workgroups of their own), so that they may differ by the rounding of fp32 sums.
  *
  * A plan holds what follows from the lengths and heads alone: one for a micro-batch serves every layer's calls, forward and backward, on any
  * streams at once (calls only read it).  host_lens is consumed before the call returns; dev_mem (spiral_attention_plan_bytes, 0 on bad

@@ -129,8 +129,10 @@ def untouched(c):
         assert (h[c.n:] == 77.0).all() and (h[:, cols:] == 77.0).all()
 
 
+# the last four: a group's heads shared out over workgroups of their own, evenly and not, beside many short sequences that are not
 SHAPES = [([1], 1, 1, 32), ([5, 0, 1, 33], 4, 2, 32), ([64, 65, 63], 2, 1, 64), ([130, 1, 31, 32], 6, 2, 128), ([257, 40], 7, 1, 128), ([0, 200, 0], 3, 3, 64),
-          ([129, 127, 128], 8, 2, 64), ([96], 16, 1, 128), ([300, 17], 5, 5, 128), ([2] * 40, 4, 4, 32), ([31, 321], 9, 3, 32), ([70, 191], 12, 4, 128)]
+          ([129, 127, 128], 8, 2, 64), ([96], 16, 1, 128), ([300, 17], 5, 5, 128), ([2] * 40, 4, 4, 32), ([31, 321], 9, 3, 32), ([70, 191], 12, 4, 128), ([500], 7, 1, 64), ([390, 3, 200], 6, 2, 128),
+          ([129] * 12, 16, 2, 32), ([700, 1, 650, 0, 33], 5, 1, 32)]
 
 
 @pytest.mark.parametrize("lens,hq,hkv,hd", SHAPES)
@@ -202,8 +204,13 @@ def test_rows_do_not_depend_on_other_sequences(sb):
             getattr(d, x).copy_(getattr(c, x)[cut])
         d.forward()
         d.backward()
-        for got, want, rows in zip(d.results(), first, (0, 1, 0, 0, 0)):
-            assert torch.equal(got, want[cut] if rows == 0 else want[:, cut])
+        for name, got, want in zip(("out", "lse", "dq", "dk", "dv"), d.results(), first):
+            want = want[:, cut] if name == "lse" else want[cut]
+            if name in ("dk", "dv"):                          # four heads' sums in another order: 2^-20 of the largest, then one rounding to 8 bits
+                assert ((got.float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 2.0 ** -20 * want.float().abs().max()).all()
+                assert (got == want).float().mean() >= 0.98
+            else:
+                assert torch.equal(got, want)
         d.free()
     c.free()
 
@@ -254,11 +261,12 @@ def test_long_sequence_against_sums_in_64_bits(sb):
     c.free()
 
 
-def test_streams_and_graphs(sb):
+@pytest.mark.parametrize("hd", [64, 128])
+def test_streams_and_graphs(sb, hd):
     """Two calls at once on two streams with one plan, then captured and replayed in turn, give what each gives alone."""
     import torch
     lens = [50, 0, 200, 129]
-    works = [Call(sb, lens, 8, 4, 64, "bfloat16", seed=21), Call(sb, lens, 8, 4, 64, "bfloat16", fused=False, seed=22)]
+    works = [Call(sb, lens, 8, 4, hd, "bfloat16", seed=21), Call(sb, lens, 8, 4, hd, "bfloat16", fused=False, seed=22)]
     sb.spiral_attention_plan_free(works[1].plan)
     works[1].plan = works[0].plan
     alone = []
