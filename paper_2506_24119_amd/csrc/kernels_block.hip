@@ -43,9 +43,10 @@ __device__ __forceinline__ uint8_t to_e4m3(float v) { return (uint8_t)(__builtin
 __device__ __forceinline__ uint32_t to_e4m3x4(const float* v) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
 }
-// what a row's outputs are multiplied by to be encoded, and its codes to be decoded; undefined where the row's largest is infinite or undefined
-__device__ __forceinline__ float code_factor(float most) { return most <= kE4m3Least ? 0.f : most < INFINITY ? 448.f / most : NAN; }
-__device__ __forceinline__ float code_scale(float most) { return most <= kE4m3Least ? 0.f : most < INFINITY ? most / 448.f : NAN; }
+// What a row's sum times gain is multiplied by to be encoded (1 / rms is in both the outputs and the largest of them, `most` times it, and left out: one rounding less next
+// to a code's border), and its codes to be decoded; undefined where the row's largest is infinite or undefined.
+__device__ __forceinline__ float code_factor(float most, float rstd) { return most * rstd <= kE4m3Least ? 0.f : most < INFINITY ? 448.f / most : NAN; }
+__device__ __forceinline__ float code_scale(float most, float rstd) { return most * rstd <= kE4m3Least ? 0.f : most < INFINITY ? most * rstd / 448.f : NAN; }
 
 // Eight neighbouring elements, aligned to one: the wide accesses take any address
 template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
@@ -112,20 +113,20 @@ __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
             const Eights<float> g = eight(a.gain + mine.at(v));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                h[v][e] *= rstd * g[e];
+                h[v][e] *= g[e];
                 if (OUT8) most = e >= mine.skip(v) ? Most()(most, fabsf(h[v][e])) : most;
             }
             if (!OUT8) {
                 Eights<T> y;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = (T)h[v][e];
+                for (int e = 0; e < 8; ++e) y[e] = (T)(h[v][e] * rstd);
                 mine.put((T*)a.out + r * a.out_stride, v, y);
             }
         }
         if (OUT8) {
             most = over_row<WAVES>(most, s, Most());
-            const float inv = code_factor(most);
-            if (mine.t == 0) a.out_scale[r] = code_scale(most);
+            const float inv = code_factor(most, rstd);
+            if (mine.t == 0) a.out_scale[r] = code_scale(most, rstd);
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
 #pragma unroll
@@ -152,16 +153,16 @@ __global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a)
         float inv = 0.f;
         if (a.out_scale) {
             float most = 0.f;
-            for (int c = threadIdx.x; c < a.d; c += kThreads) most = Most()(most, fabsf(sum_at(c) * rstd * a.gain[c]));
+            for (int c = threadIdx.x; c < a.d; c += kThreads) most = Most()(most, fabsf(sum_at(c) * a.gain[c]));
             most = over_row<4>(most, s, Most());
-            inv = code_factor(most);
-            if (threadIdx.x == 0) a.out_scale[r] = code_scale(most);
+            inv = code_factor(most, rstd);
+            if (threadIdx.x == 0) a.out_scale[r] = code_scale(most, rstd);
         }
         for (int c = threadIdx.x; c < a.d; c += kThreads) {
-            const float h = sum_at(c), y = h * rstd * a.gain[c];
+            const float h = sum_at(c), y = h * a.gain[c];
             if (a.sum) ((T*)a.sum)[r * a.sum_stride + c] = (T)h;
             if (a.out_scale) ((uint8_t*)a.out)[r * a.out_stride + c] = to_e4m3(y * inv);
-            else ((T*)a.out)[r * a.out_stride + c] = (T)y;
+            else ((T*)a.out)[r * a.out_stride + c] = (T)(y * rstd);
         }
     }
 }

@@ -460,28 +460,68 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
         delta += __shfl_xor(delta, 32, 64);
     }
     const float lse = there ? a.lse[(size_t)w.h * a.n_rows + my_row] : INFINITY, lse2 = lse * kLog2e;
-    if (there && lh == 0) a.delta[(size_t)w.h * a.n_rows + my_row] = delta;
     if (!there) delta = 0.f;
     f32x16 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = zeros();
     const int limit = w.pos0 + l32;
 
-    for (int st = 0; st < w.stages; ++st) {
+    auto arrive = [&](int st) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (st + 1 < w.stages) bring(st + 1);
-        if (st >= w.my_stages) continue;
+    };
+    auto products = [&](f32x16& s, f32x16& dp, int st, int half) {
         const char* kt = lds + (st & 1) * 2 * TB;
-        const char* vt = kt + TB;
+        s = zeros(); dp = zeros();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(kt, half, ks), qf[ks], s);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mma<T>(at.by_row(kt + TB, half, ks), df[ks], dp);
+    };
+    auto add = [&](const u32x4 (&t)[2], int st, int half) {
+        const char* kt = lds + (st & 1) * 2 * TB;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] = mma<T>(at.transposed(kt, half * 2 + g, d), t[g], acc[d]);
+    };
+    auto hidden = [&](int st, int half, int r) { return st * 64 + half * 32 + 8 * (r >> 2) + 4 * lh + (r & 3) > limit; };
+    arrive(0);
+    if (w.my_stages == 1) {
+        // All that the rows see is here, so that D can be had as sum p dp.  From `out`, whose rounding is in it, it is off by 2^-9 of what dp - D, where a
+        // row sees few tokens, nearly cancels to (dq of sequences of 2 to 20 tokens: 0.4 % off, now 0.24).  In a loop of its own: in the other one it costs that 20 %.
+        f32x16 p[2], dp[2];
+        float sum = 0.f;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            f32x16 s = zeros(), dp = zeros();
+            products(p[half], dp[half], 0, half);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(kt, half, ks), qf[ks], s);
+            for (int r = 0; r < 16; ++r) {
+                const bool hide = hidden(0, half, r);
+                p[half][r] = hide ? 0.f : __builtin_amdgcn_exp2f(fmaf(p[half][r], a.scale_log2e, -lse2));
+                dp[half][r] = hide ? 0.f : dp[half][r];
+                sum = fmaf(p[half][r], dp[half][r], sum);
+            }
+        }
+        delta = there ? sum + __shfl_xor(sum, 32, 64) : 0.f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) dp = mma<T>(at.by_row(vt, half, ks), df[ks], dp);
+        for (int half = 0; half < 2; ++half) {
+            u32x4 t[2];
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) t[r >> 3][(r >> 1) & 3] = pack2<T>(p[half][r] * (dp[half][r] - delta), p[half][r + 1] * (dp[half][r + 1] - delta));
+            add(t, 0, half);
+        }
+    }
+    const int loop_stages = w.my_stages > 1 ? w.my_stages : 0;
+    for (int st = 0; st < w.stages; ++st) {
+        if (st > 0) arrive(st);
+        if (st >= loop_stages) continue;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f32x16 s, dp;
+            products(s, dp, st, half);
             const bool cut = st * 64 + half * 32 + 31 > w.pos0;
             u32x4 t[2];
 #pragma unroll
@@ -490,18 +530,16 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     x[e] = __builtin_amdgcn_exp2f(fmaf(s[r + e], a.scale_log2e, -lse2)) * (dp[r + e] - delta);
-                    if (cut && st * 64 + half * 32 + 8 * (r >> 2) + 4 * lh + (r & 3) + e > limit) x[e] = 0.f;
+                    if (cut && hidden(st, half, r + e)) x[e] = 0.f;
                 }
                 t[r >> 3][(r >> 1) & 3] = pack2<T>(x[0], x[1]);
             }
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) acc[d] = mma<T>(at.transposed(kt, half * 2 + g, d), t[g], acc[d]);
+            add(t, st, half);
         }
     }
     __syncthreads();
     if (!w.active) return;
+    if (there && lh == 0) a.delta[(size_t)w.h * a.n_rows + my_row] = delta;          // the kernel of dk and dv takes it from there
     T* dq = (T*)a.dq + ((size_t)w.row0 + w.pos0) * a.dq_stride + w.h * HD;
     put_rows<T, HD>(acc, a.scale, lds + wave * kPutBytes<HD>, dq, a.dq_stride, w.n_valid, lane);
     uint64_t rows = __builtin_amdgcn_ballot_w64(there && lse == lse && delta == delta && any_undefined(acc));      // as in the forward kernel, of keys
