@@ -285,8 +285,9 @@ template <class T, int HD> __device__ __forceinline__ bool not_finite(const T* r
     return s != s;
 }
 
-// A workgroup's place: four units of a (sequence, kv head), a unit being 32 positions of one query head; units are counted heads first.
-struct Unit {
+// A workgroup's place: four units of a (sequence, kv head), a unit being 32 positions of one query head; units are counted heads first.  Stages of so many tokens,
+// of the workgroup and of the wave.
+template <int TOKENS> struct Unit {
     int row0, len, kvh, h, pos0, n_valid, stages, my_stages;
     bool active;
     __device__ __forceinline__ Unit(const PackArgs& a, int wave) {
@@ -298,25 +299,30 @@ struct Unit {
         h = kvh * G + (active ? u - tile * G : 0);
         pos0 = active ? tile * 32 : 0;
         n_valid = active ? min(32, len - pos0) : 0;
-        stages = (min(len, last * 32 + 32) + 63) >> 6;
-        my_stages = active ? (pos0 + n_valid + 63) >> 6 : 0;
+        stages = (last * 32 + 32 + TOKENS - 1) / TOKENS;
+        my_stages = active ? (pos0 + 32 + TOKENS - 1) / TOKENS : 0;
     }
 };
 
+// Stages of 32 tokens, of which the wave's last is the one on the diagonal.  Three workgroups share a compute unit, and what one waits for (its tiles, its barrier, the
+// matrix pipe, its exponentials) the others fill: two of them with stages of 64 tokens, the next stage's scores made under the weights of this one, took
+// 1,160 us where this takes 1,054 (16 sequences of U[1024, 4096], 32 heads on 8), 164 where 143 (24 of U[256, 1024]).
 template <class T, int HD>
-__global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
-    constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD>::BYTES;
+__global__ __launch_bounds__(256, 3) void pack_forward_kernel(PackArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD, 32>::BYTES;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TB > 4 * kPutBytes<HD> ? 4 * TB : 4 * kPutBytes<HD>];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
-    const Unit w(a, wave);
+    const Unit<32> w(a, wave);
     const T* k = (const T*)a.k + (size_t)w.row0 * a.k_stride + w.kvh * HD;
     const T* v = (const T*)a.v + (size_t)w.row0 * a.v_stride + w.kvh * HD;
-    const Bring<HD> bring_k(a.k_stride, wave, lane), bring_v(a.v_stride, wave, lane);
-    const Reads<HD> at(lane);
-    char* const vlds = lds + 2 * TB;
-    auto more_k = [&](int st) { bring_k(k + (size_t)st * 64 * a.k_stride, w.len - st * 64, lds + (st & 1) * TB, wave); };
-    auto more_v = [&](int st) { bring_v(v + (size_t)st * 64 * a.v_stride, w.len - st * 64, vlds + (st & 1) * TB, wave); };
-    more_k(0);
+    const Bring32<HD> bring_k(a.k_stride, wave, lane), bring_v(a.v_stride, wave, lane);
+    const Reads<HD, 32> at(lane);
+    auto bring = [&](int st) {
+        char* to = lds + (st & 1) * 2 * TB;
+        bring_k(k + (size_t)st * 32 * a.k_stride, w.len - st * 32, to, wave);
+        bring_v(v + (size_t)st * 32 * a.v_stride, w.len - st * 32, to + TB, wave);
+    };
+    bring(0);
     const bool there = l32 < w.n_valid;
     const size_t my_row = (size_t)w.row0 + (there ? w.pos0 + l32 : 0);
     u32x4 qf[KS];
@@ -325,36 +331,27 @@ __global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = zeros();
     float m = kLeast, l = 0.f;
-    const int limit = w.pos0 + l32;
-
-    auto second_half = [&](int st) { return st * 64 + 32 <= w.pos0 + 31; };      // whether some row sees the stage's second 32 tokens
-    auto scores = [&](f32x16 (&s)[2], int st) {
-        const char* kt = lds + (st & 1) * TB;
+    for (int st = 0; st < w.stages; ++st) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (st + 1 < w.stages) bring(st + 1);
+        if (st >= w.my_stages) continue;
+        const char* kt = lds + (st & 1) * 2 * TB;
+        f32x16 s = zeros();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (half && !second_half(st)) break;
-            s[half] = zeros();
+        for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(kt, 0, ks), qf[ks], s);
+        if (st == w.my_stages - 1) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[half] = mma<T>(at.by_row(kt, half, ks), qf[ks], s[half]);
+            for (int r = 0; r < 16; ++r)
+                if (8 * (r >> 2) + 4 * lh + (r & 3) > l32) s[r] = -INFINITY;
         }
-    };
-    // what the rows do not see of stage st, and the reference of their exponents
-    auto refer = [&](f32x16 (&s)[2], int st) {
-        if (st * 64 + 63 > w.pos0) {
+        float mx = s[0];
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (st * 64 + half * 32 + 8 * (r >> 2) + 4 * lh + (r & 3) > limit) s[half][r] = -INFINITY;
-        }
-        float mx = s[0][0];
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[half][r]);
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);
         mx = fmaxf(__int_as_float(both[0]), __int_as_float(both[1])) * a.scale_log2e;
-        if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {          // it moves only where weights would pass 2^8
+        if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {          // the reference moves only where weights would pass 2^8
             const float m_new = fmaxf(m, mx), shrink = __builtin_amdgcn_exp2f(m - m_new);
             l *= shrink;
 #pragma unroll
@@ -363,50 +360,17 @@ __global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
                 for (int r = 0; r < 16; ++r) acc[d][r] *= shrink;
             m = m_new;
         }
-    };
-    auto weigh = [&](const f32x16& s, u32x4 (&p)[2]) {
+        u32x4 p[2];
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
             const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2e, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[r + 1], a.scale_log2e, -m));
             l += x + y;
             p[r >> 3][(r >> 1) & 3] = pack2<T>(x, y);
         }
-    };
-    // Stage st's weights and products, and meanwhile the scores of the next.
-    auto step = [&](f32x16 (&s)[2], f32x16 (&next)[2], int st) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (st + 2 < w.stages) more_k(st + 2);
-        if (st + 1 < w.stages) more_v(st + 1);
-        if (st >= w.my_stages) return;
-        const char* vt = vlds + (st & 1) * TB;
-        if (st + 1 < w.my_stages) scores(next, st + 1);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (half && !second_half(st)) break;
-            u32x4 p[2];
-            weigh(s[half], p);
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) acc[d] = mma<T>(at.transposed(vt, half * 2 + g, d), p[g], acc[d]);
-        }
-        if (st + 1 < w.my_stages) refer(next, st + 1);
-    };
-    if (w.stages > 1) more_k(1);
-    more_v(0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    f32x16 s[2], next[2];
-    if (w.my_stages > 0) {
-        scores(s, 0);
-        refer(s, 0);
-    }
-    for (int st = 0; st < w.stages; st += 2) {
-        step(s, next, st);
-        if (st + 1 < w.stages) step(next, s, st + 1);
+            for (int d = 0; d < DT; ++d) acc[d] = mma<T>(at.transposed(kt + TB, g, d), p[g], acc[d]);
     }
     __syncthreads();                              // the last tiles have been read
     if (!w.active) return;
@@ -419,8 +383,8 @@ __global__ __launch_bounds__(256, 2) void pack_forward_kernel(PackArgs a) {
     uint64_t rows = __builtin_amdgcn_ballot_w64(there && l == l && any_undefined(acc));
     rows = (rows | (rows >> 32)) & 0xFFFFFFFFull;
     if (rows) {
-        const int t0 = (w.my_stages - 1) * 64, t = t0 + lane;
-        const uint64_t odd = __builtin_amdgcn_ballot_w64(t < w.len && not_finite<T, HD>(v + (size_t)t * a.v_stride));
+        const int t0 = w.pos0, t = t0 + lane;
+        const uint64_t odd = __builtin_amdgcn_ballot_w64(lane < 32 && t < w.len && not_finite<T, HD>(v + (size_t)t * a.v_stride));
         while (rows) {
             const int r = __builtin_ctzll(rows);
             rows &= rows - 1;
@@ -435,7 +399,7 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
     constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD>::BYTES;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TB > 4 * kPutBytes<HD> ? 4 * TB : 4 * kPutBytes<HD>];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
-    const Unit w(a, wave);
+    const Unit<64> w(a, wave);
     const T* k = (const T*)a.k + (size_t)w.row0 * a.k_stride + w.kvh * HD;
     const T* v = (const T*)a.v + (size_t)w.row0 * a.v_stride + w.kvh * HD;
     const Bring<HD> bring_k(a.k_stride, wave, lane), bring_v(a.v_stride, wave, lane);
