@@ -1,5 +1,10 @@
-// What a decoder block has beside its matrix products and its attention, for the learner: addition to the residual stream with RMSNorm, and the
-// norm and rotation of the q and k heads, each forward and backward.
+// What a decoder block has beside its matrix products and its attention, for the learner: addition to the residual stream with RMSNorm, and the norm and rotation of the q and k heads,
+// each forward and backward.
+//
+// All are bound by memory: a row's elements are read once, kept in registers while their sum is formed, and written once.  Figures (a copy of 4 GiB moves 4.8 TB/s; what the last
+// pass left in the 256 MB cache is read faster): addition + norm to 8 bits, 15,271 rows of 2,560 bf16, 274 MB in 48 us; gradient, 16,384 rows of 3,584 bf16, 470 MB in 98 us and 4.4 for the
+// gain's sums; heads 32 + 8 of 128, 15,271 rows bf16, 313 MB in 64 us; their gradient, 16,384 rows, 503 MB in 102 and 4.6.  A workgroup a row swept three times took 167, 298, and a wave a
+// head with an angle of its own a lane 213 and 616.
 #include <algorithm>
 
 #include "spiral_internal.h"

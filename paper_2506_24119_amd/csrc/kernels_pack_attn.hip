@@ -1,7 +1,26 @@
 // Causal attention over packed sequences, forward and backward, for the learner.
 //
-// A row alone: one wave computes one (row, head) of the outputs, of dq, or of dk and dv, token by token, and reads nothing that
-// the row does not see.  All sums are fp32.
+//   forward   s = scale q k^T, one pass over a row's tokens with a running reference m and sum l of exp2(s log2e - m); out = (sum exp2(..) v) / l, lse = ln 2 (m + log2 l)
+//   dq        p = exp2(s log2e - lse log2e), dp = dout v^T, t = p (dp - D), dq = scale t k; D = dout . out, or sum p dp where a row's tokens are all at hand
+//   dk, dv    the same p and t by columns: dv = p^T dout, dk = scale t^T q, over the group's heads
+//
+// All products are 32x32x16 matrix instructions on 16-bit operands with fp32 sums.  The scores come out transposed (a lane holds one row, its registers tokens; in the
+// dk/dv kernel one token, and rows), which is the layout in which weights are the second operand of the product that follows, so they never leave their
+// registers: rounded to the operands' type, to nearest, they are off by half a step, as q, k and v themselves are.  D, lse, m, l and all sums are fp32.
+//
+// Three kernels, seven products where the mathematics has five in the backward pass (s and dp are made twice): one kernel for all would have to add dq from many
+// workgroups, by atomics whose order changes results or by partial sums that take longer than the two products (16 sequences of U[1024, 4096]: 15 GB, 3.1 ms).
+//
+// Bound: the chip's power.  The compute units are busy, the matrix pipes 55 % of their time at 1.9 GHz; with zeros for all inputs the same launches take 17, 23 and 27 % less
+// time.  16 sequences of U[1024, 4096], 32 heads on 8, hd 128, bf16 (41 k rows): forward 1.06 ms (1.0 PFLOP/s), dq 1.70 (0.94), dk and dv 2.10 (1.02 of what is computed);
+// a library product of 16384^3 makes 1.35.  A row alone by one wave, token by token, took 534 ms for the three.
+// On the way: bank-free tiles (64 banks, not 32, serve a wave's reads) 5.1 -> 2.65 ms of dk and dv, whose addresses had been spilled; values in LDS and stages of 32 rows there 2.65 -> 2.24; three
+// forward workgroups a compute unit 1.16 -> 1.06.  Without effect, within 2 %: products interleaved with exponentials instruction by instruction, operand reads further ahead, the two score
+// chains in turn, s_setprio around products, heads in turn over the same rows (L2 hits 28 -> 74 %).  Worse: 64 rows a wave (512 registers, one wave a SIMD: forward
+// 1.16 -> 2.44 ms), eight waves a workgroup with three stages in flight (1.16 -> 1.39).
+//
+// A row alone: one wave computes one (row, head) of the outputs or of dq, token by token, and reads nothing that the row does not see.  For rows in whose sums a
+// weight of 0 has met an infinite or undefined value only.
 #include <type_traits>
 
 #include "spiral_internal.h"
@@ -36,7 +55,7 @@ __device__ __forceinline__ float wave_most(float v) {
 // A lane holds dimensions lane and lane + 64 (HD = 32: the upper half of the wave repeats the lower)
 template <int HD> constexpr int kDims = (HD + 63) / 64;
 
-// out and lse of one row; k, v: the sequence's first row
+// out and lse of one row; k, v: the sequence's first row.
 template <class T, int HD>
 __device__ void forward_row(const PackArgs& a, const T* k, const T* v, const T* q, int last, T* out, float* lse, int lane) {
     constexpr int DL = kDims<HD>;
@@ -86,50 +105,6 @@ __device__ void dq_row(const PackArgs& a, const T* k, const T* v, const T* q, co
 #pragma unroll
     for (int j = 0; j < DL; ++j)
         if (lane + 64 * j < HD) dq[lane + 64 * j] = (T)(g[j] * a.scale);
-}
-
-// dk and dv of one token and kv head from the query heads h0 .. h1 - 1, or their part of them; row0: the sequence's first row, len: its length, t: the token's position
-template <class T, int HD, bool PARTS>
-__device__ void dkv_row(const PackArgs& a, int row0, int len, int t, int kvh, int h0, int h1, int part, int lane) {
-    constexpr int DL = kDims<HD>;
-    const T* k = (const T*)a.k + (size_t)(row0 + t) * a.k_stride + kvh * HD;
-    const T* v = (const T*)a.v + (size_t)(row0 + t) * a.v_stride + kvh * HD;
-    float gk[DL] = {}, gv[DL] = {};
-    for (int h = h0; h < h1; ++h) {
-        const T* q = (const T*)a.q + (size_t)row0 * a.q_stride + h * HD;
-        const T* dout = (const T*)a.dout + (size_t)row0 * a.dout_stride + h * HD;
-        const float* lse = a.lse + (size_t)h * a.n_rows + row0;
-        const float* delta = a.delta + (size_t)h * a.n_rows + row0;
-        for (int i0 = t; i0 < len; i0 += 64) {
-            const int i = i0 + lane;
-            float p = 0.f, ds = 0.f;
-            if (i < len) {
-                p = exp2f(dot<T, HD>(q + (size_t)i * a.q_stride, k) * a.scale_log2e - lse[i] * kLog2e);
-                ds = p * (dot<T, HD>(dout + (size_t)i * a.dout_stride, v) - delta[i]);
-            }
-            for (int e = 0; e < 64 && i0 + e < len; ++e) {
-                const float pe = __shfl(p, e, 64), de = __shfl(ds, e, 64);
-                const T* qr = q + (size_t)(i0 + e) * a.q_stride;
-                const T* dr = dout + (size_t)(i0 + e) * a.dout_stride;
-#pragma unroll
-                for (int j = 0; j < DL; ++j) {
-                    gk[j] = fmaf(de, (float)qr[(lane + 64 * j) & (HD - 1)], gk[j]);
-                    gv[j] = fmaf(pe, (float)dr[(lane + 64 * j) & (HD - 1)], gv[j]);
-                }
-            }
-        }
-    }
-    const size_t width = (size_t)a.n_kv_heads * HD, plane = (size_t)a.n_rows * width;
-    float* to = PARTS ? a.part + (size_t)part * 2 * plane + (size_t)(row0 + t) * width + kvh * HD : nullptr;
-    T* dk = (T*)a.dk + (size_t)(row0 + t) * a.dk_stride + kvh * HD;
-    T* dv = (T*)a.dv + (size_t)(row0 + t) * a.dv_stride + kvh * HD;
-#pragma unroll
-    for (int j = 0; j < DL; ++j) {
-        const int d = lane + 64 * j;
-        if (d >= HD) continue;
-        if (PARTS) to[d] = gk[j], to[plane + d] = gv[j];
-        else dk[d] = (T)(gk[j] * a.scale), dv[d] = (T)gv[j];
-    }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -529,8 +504,10 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
     }
 }
 
-// 128 tokens of a kv head a workgroup, 32 a wave; the heads of the group (or a part of them) and their rows from the tokens on pass by, 32 at a time.  Keys stay in
-// registers, values in LDS: with both in registers, beside two accumulators, there are too few left to read operands ahead.
+// 128 tokens of a kv head a workgroup, 32 a wave; rows pass by, 32 at a time, from the sequence's end to the tokens, each time of all heads of the group (or a part of
+// them).  Keys stay in registers, values in LDS: with both in registers, beside two accumulators, there are too few left to read operands ahead.
+// A wave's last stages are those of its tokens' own rows, some of which do not see some tokens.  Where one of these rows is not finite, as its lse (of q) or D (of dout) then
+// is, the stage is left out, as a weight of 0 would not keep it out of the sums; this head's rows and those of the heads behind it are then added pair by pair.
 template <int HD> constexpr int kDkvBytes = 2 * Tile<HD>::BYTES + 4 * Tile<HD, 32>::BYTES + 512;
 template <class T, int HD, bool PARTS>
 __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
@@ -547,7 +524,7 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
     const int tok0 = block0 + wave * 32, n_valid = max(0, min(32, len - tok0));
     const int q_stages = (len - block0 + 31) >> 5, stages = q_stages * (h1 - h0);
     const Bring32<HD> bring_q(a.q_stride, wave, lane), bring_d(a.dout_stride, wave, lane);
-    int next_h = h0, next_q = block0;             // of the stage to be brought next
+    int next_h = h0, next_q = block0 + (q_stages - 1) * 32;      // of the stage to be brought next
     float row_value = 0.f;                        // its row l32's lse or delta
     bool row_there = false;
     auto bring = [&](int st) {
@@ -556,7 +533,7 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
         bring_d((const T*)a.dout + (size_t)(row0 + next_q) * a.dout_stride + next_h * HD, len - next_q, to + TB, wave);
         if (wave == 0) row_value = ((lh ? a.delta : a.lse) + (size_t)next_h * a.n_rows + row0 + next_q)[min(l32, len - 1 - next_q)];
         row_there = next_q + l32 < len;
-        if ((next_q += 32) >= len) { next_q = block0; ++next_h; }
+        if (++next_h == h1) { next_h = h0; next_q -= 32; }
     };
     auto park = [&](int st) {                     // rows that are not there weigh nothing
         if (wave == 0) s_row[(st & 1) * 64 + lane] = lh ? (row_there ? row_value : 0.f) : row_there ? row_value * kLog2e : INFINITY;
@@ -578,7 +555,7 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
     const Reads<HD> at_v(lane);
     const Reads<HD, 32> at(lane);
     const char* vt = lds + (wave >> 1) * Tile<HD>::BYTES;
-    int q0 = block0;
+    int q0 = block0 + (q_stages - 1) * 32, h = h0, alone_from = h1;
     for (int st = 0; st < stages; ++st) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -588,7 +565,11 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
         const char* qt = stages_lds + (st & 1) * 2 * TB;
         const char* ot = qt + TB;
         const float* rows = s_row + (st & 1) * 64 + lh * 4;
-        if (n_valid > 0 && q0 + 31 >= tok0) {
+        if (n_valid > 0 && q0 == tok0) {
+            const float x = s_row[(st & 1) * 64 + lane];
+            if (__builtin_amdgcn_ballot_w64(there && !(fabsf(x) < INFINITY)) != 0) alone_from = min(alone_from, h);
+        }
+        if (n_valid > 0 && (q0 > tok0 || (q0 == tok0 && h < alone_from))) {
             f32x16 s = zeros(), dp = zeros();
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(qt, 0, ks), kf[ks], s);
@@ -622,12 +603,38 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) dk[d] = mma<T>(at.transposed(qt, g, d), t[g], dk[d]);
         }
-        if ((q0 += 32) >= len) q0 = block0;
+        if (++h == h1) { h = h0; q0 -= 32; }
         if (more) park(st + 1);
     }
     __syncthreads();
     if (n_valid <= 0) return;
     const size_t first = (size_t)row0 + tok0;
+#pragma unroll 1
+    for (int g = alone_from; g < h1; ++g) {
+        const T* k = (const T*)a.k + (first + (there ? l32 : 0)) * a.k_stride + kvh * HD + lh * 8;
+        const T* v = (const T*)a.v + (first + (there ? l32 : 0)) * a.v_stride + kvh * HD + lh * 8;
+#pragma unroll 1
+        for (int i = 0; i < n_valid; ++i) {
+            const T* q = (const T*)a.q + (first + i) * a.q_stride + g * HD;
+            const T* o = (const T*)a.dout + (first + i) * a.dout_stride + g * HD;
+            float sc = 0.f, dp = 0.f;                 // the lane's half of the dimensions, then both
+#pragma unroll 1
+            for (int c = 0; c < HD; c += 16) sc = dot8(q + c + lh * 8, k + c, sc), dp = dot8(o + c + lh * 8, v + c, dp);
+            sc += __shfl_xor(sc, 32, 64);
+            dp += __shfl_xor(dp, 32, 64);
+            const float p = exp2f(sc * a.scale_log2e - a.lse[(size_t)g * a.n_rows + first + i] * kLog2e), t = p * (dp - a.delta[(size_t)g * a.n_rows + first + i]);
+            if (l32 <= i && there)
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int at_d = d * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
+                        dv[d][r] = fmaf(p, (float)o[at_d], dv[d][r]);
+                        dk[d][r] = fmaf(t, (float)q[at_d], dk[d][r]);
+                        asm volatile("" ::: "memory");      // a few loads at a time: more would take the registers that the loop above needs
+                    }
+        }
+    }
     if constexpr (PARTS) {                        // fp32 [part][dk or dv][row][kv head][HD]: the lane's row, four dimensions at a time
         if (there) {
             const size_t width = (size_t)a.n_kv_heads * HD, plane = (size_t)a.n_rows * width;
@@ -645,29 +652,6 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
         put_rows<T, HD>(dk, a.scale, mine, (T*)a.dk + first * a.dk_stride + kvh * HD, a.dk_stride, n_valid, lane);
         __builtin_amdgcn_wave_barrier();
         put_rows<T, HD>(dv, 1.f, mine, (T*)a.dv + first * a.dv_stride + kvh * HD, a.dv_stride, n_valid, lane);
-    }
-    // A weight of 0 times an infinite or undefined value of a row before the token: of the wave's first 32 rows only.  Tokens behind such a row are computed alone, but
-    // for those that are undefined anyway, before (or at) the last row whose weights are.
-    uint64_t toks = __builtin_amdgcn_ballot_w64(there && (any_undefined(dk) || any_undefined(dv)));
-    toks = (toks | (toks >> 32)) & 0xFFFFFFFFull;
-    if (!toks) return;
-    uint64_t odd = 0;
-    int last = -1;
-    for (int h = h0; h < h1; ++h) {
-        const size_t row = first + l32;
-        odd |= __builtin_amdgcn_ballot_w64(there && (not_finite<T, HD>((const T*)a.q + row * a.q_stride + h * HD) || not_finite<T, HD>((const T*)a.dout + row * a.dout_stride + h * HD)));
-        for (int i0 = tok0; i0 < len; i0 += 64) {
-            const int i = i0 + lane;
-            const float x = i < len ? a.lse[(size_t)h * a.n_rows + row0 + i] : 0.f;
-            const uint64_t none = __builtin_amdgcn_ballot_w64(x != x);
-            if (none) last = max(last, i0 + 63 - __builtin_clzll(none));
-        }
-    }
-    odd &= 0xFFFFFFFFull;
-    while (toks) {
-        const int r = __builtin_ctzll(toks);
-        toks &= toks - 1;
-        if (tok0 + r > last && (odd & ((1ull << r) - 1))) dkv_row<T, HD, PARTS>(a, row0, len, tok0 + r, kvh, h0, h1, part, lane);
     }
 }
 

@@ -192,6 +192,33 @@ def test_what_a_row_does_not_see_does_not_reach_it(sb, name, row, value, dtype):
     c.free()
 
 
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 2, 64), (7, 1, 128), (2, 2, 32)])
+def test_infinite_gradients_stay_where_they_belong(sb, hq, hkv, hd):
+    """Every third row of a sequence up to row 80 with an infinite element in its output's gradient: dq of the other rows, dk and dv of the tokens behind, and
+    the other sequences are what they are without."""
+    import torch
+    lens = [50, 100, 33]
+    c = Call(sb, lens, hq, hkv, hd, "float16", seed=31)
+    c.forward()
+    c.backward()
+    clean = c.results()
+    rows = torch.arange(50, 131, 3, device="cuda")
+    c.dout[rows, 0, 5] = float("inf")
+    c.backward()
+    got = c.results()
+    keep = torch.ones(c.n, dtype=torch.bool, device="cuda")
+    keep[rows] = False
+    assert torch.equal(got[2][keep], clean[2][keep])
+    behind = torch.ones(c.n, dtype=torch.bool, device="cuda")
+    behind[50:rows[-1] + 1] = False
+    # added pair by pair, a tile's weights are not rounded to half precision: each of up to 32 terms a head differs by 2^-11 of it, and none is an eighth of the largest sum
+    for name, g, w in zip(("dk", "dv"), got[3:], clean[3:]):
+        assert torch.isfinite(g[behind]).all(), name
+        assert ((g[behind].float() - w[behind].float()).abs() <= 2.0 ** -9 * (w[behind].float().abs() + w.float().abs().max() * 2.0 ** -3)).all(), name
+    assert not torch.isfinite(got[4][50, 0, 5]) and not torch.isfinite(got[2][50, 0]).all()
+    c.free()
+
+
 def test_rows_do_not_depend_on_other_sequences(sb):
     import torch
     c = Call(sb, [100, 333, 7, 64], 8, 2, 128, "bfloat16", seed=11)
