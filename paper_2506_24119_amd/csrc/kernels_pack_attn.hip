@@ -433,28 +433,16 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
     arrive(0);
     if (w.my_stages == 1) {
         // All that the rows see is here, so that D can be had as sum p dp.  From `out`, whose rounding is in it, it is off by 2^-9 of what dp - D, where a
-        // row sees few tokens, nearly cancels to (dq of sequences of 2 to 20 tokens: 0.4 % off, now 0.24).  In a loop of its own: in the other one it costs that 20 %.
-        f32x16 p[2], dp[2];
+        // row sees few tokens, nearly cancels to (dq of sequences of 2 to 20 tokens: 0.4 % off, now 0.24).
         float sum = 0.f;
-#pragma unroll
+#pragma unroll 1
         for (int half = 0; half < 2; ++half) {
-            products(p[half], dp[half], 0, half);
+            f32x16 s, dp;
+            products(s, dp, 0, half);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const bool hide = hidden(0, half, r);
-                p[half][r] = hide ? 0.f : __builtin_amdgcn_exp2f(fmaf(p[half][r], a.scale_log2e, -lse2));
-                dp[half][r] = hide ? 0.f : dp[half][r];
-                sum = fmaf(p[half][r], dp[half][r], sum);
-            }
+            for (int r = 0; r < 16; ++r) sum += hidden(0, half, r) ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2e, -lse2)) * dp[r];
         }
         delta = there ? sum + __shfl_xor(sum, 32, 64) : 0.f;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            u32x4 t[2];
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) t[r >> 3][(r >> 1) & 3] = pack2<T>(p[half][r] * (dp[half][r] - delta), p[half][r + 1] * (dp[half][r + 1] - delta));
-            add(t, 0, half);
-        }
     }
     auto both_products = [&](int st, int half, auto cut) {
         f32x16 s, dp;
@@ -476,9 +464,10 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
     for (int st = 0; st < w.stages; ++st) {
         if (st > 0) arrive(st);
         if (st < whole) {
-            both_products(st, 0, std::false_type());
-            both_products(st, 1, std::false_type());
-        } else if (st == whole && whole > 0) {
+            // (one copy of the body at 128 dimensions, two leave it too few registers to read operands ahead: 1.76 -> 1.69 ms; below it is 3 % the other way)
+#pragma unroll(HD == 128 ? 1 : 2)
+            for (int half = 0; half < 2; ++half) both_products(st, half, std::false_type());
+        } else if (st == whole) {
             both_products(st, 0, std::true_type());
             if (st * 64 + 32 <= w.pos0 + 31) both_products(st, 1, std::true_type());
         }
