@@ -51,7 +51,7 @@ def near(got, want, allowed, what):
 
 
 ROWS = [(1, 1, 0, 0), (3, 7, 1, 1), (5, 2560, 0, 0), (70, 893, 3, 1), (33, 4096, 8, 8), (2, 20011, 1, 0), (129, 256, 0, 4), (9, 8192, 0, 0), (4, 16384, 8, 0), (300, 64, 0, 0), (17, 3584, 5, 3),
-        (2, 40000, 0, 0)]
+        (2, 40000, 0, 0), (2100, 130, 1, 1), (2049, 2559, 3, 1), (2048, 9, 0, 0), (2050, 4090, 0, 0), (6, 8, 0, 1)]
 
 
 @pytest.mark.parametrize("n,d,pad,offset", ROWS)
@@ -222,6 +222,28 @@ def test_norm_rope(sb, n, hq, hkv, hd, dtype, norm, pad, offset):
     sb.spiral_norm_rope_backward(x[0], x[1], dy[0], dy[1], gains[0], gains[1], eps, theta, dpos, dy[0], dy[1], dg[0], dg[1], ws)
     sb.spiral_norm_rope(x[0], x[1], gains[0], gains[1], eps, theta, dpos, x[0], x[1])
     assert all(torch.equal(a, b) for a, b in zip(keep, (*x, *dy, *[t for t in dg if t is not None])))
+
+
+def test_rows_far_apart(sb):
+    """Rows 2^26 elements apart, the last ones behind 2^31: the bits of the same calls on rows back to back."""
+    import torch
+    rng = np.random.default_rng(6)
+    n, d = 36, 128
+    _, x = matrix(n, d, "bfloat16", values=rng.normal(size=(n, d)))
+    far = torch.empty(n << 26, dtype=torch.bfloat16, device="cuda").view(n, 1 << 26)[:, :d]
+    far.copy_(x)
+    gain = torch.from_numpy((1 + 0.3 * rng.normal(size=d)).astype(np.float32)).cuda()
+    outs = []
+    for t in (x, far):
+        out, total, rstd, dx, dg = torch.empty_like(x), torch.empty_like(x), torch.empty(n, device="cuda"), torch.empty_like(x), torch.empty(d, device="cuda")
+        ws = torch.empty(sb.spiral_add_rmsnorm_backward_workspace_bytes(n, d), dtype=torch.uint8, device="cuda")
+        sb.spiral_add_rmsnorm(t, t, gain, 1e-6, out, None, total, rstd)
+        sb.spiral_add_rmsnorm_backward(t, total, gain, rstd, t, dx, dg, ws)
+        heads = t.unflatten(1, (2, 64))
+        oq, ok, pos = torch.empty((n, 1, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((n, 1, 64), dtype=torch.bfloat16, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda")
+        sb.spiral_norm_rope(heads[:, :1], heads[:, 1:], gain[:64], gain[64:], 1e-6, 1e4, pos, oq, ok)
+        outs.append([out, total, rstd, dx, dg, oq, ok])
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
 
 
 def test_gradients_of_rows_are_those_of_differences(sb):

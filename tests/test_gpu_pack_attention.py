@@ -132,7 +132,7 @@ def untouched(c):
 # the last four: a group's heads shared out over workgroups of their own, evenly and not, beside many short sequences that are not
 SHAPES = [([1], 1, 1, 32), ([5, 0, 1, 33], 4, 2, 32), ([64, 65, 63], 2, 1, 64), ([130, 1, 31, 32], 6, 2, 128), ([257, 40], 7, 1, 128), ([0, 200, 0], 3, 3, 64),
           ([129, 127, 128], 8, 2, 64), ([96], 16, 1, 128), ([300, 17], 5, 5, 128), ([2] * 40, 4, 4, 32), ([31, 321], 9, 3, 32), ([70, 191], 12, 4, 128), ([500], 7, 1, 64), ([390, 3, 200], 6, 2, 128),
-          ([129] * 12, 16, 2, 32), ([700, 1, 650, 0, 33], 5, 1, 32)]
+          ([129] * 12, 16, 2, 32), ([700, 1, 650, 0, 33], 5, 1, 32), ([70, 35], 64, 1, 32), ([150], 40, 1, 64), ([33, 64, 1], 12, 12, 128)]
 
 
 @pytest.mark.parametrize("lens,hq,hkv,hd", SHAPES)
@@ -239,6 +239,43 @@ def test_rows_do_not_depend_on_other_sequences(sb):
             else:
                 assert torch.equal(got, want)
         d.free()
+    c.free()
+
+
+def test_many_short_sequences(sb):
+    """More than one upload of the plan's items, sequences of one to three positions: the first of each is its own value."""
+    import torch
+    lens = [1 + i % 3 for i in range(1700)]
+    c = Call(sb, lens, 4, 2, 32, "bfloat16", seed=41)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    check_forward(c)
+    check_backward(c)
+    first = torch.from_numpy(np.concatenate([[0], np.cumsum(lens)[:-1]])).cuda()
+    assert torch.equal(c.out[first], c.v[first].repeat_interleave(2, dim=1))
+    c.free()
+
+
+@pytest.mark.parametrize("which", ["q", "v", "dout", "dk"])
+def test_rows_far_apart(sb, which):
+    """Rows 2^22 elements apart, so that a matrix spans more than 2^31 of them: the bits of the same call on rows back to back."""
+    import torch
+    n = 530
+    c = Call(sb, [n - 17, 17], 4, 2, 64, "bfloat16", fused=False, seed=43)
+    c.forward()
+    c.backward()
+    want = c.results()
+    near = getattr(c, which)
+    whole = torch.empty(n << 22, dtype=near.dtype, device="cuda")
+    far = whole.view(n, 1 << 22)[:, :near.shape[1] * 64].unflatten(1, (near.shape[1], 64))
+    far.copy_(near)
+    setattr(c, which, far)
+    if which == "dk":
+        far.zero_()
+    c.forward()
+    c.backward()
+    assert all(torch.equal(a, b) for a, b in zip(c.results(), want))
     c.free()
 
 
