@@ -174,11 +174,16 @@ template <int HD> struct Bring32 {
         const int row = (wave & 1) * 16 + (lane >> 2);
         off = row * row_bytes + (((lane & 3) ^ swizzle(row)) * 16) + (wave >> 1) * 64;
     }
-    __device__ __forceinline__ void operator()(const void* first, int rows, char* lds, int wave) const {
+    __device__ __forceinline__ void operator()(const void* first, int rows, char* lds, int wave) const { bring(first, rows, lds, wave, off); }
+    // with the last row in the place of those past the end; rows >= 1, row: the lane's
+    __device__ __forceinline__ void repeat_last(const void* first, int rows, char* lds, int wave, int row) const {
+        bring(first, rows, lds, wave, off - (uint32_t)max(0, row - (rows - 1)) * row_bytes);
+    }
+    __device__ __forceinline__ void bring(const void* first, int rows, char* lds, int wave, uint32_t at) const {
         const __amdgpu_buffer_rsrc_t r = buffer_upto(first, __builtin_amdgcn_readfirstlane((uint32_t)max(0, min(rows, 32)) * row_bytes));
         char* to = lds + wave * 1024;
-        if (LOADS >= 4 || wave < LOADS) to_lds<0>(r, to, off);
-        if constexpr (LOADS > 4) to_lds<128>(r, to + 4096 - 128, off);
+        if (LOADS >= 4 || wave < LOADS) to_lds<0>(r, to, at);
+        if constexpr (LOADS > 4) to_lds<128>(r, to + 4096 - 128, at);
     }
 };
 
@@ -518,7 +523,9 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
     bool row_there = false;
     auto bring = [&](int st) {
         char* to = stages_lds + (st & 1) * 2 * TB;
-        bring_q((const T*)a.q + (size_t)(row0 + next_q) * a.q_stride + next_h * HD, len - next_q, to, wave);
+        // Rows behind the last weigh exp2(s - inf): 0, if their score is that of a row that is there.  Zeros would meet a key's infinity, which for the sequence's rows may be
+        // a score of -inf.
+        bring_q.repeat_last((const T*)a.q + (size_t)(row0 + next_q) * a.q_stride + next_h * HD, len - next_q, to, wave, (wave & 1) * 16 + (lane >> 2));
         bring_d((const T*)a.dout + (size_t)(row0 + next_q) * a.dout_stride + next_h * HD, len - next_q, to + TB, wave);
         if (wave == 0) row_value = ((lh ? a.delta : a.lse) + (size_t)next_h * a.n_rows + row0 + next_q)[min(l32, len - 1 - next_q)];
         row_there = next_q + l32 < len;

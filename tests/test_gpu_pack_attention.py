@@ -219,6 +219,29 @@ def test_infinite_gradients_stay_where_they_belong(sb, hq, hkv, hd):
     c.free()
 
 
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 2, 64), (7, 1, 128), (2, 2, 32)])
+def test_tokens_that_weigh_nothing(sb, hq, hkv, hd):
+    """Keys with an element of -inf where queries are positive: scores of -inf, weights of 0, dk and dv of 0; dq alone meets 0 times infinity."""
+    import torch
+    c = Call(sb, [50, 70, 33], hq, hkv, hd, "bfloat16", seed=37)
+    c.q[:, :, 3] = c.q[:, :, 3].abs() + 1
+    tokens = torch.tensor([1, 40, 51, 118, 152], device="cuda")
+    c.k[tokens, :, 3] = -float("inf")
+    c.forward()
+    c.backward()
+    weightless = [c.dk[tokens], c.dv[tokens]]
+    for t in (*weightless, c.out, c.lse, c.dk, c.dv):
+        assert torch.isfinite(t).all()
+    assert not any(t.any() for t in weightless)
+    q, k, v = c.host("q", "k", "v")
+    half = HALF["bfloat16"]
+    want, size = (ob.attention(q, k, x, c.lens, c.scale)[0] for x in (v, np.abs(v)))
+    c.k[tokens, :, 3] = 0.0
+    E = c.errors().T[:, :, None]
+    close(c.host("out")[0], want, (half + 2 * E) * size + half * np.abs(want) * (1 + half), "out")
+    c.free()
+
+
 def test_rows_do_not_depend_on_other_sequences(sb):
     import torch
     c = Call(sb, [100, 333, 7, 64], 8, 2, 128, "bfloat16", seed=11)
