@@ -223,7 +223,8 @@ template <int HD> __device__ __forceinline__ void hold(u32x4 (&f)[HD / 16], cons
 }
 
 // Writes 32 rows of results whose transpose the wave holds (lane: row l32; registers 4b .. 4b + 3 of tile dt: dimensions 32 dt + 8 b + 4 lh .. + 3), each times its
-// row's factor, through a private part of LDS, so that whole rows leave.
+// row's factor, through a private part of LDS, so that whole rows leave.  Nothing here reads them again: stored past the caches' order of use, they leave it to keys and
+// values (forward, 24 sequences of U[256, 1024]: 144 -> 130 us).  Loads of the same kind, of q, cost 153: a line serves eight of them.
 template <class T, int HD>
 __device__ __forceinline__ void put_rows(const f32x16 (&acc)[HD / 32], float factor, char* lds, T* first, long long stride, int n_valid, int lane) {
     constexpr int ROW = HD * 2 + 16;          // bytes between rows: 16 lanes that write 8 bytes of 16 rows each
@@ -240,7 +241,7 @@ __device__ __forceinline__ void put_rows(const f32x16 (&acc)[HD / 32], float fac
     for (int u = 0; u < 32 * LANES / 64; ++u) {
         const int row = u * (64 / LANES) + lane / LANES, piece = lane % LANES;
         const u32x4 v = *(const u32x4*)(lds + row * ROW + piece * 16);
-        if (row < n_valid) *(u32x4*)(first + (size_t)row * stride + piece * 8) = v;
+        if (row < n_valid) __builtin_nontemporal_store(v, (u32x4*)(first + (size_t)row * stride + piece * 8));
     }
 }
 template <int HD> constexpr int kPutBytes = 32 * (HD * 2 + 16);
