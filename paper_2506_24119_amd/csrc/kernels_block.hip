@@ -1,10 +1,10 @@
 // What a decoder block has beside its matrix products and its attention, for the learner: addition to the residual stream with RMSNorm, and the norm and rotation of the q and k heads,
 // each forward and backward.
 //
-// All are bound by memory: a row's elements are read once, kept in registers while their sum is formed, and written once.  Figures (a copy of 4 GiB moves 4.8 TB/s; what the last
-// pass left in the 256 MB cache is read faster): addition + norm to 8 bits, 15,271 rows of 2,560 bf16, 274 MB in 48 us; gradient, 16,384 rows of 3,584 bf16, 470 MB in 98 us and 4.4 for the
-// gain's sums; heads 32 + 8 of 128, 15,271 rows bf16, 313 MB in 64 us; their gradient, 16,384 rows, 503 MB in 102 and 4.6.  A workgroup a row swept three times took 167, 298, and a wave a
-// head with an angle of its own a lane 213 and 616.
+// All are bound by memory: a row's elements are read once, kept in registers while their sum is formed, and written once.  Figures, other inputs each time (a copy of 4 GiB moves 4.8
+// TB/s): addition + norm to 8 bits, 15,271 rows of 2,560 bf16, 274 MB in 50 us; gradient, 16,384 rows of 3,584 bf16, 470 MB in 97 us and 4.4 for the gain's sums; heads 32 + 8
+// of 128, 15,271 rows bf16, 313 MB in 65 us; their gradient, 16,384 rows, 503 MB in 96 and 4.6.  A workgroup a row swept three times took 167, 298, and a wave a head with an angle of
+// its own a lane 213 and 616.
 #include <algorithm>
 
 #include "spiral_internal.h"
@@ -57,6 +57,13 @@ __device__ __forceinline__ float code_scale(float most, float rstd) { return mos
 template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
 template <class T> using Eights = typename Eight<T>::type;
 
+// ONCE: a call that reads and writes more than the caches keep goes past their order of use.
+template <bool ONCE, class E, class V> __device__ __forceinline__ void store(E* p, V x) {
+    typedef V Any __attribute__((aligned(sizeof(E))));
+    if constexpr (ONCE) __builtin_nontemporal_store(x, (Any*)p);
+    else *(Any*)p = x;
+}
+
 // A lane's v-th eight elements of a row of d >= 8.  Those of the last v that would pass the row's end are read from d - 8 on, without a branch, and the first `skip` of
 // them (all: 8) are another lane's: they are left out of sums and not written, as their place may hold the output already.
 template <int LANES, int NV> struct Share {
@@ -64,24 +71,26 @@ template <int LANES, int NV> struct Share {
     __device__ __forceinline__ int begin(int v) const { return (v * LANES + t) * 8; }
     __device__ __forceinline__ int at(int v) const { return v < NV - 1 ? begin(v) : min(begin(v), d - 8); }
     __device__ __forceinline__ int skip(int v) const { return v < NV - 1 ? 0 : min(begin(v) - at(v), 8); }
-    template <class V, class E> __device__ __forceinline__ void put(E* row, int v, V x) const {
-        typedef V Any __attribute__((aligned(sizeof(E))));
+    template <bool ONCE, class V, class E> __device__ __forceinline__ void put(E* row, int v, V x) const {
         const int n = skip(v);
-        if (n == 0) *(Any*)(row + at(v)) = x;
+        if (n == 0) store<ONCE>(row + at(v), x);
         else
 #pragma unroll
             for (int e = 1; e < 8; ++e)
                 if (e >= n) row[at(v) + e] = __builtin_bit_cast(E __attribute__((ext_vector_type(8))), x)[e];
     }
 };
-template <class T> __device__ __forceinline__ Eights<T> eight(const T* p) { return *(const Eights<T>*)p; }
+template <bool ONCE = false, class T> __device__ __forceinline__ Eights<T> eight(const T* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load((const Eights<T>*)p);
+    else return *(const Eights<T>*)p;
+}
 // What a second sweep over the same values widens again: kept from the first, they would take three times the registers (16,384 rows of 3,584 bf16: 160 us and spills, now 97).
 template <class T> __device__ __forceinline__ void forget(Eights<T>& x) { asm volatile("" : "+v"(x)); }
 template <> __device__ __forceinline__ void forget<float>(Eights<float>&) {}
 
 // A row by one wave or by four, in registers: NV times eight elements a lane.  One read of what there is to read, one write; every load of a row is on its way before
 // its first element is needed.
-template <class T, bool OUT8, int WAVES, int NV>
+template <class T, bool OUT8, int WAVES, int NV, bool ONCE>
 __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
     __shared__ float s[WAVES];
     constexpr int LANES = 64 * WAVES;
@@ -92,8 +101,8 @@ __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
         Eights<T> xv[NV], rv[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            xv[v] = eight(x + mine.at(v));
-            if (res) rv[v] = eight(res + mine.at(v));
+            xv[v] = eight<ONCE>(x + mine.at(v));
+            if (res) rv[v] = eight<ONCE>(res + mine.at(v));
         }
         float h[NV][8], sq = 0.f;
 #pragma unroll
@@ -113,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
                 Eights<T> y;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = (T)h[v][e];
-                mine.put((T*)a.sum + r * a.sum_stride, v, y);
+                mine.template put<ONCE>((T*)a.sum + r * a.sum_stride, v, y);
             }
             const Eights<float> g = eight(a.gain + mine.at(v));
 #pragma unroll
@@ -125,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
                 Eights<T> y;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = (T)(h[v][e] * rstd);
-                mine.put((T*)a.out + r * a.out_stride, v, y);
+                mine.template put<ONCE>((T*)a.out + r * a.out_stride, v, y);
             }
         }
         if (OUT8) {
@@ -137,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) h[v][e] *= inv;
                 typedef uint32_t Codes __attribute__((ext_vector_type(2)));
-                mine.put((uint8_t*)a.out + r * a.out_stride, v, Codes{to_e4m3x4(h[v]), to_e4m3x4(h[v] + 4)});
+                mine.template put<ONCE>((uint8_t*)a.out + r * a.out_stride, v, Codes{to_e4m3x4(h[v]), to_e4m3x4(h[v] + 4)});
             }
         }
     }
@@ -173,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a)
 }
 
 // Gradient: rows as above, workgroups take every gridDim.x-th (group of four) and keep the gain's sums over their rows in registers.
-template <class T, int WAVES, int NV>
+template <class T, int WAVES, int NV, bool ONCE>
 __global__ __launch_bounds__(kThreads, 2) void norm_grad_kernel(NormGradArgs a) {
     constexpr int LANES = 64 * WAVES;
     __shared__ float s[WAVES];
@@ -187,9 +196,9 @@ __global__ __launch_bounds__(kThreads, 2) void norm_grad_kernel(NormGradArgs a) 
         Eights<T> yv[NV], hv[NV], sv[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            yv[v] = eight(dy + mine.at(v));
-            hv[v] = eight(h + mine.at(v));
-            if (ds) sv[v] = eight(ds + mine.at(v));
+            yv[v] = eight<ONCE>(dy + mine.at(v));
+            hv[v] = eight<ONCE>(h + mine.at(v));
+            if (ds) sv[v] = eight<ONCE>(ds + mine.at(v));
         }
         const float rstd = a.rstd[r];
         const float* gain = a.gain;
@@ -215,7 +224,7 @@ __global__ __launch_bounds__(kThreads, 2) void norm_grad_kernel(NormGradArgs a) 
             Eights<T> x;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = (T)(rstd * ((float)yv[v][e] * g[e] - (float)hv[v][e] * rstd * along) + (ds ? (float)sv[v][e] : 0.f));
-            mine.put(dx, v, x);
+            mine.template put<ONCE>(dx, v, x);
         }
     }
     if (!a.dgain) return;
@@ -312,7 +321,7 @@ template <int HD> __device__ __forceinline__ float over_head(float v) {
 }
 
 // A row a wave.  HD / 16 lanes share a head: each has eight pairs (c, c + HD / 2) of neighbouring c, whose angles it evaluates once for all heads of the row.
-template <class T, int HD, bool GRAD>
+template <class T, int HD, bool GRAD, bool ONCE>
 __global__ __launch_bounds__(kThreads) void norm_rope_kernel(RopeArgs a, RopeFreq f) {
     constexpr int LANES = HD / 16, SLOTS = 64 / LANES;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (lane % LANES) * 8, slot = lane / LANES;
@@ -340,8 +349,8 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(RopeArgs a, RopeFre
             const bool norm = s.gain != nullptr;
             for (int h = slot; h < s.heads; h += SLOTS) {
                 Eights<T> lo, hi, ylo, yhi;
-                if (!GRAD || norm) lo = *(const Eights<T>*)(x + h * HD), hi = *(const Eights<T>*)(x + h * HD + HD / 2);
-                if (GRAD) ylo = *(const Eights<T>*)(dy + h * HD), yhi = *(const Eights<T>*)(dy + h * HD + HD / 2);
+                if (!GRAD || norm) lo = eight<ONCE>(x + h * HD), hi = eight<ONCE>(x + h * HD + HD / 2);
+                if (GRAD) ylo = eight<ONCE>(dy + h * HD), yhi = eight<ONCE>(dy + h * HD + HD / 2);
                 float rstd = 1.f;
                 if (norm) {
                     float sq = 0.f;
@@ -379,8 +388,8 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(RopeArgs a, RopeFre
                         ohi[e] = (T)(norm ? rstd * (q[e] - (float)hi[e] * rstd * along) : q[e]);
                     }
                 }
-                *(Eights<T>*)(out + h * HD) = olo;
-                *(Eights<T>*)(out + h * HD + HD / 2) = ohi;
+                store<ONCE>(out + h * HD, olo);
+                store<ONCE>(out + h * HD + HD / 2, ohi);
             }
         }
     }
@@ -418,40 +427,48 @@ template <class T> long long norm_grad_parts(long long n_rows, int d) {
     const int waves = norm_waves(n_rows, d, kMostGradVecs<T>);
     return std::min<long long>(waves == 1 ? (n_rows + 3) / 4 : n_rows, waves ? kGradBlocks : kLongParts);
 }
+// Whether a call of so many bytes goes past the caches' order of use: from half of the largest one (256 MB) on.  Eight elements a lane are read or written once, and what the
+// last call left or the next one takes does not stay anyway.  Between a launch that writes the inputs and one that reads the outputs (15,271 rows, 16,384 of gradients): norm to 8 bits
+// 56 -> 45 us, its gradient 104 -> 96, rotation 69 -> 46, its gradient 105 -> 91.  With a quarter of the rows, 68 to 126 MB: 16.2 and 17.6, 30.0 and 31.8, 19.2 and 17.2, 31.3 and
+// 31.9; with a thirty-second 5.2 and 5.8, 12.0, 8.6 and 9.3, 17 and 19.
+bool passes_by(long long bytes) { return bytes >= 128ll << 20; }
 unsigned at_most(long long blocks, long long most) { return (unsigned)(blocks < most ? blocks : most); }
 
-template <class T, bool OUT8, int WAVES> void add_norm_rows(const NormRowsArgs& a, hipStream_t s) {
+template <class T, bool OUT8, int WAVES, bool ONCE> void add_norm_rows(const NormRowsArgs& a, hipStream_t s) {
     const dim3 grid(at_most((a.n_rows + 4 / WAVES - 1) / (4 / WAVES), kMostBlocks)), block(kThreads);
     switch ((a.d + 512 * WAVES - 1) / (512 * WAVES)) {
-        case 1: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 1>), grid, block, 0, s, a); return;
-        case 2: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 2>), grid, block, 0, s, a); return;
-        case 3: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 3>), grid, block, 0, s, a); return;
-        case 4: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 4>), grid, block, 0, s, a); return;
-        case 5: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 5>), grid, block, 0, s, a); return;
-        case 6: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 6>), grid, block, 0, s, a); return;
-        case 7: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 7>), grid, block, 0, s, a); return;
-        case 8: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 8>), grid, block, 0, s, a); return;
+        case 1: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 1, ONCE>), grid, block, 0, s, a); return;
+        case 2: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 2, ONCE>), grid, block, 0, s, a); return;
+        case 3: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 3, ONCE>), grid, block, 0, s, a); return;
+        case 4: hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 4, ONCE>), grid, block, 0, s, a); return;
+        case 5: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 5, ONCE>), grid, block, 0, s, a); return;
+        case 6: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 6, ONCE>), grid, block, 0, s, a); return;
+        case 7: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 7, ONCE>), grid, block, 0, s, a); return;
+        case 8: if constexpr (kMostVecs<T> > 4) hipLaunchKernelGGL((add_norm_kernel<T, OUT8, WAVES, 8, ONCE>), grid, block, 0, s, a); return;
     }
+}
+template <class T, bool OUT8, bool ONCE> void add_norm_wide(const NormRowsArgs& a, int waves, hipStream_t s) {
+    waves == 1 ? add_norm_rows<T, OUT8, 1, ONCE>(a, s) : add_norm_rows<T, OUT8, 4, ONCE>(a, s);
 }
 template <class T> hipError_t add_norm_of(const NormRowsArgs& a, hipStream_t s) {
     const int waves = norm_waves(a.n_rows, a.d, kMostVecs<T>);
     const bool out8 = a.out_scale != nullptr;
     if (!waves) hipLaunchKernelGGL((add_norm_long_kernel<T>), dim3(at_most(a.n_rows, kMostBlocks)), dim3(kThreads), 0, s, a);
-    else if (waves == 1) { if (out8) add_norm_rows<T, true, 1>(a, s); else add_norm_rows<T, false, 1>(a, s); }
-    else if (out8) add_norm_rows<T, true, 4>(a, s);
-    else add_norm_rows<T, false, 4>(a, s);
+    else if (passes_by(a.n_rows * a.d * (long long)(sizeof(T) * (1 + (a.residual != nullptr) + (a.sum != nullptr)) + (out8 ? 1 : sizeof(T)))))
+        out8 ? add_norm_wide<T, true, true>(a, waves, s) : add_norm_wide<T, false, true>(a, waves, s);
+    else out8 ? add_norm_wide<T, true, false>(a, waves, s) : add_norm_wide<T, false, false>(a, waves, s);
     return hipGetLastError();
 }
 
-template <class T, int WAVES> void norm_grad_rows(const NormGradArgs& a, unsigned blocks, hipStream_t s) {
+template <class T, int WAVES, bool ONCE> void norm_grad_rows(const NormGradArgs& a, unsigned blocks, hipStream_t s) {
     const dim3 grid(blocks), block(kThreads);
     switch ((a.d + 512 * WAVES - 1) / (512 * WAVES)) {
-        case 1: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 1>), grid, block, 0, s, a); return;
-        case 2: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 2>), grid, block, 0, s, a); return;
-        case 3: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 3>), grid, block, 0, s, a); return;
-        case 4: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 4>), grid, block, 0, s, a); return;
-        case 5: if constexpr (kMostGradVecs<T> > 4) hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 5>), grid, block, 0, s, a); return;
-        case 6: if constexpr (kMostGradVecs<T> > 4) hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 6>), grid, block, 0, s, a); return;
+        case 1: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 1, ONCE>), grid, block, 0, s, a); return;
+        case 2: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 2, ONCE>), grid, block, 0, s, a); return;
+        case 3: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 3, ONCE>), grid, block, 0, s, a); return;
+        case 4: hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 4, ONCE>), grid, block, 0, s, a); return;
+        case 5: if constexpr (kMostGradVecs<T> > 4) hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 5, ONCE>), grid, block, 0, s, a); return;
+        case 6: if constexpr (kMostGradVecs<T> > 4) hipLaunchKernelGGL((norm_grad_kernel<T, WAVES, 6, ONCE>), grid, block, 0, s, a); return;
     }
 }
 template <class T> hipError_t norm_grad_of(const NormGradArgs& a, hipStream_t s) {
@@ -462,8 +479,9 @@ template <class T> hipError_t norm_grad_of(const NormGradArgs& a, hipStream_t s)
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL((norm_grad_long_kernel<T>), dim3(at_most(a.n_rows, kMostBlocks)), dim3(kThreads), 0, s, a);
-    } else if (waves == 1) norm_grad_rows<T, 1>(a, (unsigned)parts, s);
-    else norm_grad_rows<T, 4>(a, (unsigned)parts, s);
+    } else if (passes_by(a.n_rows * a.d * (long long)sizeof(T) * (3 + (a.dsum != nullptr))))
+        waves == 1 ? norm_grad_rows<T, 1, true>(a, (unsigned)parts, s) : norm_grad_rows<T, 4, true>(a, (unsigned)parts, s);
+    else waves == 1 ? norm_grad_rows<T, 1, false>(a, (unsigned)parts, s) : norm_grad_rows<T, 4, false>(a, (unsigned)parts, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.dgain) return e;
     hipLaunchKernelGGL(add_parts_kernel, dim3((a.d + 31) / 32), dim3(1024), 0, s, a.part, parts, a.d, a.dgain, nullptr, a.d);
@@ -474,12 +492,13 @@ constexpr int kRopeBlocks = 512;              // of the gradient: as many parts
 int rope_grad_blocks(long long n_rows) { return (int)at_most((n_rows + 3) / 4, kRopeBlocks); }
 
 template <class T, int HD> hipError_t rope_impl(const RopeArgs& a, const RopeFreq& f, bool grad, hipStream_t s) {
+    const bool once = passes_by(a.n_rows * (a.side[0].heads + a.side[1].heads) * HD * (long long)sizeof(T) * (grad ? 3 : 2));
     if (!grad) {
-        hipLaunchKernelGGL((norm_rope_kernel<T, HD, false>), dim3(at_most((a.n_rows + 3) / 4, kMostBlocks)), dim3(kThreads), 0, s, a, f);
+        hipLaunchKernelGGL((once ? norm_rope_kernel<T, HD, false, true> : norm_rope_kernel<T, HD, false, false>), dim3(at_most((a.n_rows + 3) / 4, kMostBlocks)), dim3(kThreads), 0, s, a, f);
         return hipGetLastError();
     }
     const int blocks = rope_grad_blocks(a.n_rows);
-    hipLaunchKernelGGL((norm_rope_kernel<T, HD, true>), dim3(blocks), dim3(kThreads), 0, s, a, f);
+    hipLaunchKernelGGL((once ? norm_rope_kernel<T, HD, true, true> : norm_rope_kernel<T, HD, true, false>), dim3(blocks), dim3(kThreads), 0, s, a, f);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
     hipLaunchKernelGGL(add_parts_kernel, dim3(2 * HD / 32), dim3(1024), 0, s, a.part, (long long)blocks, 2 * HD, a.side[0].dgain, a.side[1].dgain, HD);

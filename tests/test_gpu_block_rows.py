@@ -246,6 +246,70 @@ def test_rows_far_apart(sb):
     assert all(torch.equal(a, b) for a, b in zip(*outs))
 
 
+@pytest.mark.parametrize("dtype,n,d,pad,offset", [("bfloat16", 12288, 2051, 5, 1), ("float32", 8192, 2048, 0, 0), ("float16", 8200, 5002, 3, 0)])
+def test_more_than_the_caches_keep(sb, dtype, n, d, pad, offset):
+    """Calls of 200 to 650 MB: of rows, what a call on each quarter of them gives (40 to 110 MB), bit for bit; of the gains, those calls' sums."""
+    import torch
+    torch.manual_seed(9)
+    dt = getattr(torch, dtype)
+
+    def rows(fill=None):
+        whole = torch.full((n * (d + pad) + offset + 8,), 77.0, device="cuda").to(dt)
+        t = whole[offset:offset + n * (d + pad)].view(n, d + pad)[:, :d]
+        if fill is None:
+            t.normal_()
+        return whole, t
+
+    (_, x), (_, res), (_, dy), (_, ds) = (rows() for _ in range(4))
+    gain = 1 + 0.3 * torch.randn(d, device="cuda")
+    hd, heads = 64, d // 64
+    gq, gk = 1 + 0.3 * torch.randn(hd, device="cuda"), 1 + 0.3 * torch.randn(hd, device="cuda")
+    pos = torch.randint(0, 40000, (n,), device="cuda", dtype=torch.int32)
+    q, g = (torch.randn((n, heads, hd), device="cuda").to(dt) for _ in range(2))
+
+    def call(a, b):
+        outs = [rows(0) for _ in range(3)]                    # whole buffers of all rows, of which a call writes its own
+        (_, out), (_, total), (_, dx) = outs
+        out8 = torch.zeros((n, d), dtype=torch.float8_e4m3fn, device="cuda")
+        scale, rstd, dg, dgq, dgk = (torch.zeros(m, device="cuda") for m in (n, n, d, hd, hd))
+        oq, dq = torch.zeros_like(q), torch.zeros_like(q)
+        m = b - a
+        ws = torch.empty(sb.spiral_add_rmsnorm_backward_workspace_bytes(m, d), dtype=torch.uint8, device="cuda")
+        sb.spiral_add_rmsnorm(x[a:b], res[a:b], gain, 1e-6, out[a:b], None, total[a:b], rstd[a:b])
+        sb.spiral_add_rmsnorm(x[a:b], res[a:b], gain, 1e-6, out8[a:b], scale[a:b], None, None)
+        sb.spiral_add_rmsnorm_backward(dy[a:b], total[a:b], gain, rstd[a:b], ds[a:b], dx[a:b], dg, ws)
+        ws = torch.empty(sb.spiral_norm_rope_backward_workspace_bytes(m, heads - 1, 1, hd), dtype=torch.uint8, device="cuda")
+        sides = lambda t: (t[a:b, :-1], t[a:b, -1:])  # noqa: E731
+        sb.spiral_norm_rope(*sides(q), gq, gk, 1e-6, 1e4, pos[a:b], *sides(oq))
+        sb.spiral_norm_rope_backward(*sides(q), *sides(g), gq, gk, 1e-6, 1e4, pos[a:b], *sides(dq), dgq, dgk, ws)
+        return [o[0] for o in outs] + [out8.view(torch.uint8), scale, rstd, oq, dq], [dg, dgq, dgk]
+
+    whole, sums = call(0, n)
+    first = [t.clone() for t in whole]
+    for t in whole[:3]:
+        assert (t[:offset] == 77).all() and (t[-8:] == 77).all() and (not pad or (t[offset:-8].view(n, d + pad)[:, d:] == 77).all())
+    parts = [torch.zeros_like(t, dtype=torch.float64) for t in sums]
+    for i in range(4):
+        a, b = n * i // 4, n * (i + 1) // 4
+        piece, add = call(a, b)
+        for j, (w, p) in enumerate(zip(first, piece)):
+            if j < 3:
+                w, p = (t[offset:-8].view(n, d + pad)[a:b, :d] for t in (w, p))
+            else:
+                w, p = w[a:b], p[a:b]
+            assert torch.equal(w, p), j
+        for t, y in zip(parts, add):
+            t += y.double()
+    # Sums of the gains: a term passes at most 128 additions of 32 bits, of its wave's rows and heads (6 to 30), waves, 16 parts and 32 groups of them, in either order.
+    total = whole[1][offset:-8].view(n, d + pad)[:, :d].double()
+    size = [(dy.double() * total / (total.square().mean(1, keepdim=True) + 1e-6).sqrt()).abs().sum(0)]
+    y, xn = g.double().abs(), (q.double() / (q.double().square().mean(2, keepdim=True) + 1e-6).sqrt()).abs()
+    y += y.roll(hd // 2, 2)                                   # no rotation makes more of a pair
+    size += [(y * xn)[:, :-1].sum((0, 1)), (y * xn)[:, -1].sum(0)]
+    for t, w, m in zip(parts, sums, size):
+        assert ((t - w.double()).abs() <= 2 * 128 * U * m).all()
+
+
 def test_gradients_of_rows_are_those_of_differences(sb):
     import torch
     rng = np.random.default_rng(3)
