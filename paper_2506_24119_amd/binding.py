@@ -580,9 +580,10 @@ _plans = {}                      # of every plan: rows, query heads, kv heads, h
 
 def _heads_of(t, shape, dtype, what: str):
     """(address, row stride) of [rows, heads, head_dim] with a row's heads back to back, of the given shape and type."""
-    s = t.stride()
-    if t.dtype is dtype and t.shape == shape and s[2] == 1 and s[1] == shape[2] and shape[0] > 1:        # asked for once: half the time of a small call's checks
-        return t.data_ptr(), s[0]
+    if t.dtype is dtype and t.shape == shape:                 # each asked for once: half the time of a small call's checks
+        rows, heads, elements = t.stride()
+        if elements == 1 and heads == shape[2] and shape[0] > 1:
+            return t.data_ptr(), rows
     if t.dtype is not dtype or tuple(t.shape) != shape or (shape[2] > 1 and t.stride(2) != 1) or (shape[1] > 1 and t.stride(1) != shape[2]):
         raise ValueError(f"{what}: {shape} of {dtype} with heads back to back is needed, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
     return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
@@ -592,9 +593,10 @@ def _matrix_of(t, n: int, d: int, dtype, what: str):
     """(address, row stride) of [n, d] with contiguous rows, of the given type; None stays None."""
     if t is None:
         return None, 0
-    s = t.stride()
-    if n > 1 and t.dtype is dtype and t.shape == (n, d) and s[1] == 1:
-        return t.data_ptr(), s[0]
+    if n > 1 and t.dtype is dtype and t.shape == (n, d):
+        stride, elements = t.stride()
+        if elements == 1:
+            return t.data_ptr(), stride
     rows, cols, stride = _rows_of(t, what)
     if (rows, cols) != (n, d) or t.dtype is not dtype:
         raise ValueError(f"{what}: {n} x {d} of {dtype} is needed, got {rows} x {cols} of {t.dtype}")
