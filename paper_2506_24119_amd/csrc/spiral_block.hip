@@ -73,14 +73,15 @@ extern "C" int spiral_attention_plan_create(const int32_t* host_lens, int B, int
     if (!p || !seqs || !items) return fail(SPIRAL_ERR_INVALID_ARG, "attention_plan_create: out of host memory");
     int row = 0;
     for (int i = 0; i < B; ++i) { seqs[i] = {row, host_lens[i]}; row += host_lens[i]; }
-    // Workgroups start in this order.  Of rows the longest sequences first, and of each the blocks with the most before them (4,096 tokens' keys of a head fit the L2 of an XCD, so
-    // a sequence's blocks stay together); of tokens the blocks with the most rows behind them, whatever their sequence (16 sequences of U[1024, 4096]: 2.22 -> 2.14 ms,
-    // while the rows' kernels lose 3 % by that).
+    // Workgroups start in this order: those of rows with the most tokens before them and those of tokens with the most rows behind them first, whatever their sequence, so that the last to
+    // start are short.  A sequence's blocks together instead, for the L2's sake: gradients of k and v 2.14 -> 2.22 ms (16 sequences of U[1024, 4096]), forward 36.5 -> 38.5 us (37 of
+    // U[3, 999], 64 dimensions), 128 -> 130 (24 of U[256, 1024]), the rest the same.
     std::sort(seqs.get(), seqs.get() + B, [](const Seq& x, const Seq& y) { return x.len != y.len ? x.len > y.len : x.row0 < y.row0; });
     const int group = n_q_heads / n_kv_heads;
     int4* at = items.get();
     for (int i = 0; i < B; ++i)
         for (long long b = q_blocks(seqs[i].len, group) - 1; b >= 0; --b) *at++ = int4{seqs[i].row0, seqs[i].len, (int)b, 0};
+    std::stable_sort(items.get(), at, [](const int4& x, const int4& y) { return x.z > y.z; });
     for (int i = 0; i < B; ++i)
         for (long long b = 0; b < k_blocks(seqs[i].len); ++b) *at++ = int4{seqs[i].row0, seqs[i].len, (int)b, 0};
     std::stable_sort(items.get() + z.q_items, at, [](const int4& x, const int4& y) { return x.y - 128ll * x.z > y.y - 128ll * y.z; });
