@@ -2,7 +2,7 @@
 // each forward and backward.
 //
 // All are bound by memory: a row's elements are read once, kept in registers while their sum is formed, and written once.  Figures, other inputs each time (a copy of 4 GiB moves 4.8
-// TB/s): addition + norm to 8 bits, 15,271 rows of 2,560 bf16, 274 MB in 50 us; gradient, 16,384 rows of 3,584 bf16, 470 MB in 97 us and 4.4 for the gain's sums; heads 32 + 8
+// TB/s): addition + norm to 8 bits, 15,271 rows of 2,560 bf16, 274 MB in 51 us; gradient, 16,384 rows of 3,584 bf16, 470 MB in 97 us and 4.4 for the gain's sums; heads 32 + 8
 // of 128, 15,271 rows bf16, 313 MB in 65 us; their gradient, 16,384 rows, 503 MB in 96 and 4.6.  A workgroup a row swept three times took 167, 298, and a wave a head with an angle of
 // its own a lane 213 and 616.
 #include <algorithm>
@@ -18,21 +18,28 @@ constexpr float kE4m3Least = 1e-30f;          // a row whose largest |out| is no
 
 // Sums and maxima over a wave without a trip through LDS: rotations within rows of 16 lanes, then exchanges of rows.  Every lane adds the same pairs, so all have
 // the same bits.
-template <int N> __device__ __forceinline__ float row_ror(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xF, 0xF, false)); }
-template <class Op> __device__ __forceinline__ float over_wave(float v, Op op) {
-    v = op(v, row_ror<8>(v));
-    v = op(v, row_ror<4>(v));
-    v = op(v, row_ror<2>(v));
-    v = op(v, row_ror<1>(v));
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
-    v = op(__int_as_float(r[0]), __int_as_float(r[1]));
-    r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+template <int N> __device__ __forceinline__ int row_ror(int x) { return __builtin_amdgcn_update_dpp(0, x, 0x120 + N, 0xF, 0xF, false); }
+template <class Move, class Op> __device__ __forceinline__ float moved(float v, Move move, Op op) {
+    const auto r = move(__float_as_int(v));
     return op(__int_as_float(r[0]), __int_as_float(r[1]));
 }
+template <class Move, class Op> __device__ __forceinline__ double moved(double v, Move move, Op op) {
+    const auto lo = move(__double2loint(v)), hi = move(__double2hiint(v));
+    return op(__hiloint2double(hi[0], lo[0]), __hiloint2double(hi[1], lo[1]));
+}
+template <class V, class Op> __device__ __forceinline__ V over_wave(V v, Op op) {
+    typedef int Two __attribute__((ext_vector_type(2)));
+    v = moved(v, [](int x) { return Two{x, row_ror<8>(x)}; }, op);
+    v = moved(v, [](int x) { return Two{x, row_ror<4>(x)}; }, op);
+    v = moved(v, [](int x) { return Two{x, row_ror<2>(x)}; }, op);
+    v = moved(v, [](int x) { return Two{x, row_ror<1>(x)}; }, op);
+    v = moved(v, [](int x) { const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false); return Two{(int)r[0], (int)r[1]}; }, op);
+    return moved(v, [](int x) { const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false); return Two{(int)r[0], (int)r[1]}; }, op);
+}
 struct Add { __device__ __forceinline__ float operator()(float x, float y) const { return x + y; } };
-struct Most { __device__ __forceinline__ float operator()(float x, float y) const { return x != x || y != y ? NAN : fmaxf(x, y); } };      // undefined where any is
+struct Most { template <class V> __device__ __forceinline__ V operator()(V x, V y) const { return x != x || y != y ? (V)NAN : x > y ? x : y; } };      // undefined where any is
 // over the WAVES waves that share a row
-template <int WAVES, class Op> __device__ __forceinline__ float over_row(float v, float* s, Op op) {
+template <int WAVES, class V, class Op> __device__ __forceinline__ V over_row(V v, V* s, Op op) {
     v = over_wave(v, op);
     if (WAVES == 1) return v;
     __syncthreads();
@@ -48,10 +55,16 @@ __device__ __forceinline__ uint8_t to_e4m3(float v) { return (uint8_t)(__builtin
 __device__ __forceinline__ uint32_t to_e4m3x4(const float* v) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
 }
-// What a row's sum times gain is multiplied by to be encoded (1 / rms is in both the outputs and the largest of them, `most` times it, and left out: one rounding less next
-// to a code's border), and its codes to be decoded; undefined where the row's largest is infinite or undefined.
-__device__ __forceinline__ float code_factor(float most, float rstd) { return most * rstd <= kE4m3Least ? 0.f : most < INFINITY ? 448.f / most : NAN; }
-__device__ __forceinline__ float code_scale(float most, float rstd) { return most * rstd <= kE4m3Least ? 0.f : most < INFINITY ? most * rstd / 448.f : NAN; }
+// Codes are those of the sum times the gain, exact in 64 bits, times 448 over the row's largest (1 / rms is in both and left out), rounded once.  Almost all of them 32 bits
+// tell as well: where less and more than what can be off there give the same code.  (In 32 bits alone 25 of 39 M were others; in 64 bits alone the kernel takes 55 us, this way 51.)
+constexpr float kOff = 0x1p-21f;              // the factor, the product and both their roundings: less than five of 2^-24
+__device__ __forceinline__ double exact_product(float x, float y) { return (double)x * y; }
+// of 20 bits, the last one set where anything is cut off, so that the rounding to 4 bits goes the way it would from all of them
+__device__ __forceinline__ float before_code(double v) { return (float)__hiloint2double(__double2hiint(v) | (int)min((uint32_t)__double2loint(v), 1u), 0); }
+// What the products are multiplied by, and what their codes are multiplied by to be decoded; undefined where the row's largest is infinite or undefined.
+__device__ __forceinline__ bool no_codes(double most, float rstd) { return (float)most * rstd <= kE4m3Least; }
+__device__ __forceinline__ double code_factor(double most, float rstd) { return no_codes(most, rstd) ? 0.0 : most < INFINITY ? 448.0 / most : NAN; }
+__device__ __forceinline__ float code_scale(double most, float rstd) { return no_codes(most, rstd) ? 0.f : most < INFINITY ? (float)most * rstd / 448.f : NAN; }
 
 // Eight neighbouring elements, aligned to one: the wide accesses take any address
 template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
@@ -91,8 +104,9 @@ template <> __device__ __forceinline__ void forget<float>(Eights<float>&) {}
 // A row by one wave or by four, in registers: NV times eight elements a lane.  One read of what there is to read, one write; every load of a row is on its way before
 // its first element is needed.
 template <class T, bool OUT8, int WAVES, int NV, bool ONCE>
-__global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
+__global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_norm_kernel(NormRowsArgs a) {
     __shared__ float s[WAVES];
+    __shared__ double s_most[WAVES];
     constexpr int LANES = 64 * WAVES;
     const Share<LANES, NV> mine{(int)(threadIdx.x % LANES), a.d};
     for (long long r = (long long)blockIdx.x * (4 / WAVES) + threadIdx.x / LANES; r < a.n_rows; r += (long long)gridDim.x * (4 / WAVES)) {
@@ -115,7 +129,8 @@ __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
             }
         const float rstd = 1.f / sqrtf(over_row<WAVES>(sq, s, Add()) / a.d + a.eps);
         if (a.rstd && mine.t == 0) a.rstd[r] = rstd;
-        float most = 0.f;
+        float most = 0.f, bad = 0.f;              // bad: undefined where a product is infinite or undefined
+        const float* gain = a.gain;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             if (a.sum) {
@@ -124,29 +139,59 @@ __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
                 for (int e = 0; e < 8; ++e) y[e] = (T)h[v][e];
                 mine.template put<ONCE>((T*)a.sum + r * a.sum_stride, v, y);
             }
-            const Eights<float> g = eight(a.gain + mine.at(v));
+            const Eights<float> g = eight(gain + mine.at(v));
+            if (OUT8) {                           // (elements that are another lane's as well: they are of the same row)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                h[v][e] *= g[e];
-                if (OUT8) most = e >= mine.skip(v) ? Most()(most, fabsf(h[v][e])) : most;
-            }
-            if (!OUT8) {
+                for (int e = 0; e < 8; ++e) {
+                    const float p = h[v][e] * g[e];
+                    most = fmaxf(most, fabsf(p));
+                    bad = fmaf(p, 0.f, bad);
+                }
+            } else {
                 Eights<T> y;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = (T)(h[v][e] * rstd);
+                for (int e = 0; e < 8; ++e) y[e] = (T)(h[v][e] * g[e] * rstd);
                 mine.template put<ONCE>((T*)a.out + r * a.out_stride, v, y);
             }
         }
         if (OUT8) {
-            most = over_row<WAVES>(most, s, Most());
-            const float inv = code_factor(most, rstd);
+            typedef uint32_t Codes __attribute__((ext_vector_type(2)));
+            most = over_row<WAVES>(bad != bad ? NAN : most, s, Most());
+            const float factor = (float)code_factor(most, rstd), less = factor * (1.f - kOff), more = factor * (1.f + kOff);
             if (mine.t == 0) a.out_scale[r] = code_scale(most, rstd);
+            uint32_t differ = 0;
+            asm volatile("" : "+s"(gain));        // read again, not kept
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
+                const Eights<float> g = eight(gain + mine.at(v));
+                float x[8], y[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[v][e] *= inv;
-                typedef uint32_t Codes __attribute__((ext_vector_type(2)));
-                mine.template put<ONCE>((uint8_t*)a.out + r * a.out_stride, v, Codes{to_e4m3x4(h[v]), to_e4m3x4(h[v] + 4)});
+                for (int e = 0; e < 8; ++e) x[e] = h[v][e] * g[e] * less, y[e] = h[v][e] * g[e] * more;
+                const Codes codes{to_e4m3x4(x), to_e4m3x4(x + 4)};
+                differ |= (codes[0] ^ to_e4m3x4(y)) | (codes[1] ^ to_e4m3x4(y + 4));
+                mine.template put<ONCE>((uint8_t*)a.out + r * a.out_stride, v, codes);
+            }
+            if (over_row<WAVES>(differ ? 1.f : 0.f, s, Add()) != 0.f) {
+                double exact = 0.0;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    asm volatile("" : "+s"(gain) : : "memory");      // eight at a time: a rare path is not to take registers from the other
+                    const Eights<float> g = eight(gain + mine.at(v));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) exact = fmax(exact, fabs(exact_product(h[v][e], g[e])));
+                }
+                const double f = code_factor(over_row<WAVES>(exact, s_most, Most()), rstd);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    asm volatile("" : "+s"(gain) : : "memory");
+                    const Eights<float> g = eight(gain + mine.at(v));
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(h[v][e]));      // nor widened values kept
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = before_code(exact_product(h[v][e], g[e]) * f);
+                    mine.template put<ONCE>((uint8_t*)a.out + r * a.out_stride, v, Codes{to_e4m3x4(x), to_e4m3x4(x + 4)});
+                }
             }
         }
     }
@@ -156,6 +201,7 @@ __global__ __launch_bounds__(kThreads) void add_norm_kernel(NormRowsArgs a) {
 template <class T>
 __global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a) {
     __shared__ float s[kThreads / 64];
+    __shared__ double s_most[kThreads / 64];
     for (long long r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
         const T* x = (const T*)a.x + r * a.x_stride;
         const T* res = a.residual ? (const T*)a.residual + r * a.residual_stride : nullptr;
@@ -164,19 +210,22 @@ __global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a)
         for (int c = threadIdx.x; c < a.d; c += kThreads) { const float h = sum_at(c); sq = fmaf(h, h, sq); }
         const float rstd = 1.f / sqrtf(over_row<4>(sq, s, Add()) / a.d + a.eps);
         if (a.rstd && threadIdx.x == 0) a.rstd[r] = rstd;
-        float inv = 0.f;
+        double factor = 0.0;
         if (a.out_scale) {
-            float most = 0.f;
-            for (int c = threadIdx.x; c < a.d; c += kThreads) most = Most()(most, fabsf(sum_at(c) * a.gain[c]));
-            most = over_row<4>(most, s, Most());
-            inv = code_factor(most, rstd);
+            double most = 0.0;
+            for (int c = threadIdx.x; c < a.d; c += kThreads) {
+                const float h = sum_at(c), g = a.gain[c];
+                most = Most()(most, fabsf(h * g) < INFINITY ? fabs(exact_product(h, g)) : NAN);
+            }
+            most = over_row<4>(most, s_most, Most());
+            factor = code_factor(most, rstd);
             if (threadIdx.x == 0) a.out_scale[r] = code_scale(most, rstd);
         }
         for (int c = threadIdx.x; c < a.d; c += kThreads) {
-            const float h = sum_at(c), y = h * a.gain[c];
+            const float h = sum_at(c), g = a.gain[c];
             if (a.sum) ((T*)a.sum)[r * a.sum_stride + c] = (T)h;
-            if (a.out_scale) ((uint8_t*)a.out)[r * a.out_stride + c] = to_e4m3(y * inv);
-            else ((T*)a.out)[r * a.out_stride + c] = (T)(y * rstd);
+            if (a.out_scale) ((uint8_t*)a.out)[r * a.out_stride + c] = to_e4m3(before_code(exact_product(h, g) * factor));
+            else ((T*)a.out)[r * a.out_stride + c] = (T)(h * g * rstd);
         }
     }
 }

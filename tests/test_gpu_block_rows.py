@@ -246,6 +246,24 @@ def test_rows_far_apart(sb):
     assert all(torch.equal(a, b) for a, b in zip(*outs))
 
 
+@pytest.mark.parametrize("dtype,n,d,residual", [("bfloat16", 3000, 2560, True), ("float16", 2100, 4097, False), ("float32", 2500, 2047, False), ("bfloat16", 700, 8200, True), ("float32", 600, 7001, False),
+                                                ("bfloat16", 300, 16384, True), ("bfloat16", 250, 20001, True), ("float16", 2000000, 5, True)])
+def test_codes_are_those_of_exact_products(sb, dtype, n, d, residual):
+    """5 to 10 million codes, every one that of the 64-bit quotient (32 bits alone have two in three million on a border's other side), also where the sum is written over x."""
+    import torch
+    torch.manual_seed(12)
+    dt = getattr(torch, dtype)
+    some = lambda: (torch.empty((n, d), device="cuda").uniform_(-6, 6).exp2() * torch.randn((n, d), device="cuda").sign()).to(dt)  # noqa: E731
+    x, res = some(), some() if residual else None
+    gain = 1 + 0.3 * torch.randn(d, device="cuda")
+    p = (x.double() + (res.double() if residual else 0)) * gain.double()         # at most 20 bits (one type's without residual) times 24: exact
+    out, scale = torch.empty((n, d), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(n, device="cuda")
+    sb.spiral_add_rmsnorm(x, res, gain, 1e-6, out, scale, x, None)
+    v = p * (448.0 / p.abs().amax(1, keepdim=True))
+    step = torch.exp2(torch.clamp(torch.frexp(v)[1] - 1, min=-6).double() - 3)
+    assert torch.equal(out.double(), torch.round(v / step) * step)
+
+
 @pytest.mark.parametrize("dtype,n,d,pad,offset", [("bfloat16", 12288, 2051, 5, 1), ("float32", 8192, 2048, 0, 0), ("float16", 8200, 5002, 3, 0)])
 def test_more_than_the_caches_keep(sb, dtype, n, d, pad, offset):
     """Calls of 200 to 650 MB: of rows, what a call on each quarter of them gives (40 to 110 MB), bit for bit; of the gains, those calls' sums."""
