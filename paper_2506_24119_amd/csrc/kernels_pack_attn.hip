@@ -177,7 +177,9 @@ template <int HD> struct Bring32 {
     __device__ __forceinline__ void operator()(const void* first, int rows, char* lds, int wave) const { bring(first, rows, lds, wave, off); }
     // with the last row in the place of those past the end; rows >= 1, row: the lane's
     __device__ __forceinline__ void repeat_last(const void* first, int rows, char* lds, int wave, int row) const {
-        bring(first, rows, lds, wave, off - (uint32_t)max(0, row - (rows - 1)) * row_bytes);
+        uint32_t at = off;
+        if (__builtin_amdgcn_readfirstlane(rows) < 32) at -= (uint32_t)max(0, row - (rows - 1)) * row_bytes;      // (asked for, whole tiles do not pay: 62 -> 60 us, 37 of U[3, 999])
+        bring(first, rows, lds, wave, at);
     }
     __device__ __forceinline__ void bring(const void* first, int rows, char* lds, int wave, uint32_t at) const {
         const __amdgpu_buffer_rsrc_t r = buffer_upto(first, __builtin_amdgcn_readfirstlane((uint32_t)max(0, min(rows, 32)) * row_bytes));
