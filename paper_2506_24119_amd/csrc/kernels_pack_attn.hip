@@ -11,12 +11,12 @@
 // Three kernels, seven products where the mathematics has five in the backward pass (s and dp are made twice): one kernel for all would have to add dq from many
 // workgroups, by atomics whose order changes results or by partial sums that take longer than the two products (16 sequences of U[1024, 4096]: 15 GB, 3.1 ms).
 //
-// Bound: the chip's power.  The compute units are busy, the matrix pipes 55 % of their time at 1.9 GHz; with zeros for all inputs the same launches take 17, 23 and 27 % less
-// time.  16 sequences of U[1024, 4096], 32 heads on 8, hd 128, bf16 (41 k rows): forward 1.06 ms (1.0 PFLOP/s), dq 1.70 (0.94), dk and dv 2.10 (1.02 of what is computed);
+// Bound: the chip's power.  The compute units are busy, the matrix pipes 53 to 62 % of their time at 1.9 GHz; with zeros for all inputs the same launches take 17, 23 and 27 % less
+// time.  16 sequences of U[1024, 4096], 32 heads on 8, hd 128, bf16 (41 k rows): forward 1.03 ms (1.04 PFLOP/s), dq 1.69 (0.95), dk and dv 2.12 (1.01 of what is computed);
 // a library product of 16384^3 makes 1.35.  A row alone by one wave, token by token, took 534 ms for the three.
 // On the way: bank-free tiles (64 banks, not 32, serve a wave's reads) 5.1 -> 2.65 ms of dk and dv, whose addresses had been spilled; values in LDS and stages of 32 rows there 2.65 -> 2.24; three
 // forward workgroups a compute unit 1.16 -> 1.06.  Without effect, within 2 %: products interleaved with exponentials instruction by instruction, operand reads further ahead, the two score
-// chains in turn, s_setprio around products, heads in turn over the same rows (L2 hits 28 -> 74 %).  Worse: 64 rows a wave (512 registers, one wave a SIMD: forward
+// chains in turn, s_setprio around products or for long workgroups, the group's heads one after the other or stage by stage (L2 hits 28 -> 74 %).  Worse: 64 rows a wave (512 registers, one wave a SIMD: forward
 // 1.16 -> 2.44 ms), eight waves a workgroup with three stages in flight (1.16 -> 1.39).
 //
 // A row alone: one wave computes one (row, head) of the outputs or of dq, token by token, and reads nothing that the row does not see.  For rows in whose sums a
@@ -289,7 +289,7 @@ template <int TOKENS> struct Unit {
 
 // Stages of 32 tokens, of which the wave's last is the one on the diagonal.  Three workgroups share a compute unit, and what one waits for (its tiles, its barrier, the
 // matrix pipe, its exponentials) the others fill: two of them with stages of 64 tokens, the next stage's scores made under the weights of this one, took
-// 1,160 us where this takes 1,054 (16 sequences of U[1024, 4096], 32 heads on 8), 164 where 143 (24 of U[256, 1024]).
+// 1,160 us where this took 1,054 (16 sequences of U[1024, 4096], 32 heads on 8), 164 where it took 143 (24 of U[256, 1024]).
 template <class T, int HD>
 __global__ __launch_bounds__(256, 3) void pack_forward_kernel(PackArgs a) {
     constexpr int KS = HD / 16, DT = HD / 32, TB = Tile<HD, 32>::BYTES;
