@@ -220,20 +220,11 @@ def _ip(a: Optional[np.ndarray]):
     return None if a is None else a.ctypes.data_as(C.POINTER(C.c_int32))
 
 
-_current_stream = None           # () -> handle, found at the first call that needs it
-
-
-def _find_current_stream():
-    global _current_stream
-    import torch
-    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device      # not a public name: current_stream() without its object, 0.3 us and not 3
-    _current_stream = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
-    return _current_stream
-
-
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
-        return (_current_stream or _find_current_stream())()
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # not a public name: current_stream() without its object, 0.5 us and not 3
+        return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
 
