@@ -57,13 +57,13 @@ __device__ __forceinline__ uint32_t to_e4m3x4(const float* v) {
 }
 // Codes are those of the sum times the gain, exact in 64 bits, times 448 over the row's largest (1 / rms is in both and left out), rounded once.  Almost all of them 32 bits
 // tell as well: where less and more than what can be off there give the same code.  (In 32 bits alone 25 of 39 M were others; in 64 bits alone the kernel takes 55 us, this way 51.)
-constexpr float kOff = 0x1p-21f;              // the factor, the product and both their roundings: less than five of 2^-24
+constexpr float kOff = 0x1.8p-22f;            // six of 2^-24: the largest, the factor, its margin, the product and their product are off by one each
 __device__ __forceinline__ double exact_product(float x, float y) { return (double)x * y; }
 // of 20 bits, the last one set where anything is cut off, so that the rounding to 4 bits goes the way it would from all of them
 __device__ __forceinline__ float before_code(double v) { return (float)__hiloint2double(__double2hiint(v) | (int)min((uint32_t)__double2loint(v), 1u), 0); }
 // What the products are multiplied by, and what their codes are multiplied by to be decoded; undefined where the row's largest is infinite or undefined.
 __device__ __forceinline__ bool no_codes(double most, float rstd) { return (float)most * rstd <= kE4m3Least; }
-__device__ __forceinline__ double code_factor(double most, float rstd) { return no_codes(most, rstd) ? 0.0 : most < INFINITY ? 448.0 / most : NAN; }
+template <class V> __device__ __forceinline__ V code_factor(V most, float rstd) { return no_codes(most, rstd) ? (V)0 : most < INFINITY ? (V)448 / most : (V)NAN; }
 __device__ __forceinline__ float code_scale(double most, float rstd) { return no_codes(most, rstd) ? 0.f : most < INFINITY ? (float)most * rstd / 448.f : NAN; }
 
 // Eight neighbouring elements, aligned to one: the wide accesses take any address
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
         if (OUT8) {
             typedef uint32_t Codes __attribute__((ext_vector_type(2)));
             most = over_row<WAVES>(bad != bad ? NAN : most, s, Most());
-            const float factor = (float)code_factor(most, rstd), less = factor * (1.f - kOff), more = factor * (1.f + kOff);
+            const float factor = code_factor(most, rstd), less = factor * (1.f - kOff), more = factor * (1.f + kOff);
             if (mine.t == 0) a.out_scale[r] = code_scale(most, rstd);
             uint32_t differ = 0;
             asm volatile("" : "+s"(gain));        // read again, not kept
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
                 differ |= (codes[0] ^ to_e4m3x4(y)) | (codes[1] ^ to_e4m3x4(y + 4));
                 mine.template put<ONCE>((uint8_t*)a.out + r * a.out_stride, v, codes);
             }
-            if (over_row<WAVES>(differ ? 1.f : 0.f, s, Add()) != 0.f) {
+            if (WAVES == 1 ? __builtin_amdgcn_ballot_w64(differ != 0) != 0 : __syncthreads_or(differ != 0)) {
                 double exact = 0.0;
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
