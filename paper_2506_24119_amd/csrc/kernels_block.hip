@@ -61,10 +61,19 @@ constexpr float kOff = 0x1.8p-22f;            // six of 2^-24: the largest, the 
 __device__ __forceinline__ double exact_product(float x, float y) { return (double)x * y; }
 // of 20 bits, the last one set where anything is cut off, so that the rounding to 4 bits goes the way it would from all of them
 __device__ __forceinline__ float before_code(double v) { return (float)__hiloint2double(__double2hiint(v) | (int)min((uint32_t)__double2loint(v), 1u), 0); }
-// What the products are multiplied by, and what their codes are multiplied by to be decoded; undefined where the row's largest is infinite or undefined.
-__device__ __forceinline__ bool no_codes(double most, float rstd) { return (float)most * rstd <= kE4m3Least; }
-template <class V> __device__ __forceinline__ V code_factor(V most, float rstd) { return no_codes(most, rstd) ? (V)0 : most < INFINITY ? (V)448 / most : (V)NAN; }
-__device__ __forceinline__ float code_scale(double most, float rstd) { return no_codes(most, rstd) ? 0.f : most < INFINITY ? (float)most * rstd / 448.f : NAN; }
+// Where the row's largest product is below this bound, those that still have a code may be subnormal in 32 bits, off by more than that, and below 2^-119.2 the factor passes 32
+// bits; where it is infinite, the product of a finite sum and gain may be: such rows are left to the 64 bits.
+constexpr float kLeastProduct = 0x1p-100f;
+__device__ __forceinline__ bool in_32_bits(float most) { return most >= kLeastProduct && most < INFINITY; }
+// The larger magnitude, where what is infinite or undefined is larger than all that is not (asked for by comparisons the kernel took 51.7 us, this way 51.0)
+__device__ __forceinline__ double larger(double x, double y) {
+    const uint64_t a = __double_as_longlong(x), b = __double_as_longlong(fabs(y));
+    return __longlong_as_double(a > b ? a : b);
+}
+// What the products are multiplied by, and what their codes are multiplied by to be decoded; undefined where the row's largest is undefined.
+template <class V> __device__ __forceinline__ bool no_codes(V most, float rstd) { return most * rstd <= kE4m3Least; }
+template <class V> __device__ __forceinline__ V code_factor(V most, float rstd) { return no_codes(most, rstd) ? (V)0 : (V)448 / most; }
+template <class V> __device__ __forceinline__ float code_scale(V most, float rstd) { return no_codes(most, rstd) ? 0.f : (float)(most * rstd / (V)448); }
 
 // Eight neighbouring elements, aligned to one: the wide accesses take any address
 template <class T> struct Eight { typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
@@ -159,7 +168,7 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
             most = over_row<WAVES>(bad != bad ? NAN : most, s, Most());
             const float factor = code_factor(most, rstd), less = factor * (1.f - kOff), more = factor * (1.f + kOff);
             if (mine.t == 0) a.out_scale[r] = code_scale(most, rstd);
-            uint32_t differ = 0;
+            uint32_t differ = !in_32_bits(most);
             asm volatile("" : "+s"(gain));        // read again, not kept
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -178,9 +187,11 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
                     asm volatile("" : "+s"(gain) : : "memory");      // eight at a time: a rare path is not to take registers from the other
                     const Eights<float> g = eight(gain + mine.at(v));
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) exact = fmax(exact, fabs(exact_product(h[v][e], g[e])));
+                    for (int e = 0; e < 8; ++e) exact = larger(exact, exact_product(h[v][e], g[e]));
                 }
-                const double f = code_factor(over_row<WAVES>(exact, s_most, Most()), rstd);
+                exact = over_row<WAVES>(exact < INFINITY ? exact : (double)NAN, s_most, Most());
+                const double f = code_factor(exact, rstd);
+                if (!in_32_bits(most) && mine.t == 0) a.out_scale[r] = code_scale(exact, rstd);
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
                     asm volatile("" : "+s"(gain) : : "memory");
@@ -215,9 +226,9 @@ __global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a)
             double most = 0.0;
             for (int c = threadIdx.x; c < a.d; c += kThreads) {
                 const float h = sum_at(c), g = a.gain[c];
-                most = Most()(most, fabsf(h * g) < INFINITY ? fabs(exact_product(h, g)) : NAN);
+                most = larger(most, exact_product(h, g));
             }
-            most = over_row<4>(most, s_most, Most());
+            most = over_row<4>(most < INFINITY ? most : (double)NAN, s_most, Most());
             factor = code_factor(most, rstd);
             if (threadIdx.x == 0) a.out_scale[r] = code_scale(most, rstd);
         }

@@ -1,0 +1,59 @@
+"""spiral_add_rmsnorm where sums times gains are far from 1: 8-bit codes and scales of rows whose products leave the range of 32 bits or its normal numbers.
+
+Bounds, u = 2^-24: 1 / rms is off by u (d / 128 + 16), a scale by four roundings more and its own."""
+import numpy as np
+import pytest
+
+from test_gpu_block_rows import LEAST, U, sb  # noqa: F401  (sb: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def some(dtype, n, d, size, seed):
+    """[n, d] of random signs and three binary orders of magnitude below `size`, a hundredth of them up to 20 orders."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    rand = lambda: torch.rand((n, d), device="cuda", generator=g, dtype=torch.float64)  # noqa: E731
+    x = size * torch.exp2(-3 * rand() - torch.where(rand() < 0.01, 20 * rand(), 0)) * torch.where(rand() < 0.5, -1.0, 1.0)
+    return x.to(getattr(torch, dtype))
+
+
+# the largest products: below 2^-119.2 (448 over it passes 32 bits), 2^-117 (smaller ones are subnormal where they have codes), 2^-145 (all are), 2^133 (past 32 bits)
+SIZES = [("float32", 2.0 ** -119.5, 1.0, 1e-14), ("bfloat16", 2.0 ** -119.5, 1.0, 1e-14), ("float16", 2.0 ** -22, 2.0 ** -98, 1e-14), ("float32", 2.0 ** -117, 1.0, 1e-14), ("bfloat16", 2.0 ** -117, 1.0, 1e-14),
+         ("float32", 2.0 ** -60, 2.0 ** -85, 0.0), ("bfloat16", 2.0 ** -60, 2.0 ** -85, 0.0), ("float32", 2.0 ** 50, 2.0 ** 83, 1e-6), ("bfloat16", 2.0 ** 50, 2.0 ** 83, 1e-6)]
+
+
+def exact(x, gain, eps):
+    """(sum times gain, 1 / rms) in 64 bits"""
+    h = x.double()
+    return h * gain.double(), 1 / (h.square().mean(1, keepdim=True) + float(np.float32(eps))).sqrt()
+
+
+def gain_of(d, size):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d)
+    return (size * (0.7 + 0.3 * torch.rand(d, device="cuda", generator=g, dtype=torch.float64))).float()
+
+
+@pytest.mark.parametrize("n,d", [(6, 100), (3, 2560), (5, 20000), (2100, 130), (2049, 2560), (7, 5)])
+@pytest.mark.parametrize("dtype,size,gain_size,eps", SIZES)
+def test_codes_of_products_far_from_one(sb, n, d, dtype, size, gain_size, eps):  # noqa: F811
+    """Beside rows of ordinary size, which keep theirs."""
+    import torch
+    x = some(dtype, n, d, size, n + d)
+    gain = gain_of(d, gain_size)
+    ordinary = torch.arange(n, device="cuda") % 3 == 1
+    if gain_size == 1.0:                                      # (a gain far from 1 is every row's)
+        x[ordinary] = some(dtype, n, d, 1.0, 3)[ordinary]
+    out, scale = torch.full((n, d), 1.0, device="cuda").to(torch.float8_e4m3fn), torch.full((n,), 5.0, device="cuda")
+    sb.spiral_add_rmsnorm(x, None, gain, eps, out, scale)
+    p, rstd = exact(x, gain, eps)
+    most = p.abs().amax(1, keepdim=True)
+    assert (most * rstd > 1.01e-30).all() and (most * rstd < 3e38).all()
+    v = p * (448.0 / most)
+    step = torch.exp2(torch.clamp(torch.frexp(v)[1] - 1, min=-6).double() - 3)
+    assert torch.equal(out.double(), torch.round(v / step) * step)
+    want = (most * rstd / 448)[:, 0]
+    assert ((scale.double() - want).abs() <= U * (d / 128 + 21) * want + LEAST["float32"]).all()
