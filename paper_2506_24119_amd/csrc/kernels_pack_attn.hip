@@ -575,7 +575,8 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) dp = mma<T>(at.by_row(ot, 0, ks), at_v.by_row(vt, wave & 1, ks), dp);
             // Rows before the lane's token.  Asked with a uniform `cut` first, whole stages pay nothing (128 dimensions, 16 sequences of U[1024, 4096]: 2.18 -> 2.09 ms);
-            // where products are half as long, one comparison and one choice an element are cheaper than what becomes of that (64 dimensions, 37 of U[3, 999]: 71 -> 66 us).
+            // where products are half as long, a comparison and two choices an element are cheaper than what becomes of that (64 dimensions, 37 of U[3, 999], forward and backward:
+            // 156 us, this way 151.5; 154 with t itself chosen).  dp - D is chosen as well as p: 0 times what passes 32 bits, dout . v of rows that do not see a large v, would be undefined.
             const bool cut = q0 < tok0 + 31;
             const int first_row = cut ? tok0 + l32 - q0 - lh * 4 : -1;
             u32x4 p[2], t[2];
@@ -586,8 +587,9 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     x[e] = __builtin_amdgcn_exp2f(fmaf(s[4 * b + e], a.scale_log2e, -lse2[e]));
-                    if (HD < 128 && b * 8 + e < first_row) x[e] = 0.f;
-                    y[e] = x[e] * (dp[4 * b + e] - delta[e]);
+                    float along = dp[4 * b + e] - delta[e];
+                    if (HD < 128 && b * 8 + e < first_row) x[e] = along = 0.f;
+                    y[e] = x[e] * along;
                     if (HD == 128 && cut && q0 + b * 8 + lh * 4 + e < tok0 + l32) x[e] = y[e] = 0.f;
                 }
                 p[b >> 1][(b & 1) * 2] = pack2<T>(x[0], x[1]); p[b >> 1][(b & 1) * 2 + 1] = pack2<T>(x[2], x[3]);

@@ -1,4 +1,4 @@
-"""What a position does not see, in every width of head: undefined and infinite elements of hidden tokens, keys that weigh nothing.
+"""What a position does not see, in every width of head: undefined, infinite and very large elements of hidden tokens, keys that weigh nothing.
 
 Bounds are those of the packed attention's other tests, of the elements that are compared."""
 import numpy as np
@@ -62,4 +62,26 @@ def test_rows_before_a_key_that_weighs_nothing(sb, dtype, hq, hkv, hd):  # noqa:
     torch.cuda.synchronize()
     check_dq(c, np.r_[0:30, 50:88, 120:137])
     check_backward(c)
+    c.free()
+
+
+@pytest.mark.parametrize("hq,hkv,hd", WIDTHS + [(2, 2, 64), (16, 1, 32)])
+def test_large_values_that_rows_do_not_see(sb, hq, hkv, hd):  # noqa: F811
+    """A value whose product with the gradients of rows before it passes 32 bits: it is finite and hidden from them, its own rows have no gradient, so dk and dv of it are 0."""
+    import torch
+    c = Call(sb, [40, 101], hq, hkv, hd, "bfloat16", seed=51)
+    tokens = [20, 39, 40 + 45, 40 + 100]
+    for a, b, token in ((0, 20, 20), (40, 85, 85)):
+        c.dout[a:b] = 100.0
+        c.v[token] = 3e37
+    c.v[39], c.v[140] = 3e37, 3e37
+    c.dout[20:40] = 0.0
+    c.dout[85:] = 0.0
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    check_backward(c)
+    for t in (c.dq, c.dk, c.dv):
+        assert torch.isfinite(t).all()
+    assert not c.dk[tokens].any() and not c.dv[tokens].any()
     c.free()
