@@ -505,6 +505,11 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
 // them).  Keys stay in registers, values in LDS: with both in registers, beside two accumulators, there are too few left to read operands ahead.
 // A wave's last stages are those of its tokens' own rows, some of which do not see some tokens.  Where one of these rows is not finite, as its lse (of q) or D (of dout) then
 // is, the stage is left out, as a weight of 0 would not keep it out of the sums; this head's rows and those of the heads behind it are then added pair by pair.
+// In half precision, whose normal numbers end at 2^-14, the p of dv are 2^12 times as large, from exponents that are 12 more, and their sums 2^12 times less at the end: p of long
+// histories, and of tokens beside one that takes nearly all, keep their bits down to 2^-26 (p is at most 1, but for the roundings of large scores, so none passes the range).
+// dp - D is made 2^12 times less, and t is what it was.
+template <class T> constexpr int kUp = std::is_same_v<T, _Float16> ? 12 : 0;
+template <class T> constexpr float kDown = 1.f / (1 << kUp<T>);
 template <int HD> constexpr int kDkvBytes = 2 * Tile<HD>::BYTES + 4 * Tile<HD, 32>::BYTES + 512;
 template <class T, int HD, bool PARTS>
 __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
@@ -512,7 +517,7 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     static_assert(4 * kPutBytes<HD> <= kDkvBytes<HD>, "results leave through the same LDS");
     char* const stages_lds = lds + 2 * Tile<HD>::BYTES;                          // [stage parity][queries, gradients]
-    float* const s_row = (float*)(stages_lds + 4 * TB);                         // [stage parity][lse2, delta][row]
+    float* const s_row = (float*)(stages_lds + 4 * TB);                         // [stage parity][lse2, -delta][row]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
     const int4 it = a.k_items[a.first_item + blockIdx.y];
     const int row0 = it.x, len = it.y, block0 = it.z * 128, G = a.n_q_heads / a.n_kv_heads;
@@ -535,7 +540,7 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
         if (++next_h == h1) { next_h = h0; next_q -= 32; }
     };
     auto park = [&](int st) {                     // rows that are not there weigh nothing
-        if (wave == 0) s_row[(st & 1) * 64 + lane] = lh ? (row_there ? row_value : 0.f) : row_there ? row_value * kLog2e : INFINITY;
+        if (wave == 0) s_row[(st & 1) * 64 + lane] = lh ? (row_there ? -row_value : 0.f) : row_there ? fmaf(row_value, kLog2e, (float)-kUp<T>) : INFINITY;
     };
     {
         const Bring<HD> bring_v(a.v_stride, wave, lane);
@@ -569,7 +574,13 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
             if (__builtin_amdgcn_ballot_w64(there && !(fabsf(x) < INFINITY)) != 0) alone_from = min(alone_from, h);
         }
         if (n_valid > 0 && (q0 > tok0 || (q0 == tok0 && h < alone_from))) {
-            f32x16 s = zeros(), dp = zeros();
+            f32x16 s = zeros(), dp;               // dp - D: its sums start at -D, which pays for the factor below (37 of U[3, 999], fp16: 151.5 us, 154.5 with the factor alone, 151 so)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const f32x4 d = *(const f32x4*)(rows + 32 + b * 8);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dp[4 * b + e] = d[e];
+            }
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) s = mma<T>(at.by_row(qt, 0, ks), kf[ks], s);
 #pragma unroll
@@ -582,12 +593,12 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
             u32x4 p[2], t[2];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const f32x4 lse2 = *(const f32x4*)(rows + b * 8), delta = *(const f32x4*)(rows + 32 + b * 8);
+                const f32x4 lse2 = *(const f32x4*)(rows + b * 8);
                 float x[4], y[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     x[e] = __builtin_amdgcn_exp2f(fmaf(s[4 * b + e], a.scale_log2e, -lse2[e]));
-                    float along = dp[4 * b + e] - delta[e];
+                    float along = dp[4 * b + e] * kDown<T>;
                     if (HD < 128 && b * 8 + e < first_row) x[e] = along = 0.f;
                     y[e] = x[e] * along;
                     if (HD == 128 && cut && q0 + b * 8 + lh * 4 + e < tok0 + l32) x[e] = y[e] = 0.f;
@@ -624,13 +635,14 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
             sc += __shfl_xor(sc, 32, 64);
             dp += __shfl_xor(dp, 32, 64);
             const float p = exp2f(sc * a.scale_log2e - a.lse[(size_t)g * a.n_rows + first + i] * kLog2e), t = p * (dp - a.delta[(size_t)g * a.n_rows + first + i]);
+            const float up = p * (float)(1 << kUp<T>);
             if (l32 <= i && there)
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int at_d = d * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
-                        dv[d][r] = fmaf(p, (float)o[at_d], dv[d][r]);
+                        dv[d][r] = fmaf(up, (float)o[at_d], dv[d][r]);
                         dk[d][r] = fmaf(t, (float)q[at_d], dk[d][r]);
                         asm volatile("" ::: "memory");      // a few loads at a time: more would take the registers that the loop above needs
                     }
@@ -652,7 +664,7 @@ __global__ __launch_bounds__(256, 2) void pack_dkv_kernel(PackArgs a) {
         char* mine = lds + wave * kPutBytes<HD>;
         put_rows<T, HD>(dk, a.scale, mine, (T*)a.dk + first * a.dk_stride + kvh * HD, a.dk_stride, n_valid, lane);
         __builtin_amdgcn_wave_barrier();
-        put_rows<T, HD>(dv, 1.f, mine, (T*)a.dv + first * a.dv_stride + kvh * HD, a.dv_stride, n_valid, lane);
+        put_rows<T, HD>(dv, kDown<T>, mine, (T*)a.dv + first * a.dv_stride + kvh * HD, a.dv_stride, n_valid, lane);
     }
 }
 
@@ -670,7 +682,7 @@ __global__ __launch_bounds__(256) void pack_join_kernel(PackArgs a, int width) {
     }
     const size_t j = is_v ? i - plane : i, row = j / width;
     T* to = (is_v ? (T*)a.dv + row * a.dv_stride : (T*)a.dk + row * a.dk_stride) + (j - row * width);
-    const float c = is_v ? 1.f : a.scale;
+    const float c = is_v ? kDown<T> : a.scale;
     *(u32x4*)to = u32x4{pack2<T>(g[0] * c, g[1] * c), pack2<T>(g[2] * c, g[3] * c), pack2<T>(g[4] * c, g[5] * c), pack2<T>(g[6] * c, g[7] * c)};
 }
 

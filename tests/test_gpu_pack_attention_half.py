@@ -1,0 +1,42 @@
+"""Weights far below half precision's normal range: a first token that takes nearly all of every row leaves the others 2^-20.
+
+Bounds are those of the packed attention's other tests without what they grant weights below half precision's normal range."""
+import numpy as np
+import pytest
+
+from oracle import block as ob
+from test_gpu_pack_attention import HALF, Call, close, sb  # noqa: F401  (sb: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 2, 32), (2, 2, 64), (4, 2, 64), (3, 3, 128), (7, 1, 128)])
+@pytest.mark.parametrize("undefined", [False, True])
+def test_values_of_small_weights(sb, dtype, hq, hkv, hd, undefined):  # noqa: F811
+    """dv of tokens that every row weighs 2^-20: each weight is rounded by half a step of itself, also by heads shared out and where a row is undefined."""
+    import torch
+    lens = [200, 33]
+    c = Call(sb, lens, hq, hkv, hd, dtype, seed=61, dscale=1024.0)
+    c.q[:, :, 0] = 4.0
+    c.k[:, :, 0] = 0.0
+    c.k[[0, 200], :, 0] = 14.0 * float(np.sqrt(hd)) / 4.0
+    if undefined:
+        c.dout[70, 0, 1] = float("nan")
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    half = HALF[dtype]
+    q, k, v, dout, got = c.host("q", "k", "v", "dout", "dv")
+    (_, _, want), (_, _, size) = ob.attention_grad(q, k, v, dout, lens, c.scale)
+    E = c.errors().max() + hd * 2.0 ** -23
+    allowed = (half + 4 * E) * np.where(np.isfinite(size), size, 0) + half * np.abs(np.where(np.isfinite(want), want, 0)) * (1 + half) + 2.0 ** -25
+    if dtype == "float16":                                    # the first token's own passes its range, as an infinity
+        past = np.abs(want) > 65520 + allowed
+        assert (got[past] == np.copysign(np.inf, want[past])).all()
+        near = (np.abs(want) > 65504 - allowed) & ~past
+        want = np.where(past | near, np.inf, want)
+    close(got, want, allowed, "dv")
+    for x in c.host("dq", "dk")[:2 * (not undefined)]:
+        assert np.isfinite(x).all()
+    c.free()
