@@ -411,7 +411,7 @@ int    spiral_attention_backward(const spiral_attention_plan* plan, const void* 
  *     sum = x + residual ,  rstd = (mean_c sum_c^2 + eps)^(-1/2) ,  out_c = gain_c rstd sum_c                a row of d elements each
  * in fp32; `sum` is rounded where it is written, not before it is normed.  dev_residual NULL: sum = x (dev_sum, where given, is a copy of it).
  * out_dtype: that of x, or SPIRAL_DTYPE_E4M3: codes under an fp32 scale a row, out = code * dev_out_scale[row], scale = the row's largest |out| / 448
- * (0, with codes of 0, where that is at most 1e-30), codes rounded to nearest even from gain sum 448 / its largest in 64 bits; a row whose sum or gain has a NaN or an infinity has scale NaN and codes NaN.
+ * (0, with codes of 0, where that is at most 1e-30), codes rounded to nearest even from gain sum 448 / its largest in 64 bits, the sum of FP32 too; a row whose sum or gain has a NaN or an infinity has scale NaN and codes NaN.
  * dev_x, dev_residual, dev_sum, dev_out: [n_rows, d], rows `stride` elements apart, aligned to an element; x, residual and sum of `dtype` (FP32, BF16, FP16).  dev_gain
  * fp32 [d].  dev_sum, dev_rstd (fp32 [n_rows]) may be NULL; dev_sum may be dev_x or dev_residual itself (same pointer and stride).
  * Backward, for gradients dout of out and dsum of sum (the residual branch's; NULL: none), with the sum and rstd that the forward call wrote:

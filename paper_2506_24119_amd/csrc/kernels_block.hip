@@ -57,14 +57,22 @@ __device__ __forceinline__ uint32_t to_e4m3x4(const float* v) {
 }
 // Codes are those of the sum times the gain, exact in 64 bits, times 448 over the row's largest (1 / rms is in both and left out), rounded once.  Almost all of them 32 bits
 // tell as well: where less and more than what can be off there give the same code.  (In 32 bits alone 25 of 39 M were others; in 64 bits alone the kernel takes 55 us, this way 51.)
-constexpr float kOff = 0x1.8p-22f;            // six of 2^-24: the largest, the factor, its margin, the product and their product are off by one each
+// The sum itself is one of 64 bits where its parts are of 32 (in 32 bits half as many codes were others as with no 64 bits at all); of 16-bit parts 32 bits hold it, but for the last
+// bits of parts 2^13 and more apart: one code in 10^8, for which the kernel would take 54 us.
+template <class T> constexpr bool kWideSum = sizeof(T) == 4;
+// eight of 2^-24: the sum, its product, both of the largest, the factor, its margin and their product are off by one each
+constexpr float kOff = 0x1p-21f;
 __device__ __forceinline__ double exact_product(float x, float y) { return (double)x * y; }
+__device__ __forceinline__ double exact_product(float x, float residual, float y) {
+    const float sum = x + residual;
+    return (fabsf(sum) < INFINITY ? (double)x + residual : (double)sum) * y;
+}
 // of 20 bits, the last one set where anything is cut off, so that the rounding to 4 bits goes the way it would from all of them
 __device__ __forceinline__ float before_code(double v) { return (float)__hiloint2double(__double2hiint(v) | (int)min((uint32_t)__double2loint(v), 1u), 0); }
 // Where the row's largest product is below this bound, those that still have a code may be subnormal in 32 bits, off by more than that, and below 2^-119.2 the factor passes 32
-// bits; where it is infinite, the product of a finite sum and gain may be: such rows are left to the 64 bits.
+// bits; where it is infinite, the product of a finite sum and gain may be: such rows are left to the 64 bits (but for those that hold zeros in any case).
 constexpr float kLeastProduct = 0x1p-100f;
-__device__ __forceinline__ bool in_32_bits(float most) { return most >= kLeastProduct && most < INFINITY; }
+__device__ __forceinline__ bool in_32_bits(float most, float rstd) { return (most >= kLeastProduct || (most + 0x1p-148f) * rstd < 0.99f * kE4m3Least) && most < INFINITY; }
 // The larger magnitude, where what is infinite or undefined is larger than all that is not (asked for by comparisons the kernel took 51.7 us, this way 51.0)
 __device__ __forceinline__ double larger(double x, double y) {
     const uint64_t a = __double_as_longlong(x), b = __double_as_longlong(fabs(y));
@@ -140,14 +148,17 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
         if (a.rstd && mine.t == 0) a.rstd[r] = rstd;
         float most = 0.f, bad = 0.f;              // bad: undefined where a product is infinite or undefined
         const float* gain = a.gain;
+        const bool late = OUT8 && kWideSum<T> && (a.sum == a.x || a.sum == a.residual);      // over what open codes are made of
+        auto put_sum = [&](int v) {
+            if (!a.sum) return;
+            Eights<T> y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = (T)h[v][e];
+            mine.template put<ONCE>((T*)a.sum + r * a.sum_stride, v, y);
+        };
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if (a.sum) {
-                Eights<T> y;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = (T)h[v][e];
-                mine.template put<ONCE>((T*)a.sum + r * a.sum_stride, v, y);
-            }
+            if (!late) put_sum(v);
             const Eights<float> g = eight(gain + mine.at(v));
             if (OUT8) {                           // (elements that are another lane's as well: they are of the same row)
 #pragma unroll
@@ -168,7 +179,7 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
             most = over_row<WAVES>(bad != bad ? NAN : most, s, Most());
             const float factor = code_factor(most, rstd), less = factor * (1.f - kOff), more = factor * (1.f + kOff);
             if (mine.t == 0) a.out_scale[r] = code_scale(most, rstd);
-            uint32_t differ = !in_32_bits(most);
+            uint32_t differ = !in_32_bits(most, rstd);
             asm volatile("" : "+s"(gain));        // read again, not kept
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -181,29 +192,74 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
                 mine.template put<ONCE>((uint8_t*)a.out + r * a.out_stride, v, codes);
             }
             if (WAVES == 1 ? __builtin_amdgcn_ballot_w64(differ != 0) != 0 : __syncthreads_or(differ != 0)) {
-                double exact = 0.0;
+                if constexpr (!kWideSum<T>) {
+                    double exact = 0.0;
 #pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    asm volatile("" : "+s"(gain) : : "memory");      // eight at a time: a rare path is not to take registers from the other
-                    const Eights<float> g = eight(gain + mine.at(v));
+                    for (int v = 0; v < NV; ++v) {
+                        asm volatile("" : "+s"(gain) : : "memory");      // eight at a time: a rare path is not to take registers from the other
+                        const Eights<float> g = eight(gain + mine.at(v));
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) exact = larger(exact, exact_product(h[v][e], g[e]));
-                }
-                exact = over_row<WAVES>(exact < INFINITY ? exact : (double)NAN, s_most, Most());
-                const double f = code_factor(exact, rstd);
-                if (!in_32_bits(most) && mine.t == 0) a.out_scale[r] = code_scale(exact, rstd);
+                        for (int e = 0; e < 8; ++e) exact = larger(exact, exact_product(h[v][e], g[e]));
+                    }
+                    exact = over_row<WAVES>(exact < INFINITY ? exact : (double)NAN, s_most, Most());
+                    const double f = code_factor(exact, rstd);
+                    if (!in_32_bits(most, rstd) && mine.t == 0) a.out_scale[r] = code_scale(exact, rstd);
 #pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    asm volatile("" : "+s"(gain) : : "memory");
-                    const Eights<float> g = eight(gain + mine.at(v));
-                    float x[8];
+                    for (int v = 0; v < NV; ++v) {
+                        asm volatile("" : "+s"(gain) : : "memory");
+                        const Eights<float> g = eight(gain + mine.at(v));
+                        float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(h[v][e]));      // nor widened values kept
+                        for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(h[v][e]));      // nor widened values kept
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = before_code(exact_product(h[v][e], g[e]) * f);
-                    mine.template put<ONCE>((uint8_t*)a.out + r * a.out_stride, v, Codes{to_e4m3x4(x), to_e4m3x4(x + 4)});
+                        for (int e = 0; e < 8; ++e) x[e] = before_code(exact_product(h[v][e], g[e]) * f);
+                        mine.template put<ONCE>((uint8_t*)a.out + r * a.out_stride, v, Codes{to_e4m3x4(x), to_e4m3x4(x + 4)});
+                    }
+                } else {
+                    // The elements that may be the largest and those whose codes are open, one by one, read again.  (All of them, from registers: 11.1 us for 200 rows of 8,192, this
+                    // way 8.9, and 62 for 8,192 of 2,560, this way 63.)
+                    const bool told = in_32_bits(most, rstd);
+                    uint32_t largest = 0, open = 0;
+                    if (told) {
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) {
+                            const Eights<float> g = eight(gain + mine.at(v));
+                            float below[8], above[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float p = h[v][e] * g[e];
+                                below[e] = p * less, above[e] = p * more;
+                                if (fabsf(p) >= most * (1.f - kOff)) largest |= 1u << (8 * v + e);
+                            }
+#pragma unroll
+                            for (int b = 0; b < 8; b += 4) {
+                                const uint32_t d = to_e4m3x4(below + b) ^ to_e4m3x4(above + b);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if ((d >> (8 * e)) & 0xFF) open |= 1u << (8 * v + b + e);
+                            }
+                        }
+                    } else largest = open = ~0u >> (32 - 8 * NV);
+                    auto next = [&](uint32_t& left, int& v, int& e) { const int i = __builtin_ctz(left); left &= left - 1; v = i >> 3; e = i & 7; };
+                    auto product = [&](int c) { return exact_product(x[c], res ? res[c] : 0.f, gain[c]); };
+                    double exact = 0.0;
+                    int v, e;
+                    while (largest) {
+                        next(largest, v, e);
+                        exact = larger(exact, product(mine.at(v) + e));
+                    }
+                    exact = over_row<WAVES>(exact < INFINITY ? exact : (double)NAN, s_most, Most());
+                    const double f = code_factor(exact, rstd);
+                    if (!told && mine.t == 0) a.out_scale[r] = code_scale(exact, rstd);
+                    while (open) {
+                        next(open, v, e);
+                        if (e >= mine.skip(v)) ((uint8_t*)a.out)[r * a.out_stride + mine.at(v) + e] = to_e4m3(before_code(product(mine.at(v) + e) * f));
+                    }
                 }
             }
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                if (late) put_sum(v);
         }
     }
 }
@@ -217,6 +273,7 @@ __global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a)
         const T* x = (const T*)a.x + r * a.x_stride;
         const T* res = a.residual ? (const T*)a.residual + r * a.residual_stride : nullptr;
         auto sum_at = [&](int c) { return (float)x[c] + (res ? (float)res[c] : 0.f); };
+        auto product_at = [&](int c, float h) { return kWideSum<T> && res ? exact_product((float)x[c], (float)res[c], a.gain[c]) : exact_product(h, a.gain[c]); };
         float sq = 0.f;
         for (int c = threadIdx.x; c < a.d; c += kThreads) { const float h = sum_at(c); sq = fmaf(h, h, sq); }
         const float rstd = 1.f / sqrtf(over_row<4>(sq, s, Add()) / a.d + a.eps);
@@ -224,19 +281,16 @@ __global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a)
         double factor = 0.0;
         if (a.out_scale) {
             double most = 0.0;
-            for (int c = threadIdx.x; c < a.d; c += kThreads) {
-                const float h = sum_at(c), g = a.gain[c];
-                most = larger(most, exact_product(h, g));
-            }
+            for (int c = threadIdx.x; c < a.d; c += kThreads) most = larger(most, product_at(c, sum_at(c)));
             most = over_row<4>(most < INFINITY ? most : (double)NAN, s_most, Most());
             factor = code_factor(most, rstd);
             if (threadIdx.x == 0) a.out_scale[r] = code_scale(most, rstd);
         }
         for (int c = threadIdx.x; c < a.d; c += kThreads) {
             const float h = sum_at(c), g = a.gain[c];
-            if (a.sum) ((T*)a.sum)[r * a.sum_stride + c] = (T)h;
-            if (a.out_scale) ((uint8_t*)a.out)[r * a.out_stride + c] = to_e4m3(before_code(exact_product(h, g) * factor));
+            if (a.out_scale) ((uint8_t*)a.out)[r * a.out_stride + c] = to_e4m3(before_code(product_at(c, h) * factor));
             else ((T*)a.out)[r * a.out_stride + c] = (T)(h * g * rstd);
+            if (a.sum) ((T*)a.sum)[r * a.sum_stride + c] = (T)h;
         }
     }
 }

@@ -1,4 +1,5 @@
-"""spiral_add_rmsnorm where sums times gains are far from 1: 8-bit codes and scales of rows whose products leave the range of 32 bits or its normal numbers.
+"""spiral_add_rmsnorm where 32 bits do not tell: 8-bit codes and scales of rows whose products of sums and gains leave their range or their normal numbers, codes of sums that
+they do not hold.
 
 Bounds, u = 2^-24: 1 / rms is off by u (d / 128 + 16), a scale by four roundings more and its own."""
 import numpy as np
@@ -57,3 +58,23 @@ def test_codes_of_products_far_from_one(sb, n, d, dtype, size, gain_size, eps): 
     assert torch.equal(out.double(), torch.round(v / step) * step)
     want = (most * rstd / 448)[:, 0]
     assert ((scale.double() - want).abs() <= U * (d / 128 + 21) * want + LEAST["float32"]).all()
+
+
+@pytest.mark.parametrize("n,d", [(4000, 2560), (700, 8200), (40, 20001), (2100, 4090), (300000, 5)])
+@pytest.mark.parametrize("dtype,apart", [("float32", 0), ("float32", 12), ("bfloat16", 17), ("float16", 16)])
+@pytest.mark.parametrize("place", ["apart", "over x", "over residual", "none"])
+def test_codes_of_sums_that_32_bits_do_not_hold(sb, n, d, dtype, apart, place):  # noqa: F811
+    """Sums of more than 24 bits, x `apart` orders of magnitude below the residual stream: every code that of the 64-bit quotient, of sums in 64 bits where their parts are of 32
+    and in 32 where they are of 16, wherever the sum goes."""
+    import torch
+    x, res = some(dtype, n, d, 4.0 * 2.0 ** -apart, n), some(dtype, n, d, 4.0, d)
+    gain = gain_of(d, 1.0)
+    p = (x.double() + res.double() if dtype == "float32" else (x.float() + res.float()).double()) * gain.double()
+    total = (x.float() + res.float()).to(x.dtype)
+    out, scale = torch.empty((n, d), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(n, device="cuda")
+    into = {"apart": torch.empty_like(x), "over x": x, "over residual": res, "none": None}[place]
+    sb.spiral_add_rmsnorm(x, res, gain, 1e-6, out, scale, into)
+    v = p * (448.0 / p.abs().amax(1, keepdim=True))
+    step = torch.exp2(torch.clamp(torch.frexp(v)[1] - 1, min=-6).double() - 3)
+    assert torch.equal(out.double(), torch.round(v / step) * step)
+    assert into is None or torch.equal(into, total)
