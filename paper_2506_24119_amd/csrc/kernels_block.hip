@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
             } else {
                 Eights<T> y;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = (T)(h[v][e] * g[e] * rstd);
+                for (int e = 0; e < 8; ++e) y[e] = (T)(h[v][e] * rstd * g[e]);      // (in this order: at most sqrt(d) times the gain on the way)
                 mine.template put<ONCE>((T*)a.out + r * a.out_stride, v, y);
             }
         }
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kThreads) void add_norm_long_kernel(NormRowsArgs a)
         for (int c = threadIdx.x; c < a.d; c += kThreads) {
             const float h = sum_at(c), g = a.gain[c];
             if (a.out_scale) ((uint8_t*)a.out)[r * a.out_stride + c] = to_e4m3(before_code(product_at(c, h) * factor));
-            else ((T*)a.out)[r * a.out_stride + c] = (T)(h * g * rstd);
+            else ((T*)a.out)[r * a.out_stride + c] = (T)(h * rstd * g);
             if (a.sum) ((T*)a.sum)[r * a.sum_stride + c] = (T)h;
         }
     }
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(RopeArgs a, RopeFre
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         float p = (float)lo[e], q = (float)hi[e];
-                        if (norm) p *= rstd * gain[i][0][e], q *= rstd * gain[i][1][e];
+                        if (norm) p = p * rstd * gain[i][0][e], q = q * rstd * gain[i][1][e];
                         const float2 y = rotate_pair(p, q, cs[e], sn[e]);
                         olo[e] = (T)y.x; ohi[e] = (T)y.y;
                     }

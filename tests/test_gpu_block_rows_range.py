@@ -1,11 +1,11 @@
 """spiral_add_rmsnorm where 32 bits do not tell: 8-bit codes and scales of rows whose products of sums and gains leave their range or their normal numbers, codes of sums that
-they do not hold.
+they do not hold, outputs whose products of sum and gain, or of 1 / rms and gain, they do not.
 
-Bounds, u = 2^-24: 1 / rms is off by u (d / 128 + 16), a scale by four roundings more and its own."""
+Bounds, u = 2^-24: 1 / rms is off by u (d / 128 + 16), a scale by four roundings more and its own, an output by that and half a step of its type."""
 import numpy as np
 import pytest
 
-from test_gpu_block_rows import LEAST, U, sb  # noqa: F401  (sb: the fixture)
+from test_gpu_block_rows import HALF, LEAST, U, sb  # noqa: F401  (sb: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,34 @@ def test_codes_of_sums_that_32_bits_do_not_hold(sb, n, d, dtype, apart, place): 
     step = torch.exp2(torch.clamp(torch.frexp(v)[1] - 1, min=-6).double() - 3)
     assert torch.equal(out.double(), torch.round(v / step) * step)
     assert into is None or torch.equal(into, total)
+
+
+@pytest.mark.parametrize("n,d", [(6, 100), (3, 2560), (5, 40000), (2100, 130), (7, 5)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size,gain_size", [(2.0 ** 50, 2.0 ** 83), (2.0 ** -60, 2.0 ** -80)])
+def test_outputs_whose_products_leave_32_bits(sb, n, d, dtype, size, gain_size):  # noqa: F811
+    """gain rstd sum is in range, gain sum alone is not."""
+    import torch
+    x, gain = some(dtype, n, d, size, 5), gain_of(d, gain_size)
+    out = torch.zeros_like(x)
+    sb.spiral_add_rmsnorm(x, None, gain, 0.0, out)
+    p, rstd = exact(x, gain, 0.0)
+    want = p * rstd
+    assert torch.isfinite(want.to(out.dtype)).all()
+    half = HALF[dtype]
+    assert ((out.double() - want).abs() <= (half + U * (d / 128 + 24)) * want.abs() * (1 + half) + LEAST[dtype]).all()
+
+
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size,gain_size", [(2.0 ** -60, 2.0 ** 83), (2.0 ** 55, 2.0 ** -85)])
+def test_heads_whose_gain_over_rms_leaves_32_bits(sb, hd, dtype, size, gain_size):  # noqa: F811
+    """At position 0 a head's output is its norm."""
+    import torch
+    x, gain = some(dtype, 50, 5 * hd, size, hd).unflatten(1, (5, hd)), gain_of(hd, gain_size)
+    out = torch.zeros_like(x)
+    sb.spiral_norm_rope(x[:, :4], x[:, 4:], gain, gain, 0.0, 1e4, torch.zeros(50, dtype=torch.int32, device="cuda"), out[:, :4], out[:, 4:])
+    want = x.double() * gain.double() / x.double().square().mean(2, keepdim=True).sqrt()
+    assert torch.isfinite(want.to(out.dtype)).all()
+    half = HALF[dtype]
+    assert ((out.double() - want).abs() <= (half + U * (hd / 32 + 32)) * want.abs() * (1 + half) + LEAST[dtype]).all()
