@@ -376,7 +376,7 @@ int spiral_policy_gradient(const void* dev_logits, int dtype, long long row_stri
  * the sums of dk and dv also over the query heads that share the kv head.  Nothing that a position does not see reaches its results, NaN and
  * infinities included, and rows behind the last sequence are neither read nor written.  Sums and the softmax are fp32; p and t are
  * rounded to the operands' type before they are multiplied (in fp16 a t below 2^-25 is 0: scale the loss as half precision wants it; p has half precision's 11 bits down to 2^-26 in dv, and
- * in out down to 2^-14 of the row's largest), outputs
+ * in out down to 2^-21 of the row's largest), outputs
  * and gradients once at the end (in fp16 what passes its range is infinite, so that a loss scale that is too large shows).  Results repeat bit for bit.  A sequence's out, lse and dq do not depend on the other sequences of the call; of dk and dv the order in which a group's
  * heads are added follows from the call's lengths (few and long ones: some heads by workgroups of their own), so that they may differ by the rounding of fp32 sums.
  *

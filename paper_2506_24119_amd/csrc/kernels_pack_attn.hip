@@ -287,6 +287,10 @@ template <int TOKENS> struct Unit {
     }
 };
 
+// Powers of two that weights reach before the reference moves, and that the largest has when it has moved.  Half precision's normal numbers end at 2^-14 and at 2^16: there the
+// largest is 2^7 at least, so that weights keep their 11 bits down to 2^-21 of it.
+template <class T> constexpr float kMost = std::is_same_v<T, _Float16> ? 15.f : 8.f;
+template <class T> constexpr float kTop = std::is_same_v<T, _Float16> ? 7.f : 0.f;
 // Stages of 32 tokens, of which the wave's last is the one on the diagonal.  Three workgroups share a compute unit, and what one waits for (its tiles, its barrier, the
 // matrix pipe, its exponentials) the others fill: two of them with stages of 64 tokens, the next stage's scores made under the weights of this one, took
 // 1,160 us where this took 1,054 (16 sequences of U[1024, 4096], 32 heads on 8), 164 where it took 143 (24 of U[256, 1024]).
@@ -334,8 +338,8 @@ __global__ __launch_bounds__(256, 3) void pack_forward_kernel(PackArgs a) {
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);
         mx = fmaxf(__int_as_float(both[0]), __int_as_float(both[1])) * a.scale_log2e;
-        if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {          // the reference moves only where weights would pass 2^8
-            const float m_new = fmaxf(m, mx), shrink = __builtin_amdgcn_exp2f(m - m_new);
+        if (__builtin_amdgcn_ballot_w64(mx > m + kMost<T>) != 0) {     // the reference moves only where weights would pass 2^kMost
+            const float m_new = fmaxf(m, mx - kTop<T>), shrink = __builtin_amdgcn_exp2f(m - m_new);
             l *= shrink;
 #pragma unroll
             for (int d = 0; d < DT; ++d)

@@ -40,3 +40,24 @@ def test_values_of_small_weights(sb, dtype, hq, hkv, hd, undefined):  # noqa: F8
     for x in c.host("dq", "dk")[:2 * (not undefined)]:
         assert np.isfinite(x).all()
     c.free()
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 2, 32), (2, 2, 64), (7, 1, 128)])
+def test_outputs_of_small_weights(sb, dtype, hq, hkv, hd):  # noqa: F811
+    """A first token that takes nearly all and is 0 itself: what remains are the others, of 2^-20 of its weight each, all rounded alike."""
+    import torch
+    lens = [200, 33, 500]
+    c = Call(sb, lens, hq, hkv, hd, dtype, seed=67)
+    c.q[:, :, 0] = 4.0
+    c.k.zero_()
+    first = torch.tensor([0, 200, 233], device="cuda")
+    c.k[first, :, 0] = 14.03 * float(np.sqrt(hd)) / 4.0
+    c.v[first] = 0.0
+    c.forward()
+    torch.cuda.synchronize()
+    half = HALF[dtype]
+    q, k, v, out = c.host("q", "k", "v", "out")
+    want, size = (ob.attention(q, k, x, lens, c.scale)[0] for x in (v, np.abs(v)))
+    close(out, want, (half + 2 * c.errors().T[:, :, None]) * size + half * np.abs(want) * (1 + half) + 2.0 ** -25, "out")
+    c.free()
