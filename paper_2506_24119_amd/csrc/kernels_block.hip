@@ -630,7 +630,11 @@ hipError_t rope_any(const RopeArgs& a, const RopeFreq& f, int dtype, int hd, boo
 hipError_t launch_add_norm_rows(const NormRowsArgs& a, int dtype, hipStream_t s) {
     return dtype == SPIRAL_DTYPE_FP32 ? add_norm_of<float>(a, s) : dtype == SPIRAL_DTYPE_BF16 ? add_norm_of<__bf16>(a, s) : add_norm_of<_Float16>(a, s);
 }
-size_t norm_grad_workspace_bytes(long long n_rows, int d) { return (size_t)std::min<long long>(n_rows, kGradBlocks) * d * 4; }      // of any type
+// as many parts as any type's rows of that width are cut into
+size_t norm_grad_workspace_bytes(long long n_rows, int d) {
+    const bool long_rows = d < 8 || d > 4 * 512 * std::max(kMostGradVecs<float>, kMostGradVecs<__bf16>);
+    return (size_t)std::min<long long>(n_rows, long_rows ? kLongParts : kGradBlocks) * d * 4;
+}
 hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, hipStream_t s) {
     return dtype == SPIRAL_DTYPE_FP32 ? norm_grad_of<float>(a, s) : dtype == SPIRAL_DTYPE_BF16 ? norm_grad_of<__bf16>(a, s) : norm_grad_of<_Float16>(a, s);
 }

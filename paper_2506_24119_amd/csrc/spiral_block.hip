@@ -99,7 +99,7 @@ extern "C" int spiral_attention_plan_create(const int32_t* host_lens, int B, int
 
 extern "C" void spiral_attention_plan_free(spiral_attention_plan* plan) { delete plan; }
 
-// a matrix of the call: its pointer and stride, and as rows for the test of shared elements
+// pointer and stride of a matrix of the call
 static bool matrix_ok(const void* p, long long stride, long long width) {
     return p && aligned(p, 16) && stride >= width && stride % 8 == 0 && stride <= (1ll << 22);
 }
@@ -197,7 +197,7 @@ extern "C" int spiral_add_rmsnorm(const void* dev_x, long long x_stride, const v
     if (any_meet(rows, 7)) return fail(SPIRAL_ERR_INVALID_ARG, "add_rmsnorm: a buffer that is written overlaps another");
     NormRowsArgs a = {};
     a.x = dev_x; a.x_stride = x_stride; a.residual = dev_residual; a.residual_stride = residual_stride; a.gain = dev_gain;
-    a.n_rows = n_rows; a.d = d; a.eps = eps; a.out_dtype = out_dtype;
+    a.n_rows = n_rows; a.d = d; a.eps = eps;
     a.out = dev_out; a.out_stride = out_stride; a.sum = dev_sum; a.sum_stride = sum_stride; a.out_scale = dev_out_scale; a.rstd = dev_rstd;
     return done(launch_add_norm_rows(a, dtype, (hipStream_t)stream), "add_rmsnorm");
 }

@@ -274,7 +274,7 @@ struct NormRowsArgs {
     const void *x, *residual; long long x_stride, residual_stride;
     const float* gain;
     long long n_rows;
-    int32_t d, out_dtype;
+    int32_t d;
     float eps;
     void *out, *sum; long long out_stride, sum_stride;      // sum: or null
     float *out_scale, *rstd;                  // or null
