@@ -319,7 +319,8 @@ __global__ __launch_bounds__(256, 3) void pack_forward_kernel(PackArgs a) {
     for (int d = 0; d < DT; ++d) acc[d] = zeros();
     float m = kLeast, l = 0.f;
     for (int st = 0; st < w.stages; ++st) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // This stage's tiles are here, and those that the next loads go over have been read (a barrier does not wait for either by itself).
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (st + 1 < w.stages) bring(st + 1);
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
     const int limit = w.pos0 + l32;
 
     auto arrive = [&](int st) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (st + 1 < w.stages) bring(st + 1);
