@@ -60,8 +60,8 @@ __device__ __forceinline__ uint32_t to_e4m3x4(const float* v) {
 // The sum itself is one of 64 bits where its parts are of 32 (in 32 bits half as many codes were others as with no 64 bits at all); of 16-bit parts 32 bits hold it, but for the last
 // bits of parts 2^13 and more apart: one code in 10^8, for which the kernel would take 54 us.
 template <class T> constexpr bool kWideSum = sizeof(T) == 4;
-// eight of 2^-24: the sum, its product, both of the largest, the factor, its margin and their product are off by one each
-constexpr float kOff = 0x1p-21f;
+// six of 2^-24: the largest, the factor, its margin, the product and their product are off by one each; eight where the sum and that of the largest are, too
+template <class T> constexpr float kOff = kWideSum<T> ? 0x1p-21f : 0x1.8p-22f;
 __device__ __forceinline__ double exact_product(float x, float y) { return (double)x * y; }
 __device__ __forceinline__ double exact_product(float x, float residual, float y) {
     const float sum = x + residual;
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
         if (OUT8) {
             typedef uint32_t Codes __attribute__((ext_vector_type(2)));
             most = over_row<WAVES>(bad != bad ? NAN : most, s, Most());
-            const float factor = code_factor(most, rstd), less = factor * (1.f - kOff), more = factor * (1.f + kOff);
+            const float factor = code_factor(most, rstd), less = factor * (1.f - kOff<T>), more = factor * (1.f + kOff<T>);
             if (mine.t == 0) a.out_scale[r] = code_scale(most, rstd);
             uint32_t differ = !in_32_bits(most, rstd);
             asm volatile("" : "+s"(gain));        // read again, not kept
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(kThreads, NV <= 2 ? 4 : NV <= 5 ? 3 : 2) void add_n
                             for (int e = 0; e < 8; ++e) {
                                 const float p = h[v][e] * g[e];
                                 below[e] = p * less, above[e] = p * more;
-                                if (fabsf(p) >= most * (1.f - kOff)) largest |= 1u << (8 * v + e);
+                                if (fabsf(p) >= most * (1.f - kOff<T>)) largest |= 1u << (8 * v + e);
                             }
 #pragma unroll
                             for (int b = 0; b < 8; b += 4) {
