@@ -447,15 +447,20 @@ __global__ __launch_bounds__(256, 2) void pack_dq_kernel(PackArgs a) {
     if (w.my_stages == 1) {
         // All that the rows see is here, so that D can be had as sum p dp.  From `out`, whose rounding is in it, it is off by 2^-9 of what dp - D, where a
         // row sees few tokens, nearly cancels to (dq of sequences of 2 to 20 tokens: 0.4 % off, now 0.24).
-        float sum = 0.f;
+        // Divided by sum p, which the rounding of lse leaves off 1 by 2^-24 of a large score: where one token has nearly all the weight, that times dp would stand for dp - D.
+        float sum = 0.f, weight = 0.f;
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             f32x16 s, dp;
             products(s, dp, 0, half);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += hidden(0, half, r) ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2e, -lse2)) * dp[r];
+            for (int r = 0; r < 16; ++r) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2e, -lse2));
+                sum += hidden(0, half, r) ? 0.f : p * dp[r];
+                weight += hidden(0, half, r) ? 0.f : p;
+            }
         }
-        delta = there ? sum + __shfl_xor(sum, 32, 64) : 0.f;
+        delta = there ? (sum + __shfl_xor(sum, 32, 64)) / (weight + __shfl_xor(weight, 32, 64)) : 0.f;
     }
     auto both_products = [&](int st, int half, auto cut) {
         f32x16 s, dp;
