@@ -8,8 +8,8 @@
  * i.e. an untruncated categorical), plus the role-conditioned advantage
  * estimation baseline (Sec. 3, RAE equation; Alg. 1, policy-optimisation loop), and
  * what closes an update of the policy: a draw with its log-probability, the gradient
- * of the objective in the logits, what a decoder block has between its matrix products
- * (attention, norms, rotation) forward and backward, AdamW.
+ * of the objective in the logits, attention, norms and rotation of a decoder block forward
+ * and backward (its matrix products and its activation are the caller's), AdamW.
  *
  * General rules
  *  - Every function returns SPIRAL_OK (0) or a negative SPIRAL_ERR_* code; it
@@ -411,7 +411,7 @@ int    spiral_attention_backward(const spiral_attention_plan* plan, const void* 
  *     sum = x + residual ,  rstd = (mean_c sum_c^2 + eps)^(-1/2) ,  out_c = gain_c rstd sum_c                a row of d elements each
  * in fp32; `sum` is rounded where it is written, not before it is normed.  dev_residual NULL: sum = x (dev_sum, where given, is a copy of it).
  * out_dtype: that of x, or SPIRAL_DTYPE_E4M3: codes under an fp32 scale a row, out = code * dev_out_scale[row], scale = the row's largest |out| / 448
- * (0, with codes of 0, where that is at most 1e-30), codes rounded to nearest even from gain sum 448 / its largest in 64 bits, the sum of FP32 too; a row whose sum or gain has a NaN or an infinity has scale NaN and codes NaN.
+ * (0, with codes of 0, where that is at most 1e-30; such rows are for an 8-bit product of the caller's, no call of this library reads them), codes rounded to nearest even from gain sum 448 / its largest in 64 bits, the sum of FP32 too; a row whose sum or gain has a NaN or an infinity has scale NaN and codes NaN.
  * dev_x, dev_residual, dev_sum, dev_out: [n_rows, d], rows `stride` elements apart, aligned to an element; x, residual and sum of `dtype` (FP32, BF16, FP16).  dev_gain
  * fp32 [d].  dev_sum, dev_rstd (fp32 [n_rows]) may be NULL; dev_sum may be dev_x or dev_residual itself (same pointer and stride).
  * Backward, for gradients dout of out and dsum of sum (the residual branch's; NULL: none), with the sum and rstd that the forward call wrote:

@@ -1,5 +1,4 @@
-// What a decoder block has beside its matrix products and its attention, for the learner: addition to the residual stream with RMSNorm, and the norm and rotation of the q and k heads,
-// each forward and backward.
+// Rows of a decoder block, for the learner: addition to the residual stream with RMSNorm, and the norm and rotation of the q and k heads, each forward and backward.
 //
 // All are bound by memory: a row's elements are read once, kept in registers while their sum is formed, and written once.  Figures, other inputs each time (a copy of 4 GiB moves 4.8
 // TB/s): addition + norm to 8 bits, 15,271 rows of 2,560 bf16, 274 MB in 51 us; gradient, 16,384 rows of 3,584 bf16, 470 MB in 97 us and 4.4 for the gain's sums; heads 32 + 8

@@ -11,8 +11,9 @@
 // Three kernels, seven products where the mathematics has five in the backward pass (s and dp are made twice): one kernel for all would have to add dq from many
 // workgroups, by atomics whose order changes results or by partial sums that take longer than the two products (16 sequences of U[1024, 4096]: 15 GB, 3.1 ms).
 //
-// Bound: the chip's power.  The compute units are busy, the matrix pipes 53 to 62 % of their time at 1.9 GHz; with zeros for all inputs the same launches take 17, 23 and 27 % less
-// time.  16 sequences of U[1024, 4096], 32 heads on 8, hd 128, bf16 (41 k rows): forward 1.03 ms (1.04 PFLOP/s), dq 1.69 (0.95), dk and dv 2.12 (1.01 of what is computed);
+// Bound: the chip's power, and waits.  The compute units are busy, the matrix pipes 54 to 62 % of their time, at 1.9 GHz in place of 2.4; with zeros for all inputs the same launches take
+// 17, 23 and 27 % less time.  Waves wait for 31 to 36 % of their cycles, for operands from LDS for 4 to 6 %; how much of the rest is for stages' loads and how much at their barriers is
+// not told apart.  16 sequences of U[1024, 4096], 32 heads on 8, hd 128, bf16 (41 k rows): forward 1.02 ms (1.04 PFLOP/s), dq 1.72 (0.93), dk and dv 2.08 (1.03 of what is computed; cards differ by 4 %);
 // a library product of 16384^3 makes 1.35.  A row alone by one wave, token by token, took 534 ms for the three.
 // On the way: bank-free tiles (64 banks, not 32, serve a wave's reads) 5.1 -> 2.65 ms of dk and dv, whose addresses had been spilled; values in LDS and stages of 32 rows there 2.65 -> 2.24; three
 // forward workgroups a compute unit 1.16 -> 1.06.  Without effect, within 2 %: products interleaved with exponentials instruction by instruction, operand reads further ahead, the two score
