@@ -289,8 +289,8 @@ template <int TOKENS> struct Unit {
 };
 
 // Powers of two that weights reach before the reference moves, and that the largest has when it has moved.  Half precision's normal numbers end at 2^-14 and at 2^16: there the
-// largest is 2^7 at least, so that weights keep their 11 bits down to 2^-21 of it.
-template <class T> constexpr float kMost = std::is_same_v<T, _Float16> ? 15.f : 8.f;
+// largest is 2^7 at least, so that weights keep their 11 bits down to 2^-21 of it, and 2^12 at most: scores of 2^26 are off by 4 themselves.
+template <class T> constexpr float kMost = std::is_same_v<T, _Float16> ? 12.f : 8.f;
 template <class T> constexpr float kTop = std::is_same_v<T, _Float16> ? 7.f : 0.f;
 // Stages of 32 tokens, of which the wave's last is the one on the diagonal.  Three workgroups share a compute unit, and what one waits for (its tiles, its barrier, the
 // matrix pipe, its exponentials) the others fill: two of them with stages of 64 tokens, the next stage's scores made under the weights of this one, took

@@ -61,3 +61,24 @@ def test_outputs_of_small_weights(sb, dtype, hq, hkv, hd):  # noqa: F811
     want, size = (ob.attention(q, k, x, lens, c.scale)[0] for x in (v, np.abs(v)))
     close(out, want, (half + 2 * c.errors().T[:, :, None]) * size + half * np.abs(want) * (1 + half) + 2.0 ** -25, "out")
     c.free()
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_equal_scores_of_ten_millions(sb, dtype, hd):  # noqa: F811
+    """One bit of a score is a unit there, but equal keys have the same bits: every row's output is the mean of what it sees, none of its weights past half precision's range."""
+    import torch
+    lens = [150, 40]
+    c = Call(sb, lens, 4, 2, hd, dtype, seed=73)
+    c.q.zero_()
+    c.k.zero_()
+    c.q[:, :, 0], c.k[:, :, 0] = 3000.0, 2.0 ** 15 * float(np.sqrt(hd / 64))
+    c.forward()
+    torch.cuda.synchronize()
+    half = HALF[dtype]
+    v, out = (x.astype(np.float64) for x in c.host("v", "out"))
+    for a, n in ((0, 150), (150, 40)):
+        count = np.arange(1, n + 1)[:, None, None]
+        want, size = (np.repeat(np.cumsum(x[a:a + n], axis=0) / count, 2, axis=1) for x in (v, np.abs(v)))
+        close(out[a:a + n], want, (half + 2.0 ** -24 * (n + 64)) * size + half * np.abs(want) * (1 + half) + 2.0 ** -25, "out")
+    c.free()
